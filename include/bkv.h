@@ -311,6 +311,75 @@ typedef struct {
 } bkv_rows;
 bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes, hipStream_t stream);
 
+/* ---- Attention over the cache --------------------------------------------------
+ * What the cache is kept for: the newest T tokens of every sequence attend to
+ * it, and, optionally, every cached token collects the weight it was given,
+ * which bkv_evict_mass ranks by.  With l_tj = scale * <q_t, k_j> (fp32; scale 0
+ * selects fp32(1/sqrt(D))), query head hq = h * G + g reading kv-head h:
+ *   lse_t = log sum_j exp(l_tj),   out_t = sum_j exp(l_tj - lse_t) v_j,
+ *   mass_j += sum over g and t of exp(l_tj - lse_t),
+ * over the keys that query t sees: j < len, and with BKV_ATTEND_CAUSAL (the T
+ * queries are the cache's newest tokens, oldest first) j <= len - T + t.  A
+ * query that sees no key has out 0 and lse -inf and gives no weight.
+ *   q, out  [B, Hq, T, D] post-RoPE queries and their outputs, dtype of the
+ *           dims; out must not overlap any input.
+ *   K, V    [B, Hkv, N_cap, D] (may be NULL when N is 0); 0 <= N <= N_cap.
+ *   lens    optional device [B] int32: sequence b holds lens[b] tokens, taken
+ *           as 0 below 0 and as N above N; NULL: N each.
+ *   lse     optional [B, Hq, T] fp32 (NULL to skip).
+ *   mass    optional [B, Hkv, N_cap] fp32, read and written for the tokens
+ *           j < len only (NULL to skip).
+ * The rows of K, V at or past len are not read, whatever they hold.  Sums,
+ * maxima and normalisers are fp32 and no sum depends on the launch; weights
+ * enter the matrix cores as bf16 for bf16 caches.  Of the dims, B, Hq, Hkv, D,
+ * N, N_cap and dtype are used; the others need only pass bkv_validate.  N may
+ * be 0 (then every query sees nothing).  B * Hq * T < 2^31; T == 0 or B == 0
+ * enqueues nothing.
+ * The workspace needs no initialisation and holds nothing between calls; its
+ * size covers every N <= N_cap.  mass: whether calls pass a mass; groups and
+ * P_cap: those of bkv_attend_shared (0, 0 for bkv_attend).  0 bytes: none is
+ * needed, or the arguments are invalid. */
+#define BKV_ATTEND_CAUSAL 1
+size_t bkv_attend_workspace_bytes(const bkv_dims* d, int32_t T, int32_t mass, int32_t groups, int32_t P_cap);
+bkv_status bkv_attend(const bkv_dims* d, int32_t flags, const void* q, int32_t T, const void* K, const void* V,
+                      const int32_t* lens, float scale, void* out, float* lse, float* mass, void* ws, size_t ws_bytes,
+                      hipStream_t stream);
+
+/* bkv_attend for sequences that share a prefix held once: the batch is
+ * `groups` groups of B / groups consecutive sequences (answers to one prompt;
+ * stacked layers are groups), and every query of a group's sequences sees all
+ * of the group's prefix, then its own cache as in bkv_attend.  One softmax
+ * spans both.  The prefix is read once for all rows of a group.
+ *   PK, PV  [groups, Hkv, P_cap, D], dtype of the dims (may be NULL when P is
+ *           0); 0 <= P <= P_cap, P_cap >= 1.
+ *   p_lens  optional device [groups] int32: group i's prefix holds p_lens[i]
+ *           tokens, taken as 0 below 0 and as P above P; NULL: P each.
+ * mass collects the weights of the sequences' own tokens (the prefix is never
+ * evicted), under the normaliser of both.  groups >= 1 divides B. */
+bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32_t groups, const void* PK,
+                             const void* PV, int32_t P, int32_t P_cap, const int32_t* p_lens, const void* K,
+                             const void* V, const int32_t* lens, float scale, void* out, float* lse, float* mass,
+                             void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Eviction by accumulated attention weight: bkv_topk's rule on mass [B, Hkv,
+ * N_cap] in the place of the scores (the first n_prefix and the last W tokens,
+ * then the largest masses, ties to the lower index, -0 equal to +0; a NaN of
+ * either sign ranks by its bits, beyond the infinity of its sign), and K, V
+ * and mass are compacted in place, bit for bit: row i < n = min(budget, N)
+ * becomes row kept[i].
+ *   flags 0: order preserved, as bkv_compact; kept is ascending.
+ *   BKV_EVICT_FILL: the layout of bkv_compact_fill, any n; kept[i] is the old
+ *           row now at row i (what bkv_compact_fill calls src_of).
+ * Rows of K and V from n on are left as they were; mass[n..N) becomes 0, so
+ * that tokens appended there start from nothing.  N <= budget changes nothing.
+ *   kept    optional [B, Hkv, n] int32 (NULL to skip).
+ * Workspace: bkv_mass_workspace_bytes(d), which covers every N <= N_cap,
+ * initialised by bkv_workspace_init and usable with bkv_device_status. */
+#define BKV_EVICT_FILL 1
+size_t bkv_mass_workspace_bytes(const bkv_dims* d);
+bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, float* mass, int32_t* kept, void* ws,
+                          size_t ws_bytes, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* bkv_status_string(bkv_status s);
 

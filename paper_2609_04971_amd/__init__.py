@@ -25,9 +25,13 @@ OP_BEACON_UPDATE, OP_SCORE, OP_TOPK, OP_COMPACT, OP_EVICT = range(5)
 EXPORTS = ("bkv_validate", "bkv_workspace_bytes", "bkv_workspace_init", "bkv_device_status",
            "bkv_beacon_update", "bkv_score", "bkv_topk", "bkv_compact", "bkv_evict",
            "bkv_score_ex", "bkv_evict_ex", "bkv_fps", "bkv_fps_gather", "bkv_status_string",
-           "bkv_abi_version", "bkv_compact_fill", "bkv_evict_noalloc", "bkv_append_rows")
+           "bkv_abi_version", "bkv_compact_fill", "bkv_evict_noalloc", "bkv_append_rows",
+           "bkv_attend", "bkv_attend_shared", "bkv_attend_workspace_bytes", "bkv_evict_mass",
+           "bkv_mass_workspace_bytes")
 APPEND_MAX = 4
 SCORE_MEAN, SCORE_CAUSAL = 1, 2
+ATTEND_CAUSAL = 1
+EVICT_FILL = 1
 
 
 class Dims(ctypes.Structure):
@@ -95,6 +99,12 @@ _SIGS = {
     "bkv_fps": ([_I] * 5 + [_P, _I, _P, _P], ctypes.c_int),
     "bkv_fps_gather": ([_I] * 5 + [_P, _I, _P, _I, _I, _P, _P, _P], ctypes.c_int),
     "bkv_append_rows": ([ctypes.POINTER(Rows), _I, _I, _P], ctypes.c_int),
+    "bkv_attend_workspace_bytes": ([_D] + [_I] * 4, _S),
+    "bkv_attend": ([_D, _I, _P, _I, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P, _S, _P], ctypes.c_int),
+    "bkv_attend_shared": ([_D, _I, _P, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P, _S, _P],
+                          ctypes.c_int),
+    "bkv_mass_workspace_bytes": ([_D], _S),
+    "bkv_evict_mass": ([_D, _I, _P, _P, _P, _P, _P, _S, _P], ctypes.c_int),
     "bkv_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "bkv_abi_version": ([], ctypes.c_int32),
 }
@@ -301,6 +311,95 @@ def evict_noalloc(d: Dims, K, V, q_win, beacons, counts, kept=None, scores=None,
         _ptr(row_lse, (d.B, d.Hkv, d.C + d.G * d.W), torch.float32, "row_lse", optional=True),
         _ptr(status, (1,), torch.int32, "status", optional=True), _stream())
     _check(st, "bkv_evict_noalloc")
+
+
+# ---- attention over the cache, eviction by accumulated weight ----------------------
+def _here(t, name):
+    """Tensors of another GPU than the current one are refused: work goes to
+    the current device's stream."""
+    if t is not None and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on GPU {t.get_device()}, the current device is {torch.cuda.current_device()}")
+
+
+def attend_workspace(d: Dims, T: int = 1, mass: bool = False, groups: int = 0, P_cap: int = 0, device="cuda"):
+    """Workspace of attend (or, with groups and P_cap, attend_shared) for T
+    queries on `d`, for every N <= N_cap and P <= P_cap; mass: whether calls
+    pass a mass.  Nothing in it has to be initialised or outlives a call."""
+    n = int(lib().bkv_attend_workspace_bytes(ctypes.byref(d), int(T), int(bool(mass)), int(groups), int(P_cap)))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def _attend_args(d, q, K, V, out, lens, lse, mass):
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a tensor [B, Hq, T, D]")
+    T = q.shape[2]
+    cache = (d.B, d.Hkv, d.N_cap, d.D)
+    p = (_ptr(q, (d.B, d.Hq, T, d.D), _tdtype(d), "q"), _ptr(K, cache, _tdtype(d), "K"), _ptr(V, cache, _tdtype(d), "V"),
+         _ptr(lens, (d.B,), torch.int32, "lens", optional=True),
+         _ptr(out, (d.B, d.Hq, T, d.D), _tdtype(d), "out"),
+         _ptr(lse, (d.B, d.Hq, T), torch.float32, "lse", optional=True),
+         _ptr(mass, cache[:3], torch.float32, "mass", optional=True))
+    for t, name in ((q, "q"), (K, "K"), (V, "V"), (lens, "lens"), (out, "out"), (lse, "lse"), (mass, "mass")):
+        _here(t, name)
+    return T, p
+
+
+def attend(d: Dims, q, K, V, out, ws, lens=None, lse=None, mass=None, scale: float = 0.0, causal: bool = False):
+    """Attention of the newest T queries q [B,Hq,T,D] (post-RoPE) over the
+    cache: out [B,Hq,T,D] and, where given, lse [B,Hq,T] written, and every
+    cached token's weights added to mass [B,Hkv,N_cap].  lens [B] int32:
+    ragged lengths.  causal: query t sees the tokens up to its own."""
+    T, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass)
+    wp, wn = _ws(ws)
+    _here(ws, "workspace")
+    st = lib().bkv_attend(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, kp, vp, lp, float(scale), op, ep, mp,
+                          wp, wn, _stream())
+    _check(st, "bkv_attend")
+
+
+def attend_shared(d: Dims, q, PK, PV, K, V, out, ws, P: int | None = None, p_lens=None, lens=None, lse=None, mass=None,
+                  scale: float = 0.0, causal: bool = False):
+    """attend() for groups of consecutive sequences that share a prefix PK, PV
+    [groups,Hkv,P_cap,D], of which the first P tokens are valid (default: all;
+    p_lens [groups] int32: ragged).  mass collects the own tokens' weights."""
+    if not isinstance(PK, torch.Tensor) or PK.dim() != 4:
+        raise ValueError("PK must be a tensor [groups, Hkv, P_cap, D]")
+    groups, P_cap = PK.shape[0], PK.shape[2]
+    T, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass)
+    shape = (groups, d.Hkv, P_cap, d.D)
+    pk, pv = _ptr(PK, shape, _tdtype(d), "PK"), _ptr(PV, shape, _tdtype(d), "PV")
+    pl = _ptr(p_lens, (groups,), torch.int32, "p_lens", optional=True)
+    wp, wn = _ws(ws)
+    for t, name in ((PK, "PK"), (PV, "PV"), (p_lens, "p_lens"), (ws, "workspace")):
+        _here(t, name)
+    st = lib().bkv_attend_shared(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, groups, pk, pv,
+                                 P_cap if P is None else int(P), P_cap, pl, kp, vp, lp, float(scale), op, ep, mp, wp, wn,
+                                 _stream())
+    _check(st, "bkv_attend_shared")
+
+
+def mass_workspace(d: Dims, device="cuda") -> torch.Tensor:
+    """Allocate and initialise a workspace of evict_mass, for every N <= N_cap."""
+    n = int(lib().bkv_mass_workspace_bytes(ctypes.byref(d)))
+    ws = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    workspace_init(d, ws)
+    return ws
+
+
+def evict_mass(d: Dims, K, V, mass, ws, kept=None, fill: bool = False):
+    """Keep the prefix, the last W tokens and the largest masses of each head:
+    K, V and mass [B,Hkv,N_cap] compacted in place (fill: the layout of
+    compact_fill), mass 0 from the budget to N.  kept [B,Hkv,min(budget,N)]
+    int32, optional, receives the old row now at each row."""
+    cache = (d.B, d.Hkv, d.N_cap, d.D)
+    kp, vp = _ptr(K, cache, _tdtype(d), "K"), _ptr(V, cache, _tdtype(d), "V")
+    mp = _ptr(mass, cache[:3], torch.float32, "mass")
+    op = _ptr(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", optional=True)
+    wp, wn = _ws(ws)
+    for t, name in ((K, "K"), (V, "V"), (mass, "mass"), (kept, "kept"), (ws, "workspace")):
+        _here(t, name)
+    st = lib().bkv_evict_mass(ctypes.byref(d), EVICT_FILL if fill else 0, kp, vp, mp, op, wp, wn, _stream())
+    _check(st, "bkv_evict_mass")
 
 
 # ---- appending a step's rows -------------------------------------------------------

@@ -1,0 +1,91 @@
+// Shared by the attention kernels (attend.hip, attend_tile.hip): what a call
+// reads and writes, how its work is cut, and the row arithmetic.
+#pragma once
+
+#include "device_common.h"
+#include "internal.h"
+
+namespace bkv {
+namespace attend {
+
+// Keys that many query rows attend to: one sequence's cache (own), or the
+// prefix of a group of sequences.  A unit is one (sequence or group, kv-head)
+// pair.  Its rows are those of seqs consecutive sequences, R = G*T each, in
+// the order sequence, query, head of the kv-head's group; a unit's rows are
+// cut into nrb row blocks and its keys into ns splits of `chunk` keys, and
+// every (unit, row block, split) is one work item.
+struct Segment {
+    const void* K;
+    const void* V;
+    const int32_t* lens;  // valid keys of each sequence or group, or null: n of all
+    int n, cap;           // keys at most; keys allocated, the unit stride of K and V
+    int units, seqs, rows;
+    int nrb, ns, chunk;
+    int split0;           // its first partial of every row
+    int causal;
+};
+
+struct Args {
+    Segment seg[2];       // 0 the prefix (units 0 without one), 1 the sequences' own caches
+    int items0;           // work items of seg[0]
+    const void* q;
+    void* out;
+    float* lse;           // or null
+    float* mass;          // or null
+    float* part_o;        // [row][ns][D] unnormalised sums of exp2(l2 - m) v
+    float* part_ml;       // [row][ns][2] m and z = sum of exp2(l2 - m)
+    float* row_lse2;      // [row] log2-normaliser, +inf for a row that sees nothing
+    float* logits;        // [own unit][R][lstride] l2 = l log2(e), -inf where not seen
+    int lstride;
+    int Hq, Hkv, G, T, R, D;
+    int N, N_cap;
+    int rows;             // B * Hq * T
+    int ns;               // partials per row; 1: the outputs are written directly
+    float scale2;         // scale * log2(e)
+};
+
+// How a call is cut.  Everything but the splits depends on the capacities
+// only, and the splits are at most those of the capacities, so a workspace
+// serves every N <= N_cap and P <= P_cap.
+struct Plan {
+    bool own_tile, pre_tile;  // which kernel takes the segment
+    int own_ns, own_chunk, pre_ns, pre_chunk;
+    int own_ns_cap, pre_ns_cap;
+    size_t part_o, part_ml, row_lse2, logits, end;
+    int lstride_cap;
+};
+Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap);
+
+// A row of a segment's unit: which query it is.
+struct Row {
+    int t;          // query, 0..T-1
+    long long gr;   // row of the partials: (sequence, kv-head, query, head of the group)
+    long long q;    // element offset of the query and of its output
+    long long lse;  // offset of its normaliser
+};
+__device__ __forceinline__ Row decode_row(const Args& a, int unit, int seqs, int rr) {
+    const int h = unit % a.Hkv, grp = unit / a.Hkv;
+    const int b = grp * seqs + rr / a.R, r = rr % a.R;
+    const int t = r / a.G, g = r - t * a.G;
+    Row x;
+    x.t = t;
+    x.gr = ((long long)b * a.Hkv + h) * a.R + r;
+    x.lse = ((long long)b * a.Hq + h * a.G + g) * a.T + t;
+    x.q = x.lse * a.D;
+    return x;
+}
+
+// Lowest running maximum: finite, so that exp2(-inf - m) is 0 and not NaN in
+// a row that has seen nothing yet.
+constexpr float kLowest = -3.402823466e38f;
+
+}  // namespace attend
+
+// Segments (bit 0: prefix, bit 1: own) that the streaming kernel takes, in one launch.
+hipError_t launch_attend_stream(const attend::Args& a, int dtype, bool wide, hipStream_t s);
+// Joins the partials and, where the logits were kept, adds the weights to the mass.
+hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s);
+// Adds the weights to the mass from the queries and keys (R > 32).
+hipError_t launch_attend_mass(const attend::Args& a, int dtype, hipStream_t s);
+
+}  // namespace bkv

@@ -1,0 +1,539 @@
+// Attention of the newest queries over the cache, for gfx950: the streaming
+// kernel, the join of its partials, and the weights' sums.
+//
+// For a row (one query of one query head) with key logits l_j = scale q.k_j:
+//   lse = log sum_j exp(l_j),  out = sum_j exp(l_j - lse) v_j
+// over the keys it sees.  Everything is kept in log2 units, l2 = l log2(e),
+// so that an exponential is one v_exp_f32.  A pass over some of the keys
+// leaves m (their maximum), z = sum exp2(l2 - m) and o = sum exp2(l2 - m) v,
+// and two such partials join by
+//   M = max(m, m'), z <- z exp2(m - M) + z' exp2(m' - M), o likewise.
+#include "attend.h"
+
+namespace bkv {
+namespace attend {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---- one group of keys through the matrix cores ---------------------------------
+// Transposed products: S^T = K Q^T puts a row's logits into one lane column
+// (lane % 16 is the row, 4 (lane / 16) + i the key), which is the layout the
+// B operand of out^T = V^T P^T wants, so the weights never leave their lane.
+// The A operand V^T needs the keys of one coordinate in one lane.  V is
+// loaded by whole rows, D/16 consecutive coordinates a lane, and transposed
+// in registers: coordinate dd of the lane's keys is a byte permute of two
+// registers.  MFMA tile dd then holds the coordinates (D/16) m + dd, m the
+// lane column, and lane 16 g + row ends up with D/4 consecutive coordinates
+// of its row's sum.
+
+template <int D>
+struct Bf16 {
+    typedef uint16_t elem;
+    static constexpr int kKeys = 32;    // keys per group
+    static constexpr int kTiles = 2;    // S tiles of 16 keys
+    static constexpr int kKK = D / 32;  // 16-byte loads per lane and key tile
+    static constexpr int kDV = D / 16;
+    struct Q { dev::u32x4 v[kKK]; };
+    struct K { dev::u32x4 v[kTiles][kKK]; };
+    struct V { unsigned v[8][kDV / 2]; };
+
+    // Which 16-byte chunk of a row (in elements) load kk of lane group g takes.
+    __device__ static int chunk(int kk, int g) { return 32 * kk + 8 * g; }
+
+    __device__ static void load_k(K& k, const elem* base, int k0, int last, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        dev::static_for<kTiles>([&](auto ac) {
+            constexpr int a = decltype(ac)::value;
+            const elem* p = base + (long long)min(k0 + 16 * a + m, last) * D;
+            dev::static_for<kKK>([&](auto c) {
+                constexpr int kk = decltype(c)::value;
+                k.v[a][kk] = *reinterpret_cast<const dev::u32x4*>(p + chunk(kk, g));
+            });
+        });
+    }
+    __device__ static void load_v(V& v, const elem* base, int k0, int last, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        dev::static_for<8>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            const elem* p = base + (long long)min(k0 + 16 * (j / 4) + 4 * g + j % 4, last) * D + kDV * m;
+            if constexpr (kDV == 8) {
+                const dev::u32x4 x = *reinterpret_cast<const dev::u32x4*>(p);
+                dev::static_for<4>([&](auto c) { v.v[j][decltype(c)::value] = x[decltype(c)::value]; });
+            } else {
+                const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+                dev::static_for<2>([&](auto c) { v.v[j][decltype(c)::value] = x[decltype(c)::value]; });
+            }
+        });
+    }
+    __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const Q& q) {
+        dev::static_for<kTiles>([&](auto ac) {
+            constexpr int a = decltype(ac)::value;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            dev::static_for<kKK>([&](auto c) {
+                constexpr int kk = decltype(c)::value;
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k.v[a][kk]),
+                                                              __builtin_bit_cast(bf16x8_t, q.v[kk]), acc, 0, 0, 0);
+            });
+            s[a] = acc;
+        });
+    }
+    // o += V^T P^T.  The weights go in as two bf16 terms, high part and rest,
+    // so that their rounding (2^-17) stays below the output's own: the
+    // streaming kernel waits for memory, and the second product is free.
+    template <int RT>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
+        bf16x8_t hi[RT], lo[RT];
+        dev::static_for<RT>([&](auto rc) {
+            constexpr int rt = decltype(rc)::value;
+            dev::static_for<8>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                const float x = p[rt][j / 4][j % 4];
+                const __bf16 h = (__bf16)x;
+                hi[rt][j] = h;
+                lo[rt][j] = (__bf16)(x - (float)h);
+            });
+        });
+        dev::static_for<kDV>([&](auto dc) {
+            constexpr int dd = decltype(dc)::value;
+            constexpr unsigned sel = dd % 2 ? 0x07060302u : 0x05040100u;  // a half of two registers
+            dev::u32x4 t;
+            dev::static_for<4>([&](auto c) {
+                constexpr int i = decltype(c)::value;
+                t[i] = __builtin_amdgcn_perm(v.v[2 * i + 1][dd / 2], v.v[2 * i][dd / 2], sel);
+            });
+            const bf16x8_t a = __builtin_bit_cast(bf16x8_t, t);
+            dev::static_for<RT>([&](auto rc) {
+                constexpr int rt = decltype(rc)::value;
+                o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[rt], o[rt][dd], 0, 0, 0);
+                o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[rt], o[rt][dd], 0, 0, 0);
+            });
+        });
+    }
+    __device__ static void store(elem* p, float x) { *p = dev::f32_to_bf16_rne(x); }
+};
+
+template <int D>
+struct F32 {
+    typedef float elem;
+    static constexpr int kKeys = 16;
+    static constexpr int kTiles = 1;
+    static constexpr int kKK = D / 16;
+    static constexpr int kDV = D / 16;
+    struct Q { f32x4 v[kKK]; };
+    struct K { f32x4 v[1][kKK]; };
+    struct V { f32x4 v[4][kDV / 4]; };
+
+    __device__ static int chunk(int kk, int g) { return 16 * kk + 4 * g; }
+
+    __device__ static void load_k(K& k, const elem* base, int k0, int last, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        const elem* p = base + (long long)min(k0 + m, last) * D;
+        dev::static_for<kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            k.v[0][kk] = *reinterpret_cast<const f32x4*>(p + chunk(kk, g));
+        });
+    }
+    __device__ static void load_v(V& v, const elem* base, int k0, int last, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        dev::static_for<4>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            const elem* p = base + (long long)min(k0 + 4 * g + j, last) * D + kDV * m;
+            dev::static_for<kDV / 4>([&](auto c) {
+                constexpr int i = decltype(c)::value;
+                v.v[j][i] = *reinterpret_cast<const f32x4*>(p + 4 * i);
+            });
+        });
+    }
+    __device__ static void logits(f32x4 (&s)[1], const K& k, const Q& q) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        dev::static_for<kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            dev::static_for<4>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k.v[0][kk][j], q.v[kk][j], acc, 0, 0, 0);
+            });
+        });
+        s[0] = acc;
+    }
+    template <int RT>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][1]) {
+        dev::static_for<4>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            dev::static_for<kDV>([&](auto dc) {
+                constexpr int dd = decltype(dc)::value;
+                dev::static_for<RT>([&](auto rc) {
+                    constexpr int rt = decltype(rc)::value;
+                    o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.v[j][dd / 4][dd % 4], p[rt][0][j], o[rt][dd], 0,
+                                                                     0, 0);
+                });
+            });
+        });
+    }
+    __device__ static void store(elem* p, float x) { *p = x; }
+};
+
+// Length of a unit's keys: lens may hold anything, the keys read stay in [0, n).
+__device__ __forceinline__ int unit_len(const Segment& sg, int unit, int Hkv) {
+    return sg.lens ? min(max(sg.lens[unit / Hkv], 0), sg.n) : sg.n;
+}
+
+// Keys that query t sees: the T queries are the newest tokens of the cache.
+__device__ __forceinline__ int seen_by(const Args& a, const Segment& sg, int len, int t) {
+    return sg.causal ? max(0, len - a.T + 1 + t) : len;
+}
+
+template <class E, int D>
+__device__ __forceinline__ typename E::Q load_q(const Args& a, const Row& x, bool valid, int g) {
+    typename E::Q q;
+    const typename E::elem* p = static_cast<const typename E::elem*>(a.q) + x.q;
+    dev::static_for<E::kKK>([&](auto c) {
+        constexpr int kk = decltype(c)::value;
+        typedef std::remove_reference_t<decltype(q.v[0])> V;
+        q.v[kk] = valid ? *reinterpret_cast<const V*>(p + E::chunk(kk, g)) : V{};
+    });
+    return q;
+}
+
+// ---- streaming kernel ------------------------------------------------------------
+// One work item: up to 16 RT rows of a unit against a chunk of its keys.  The
+// four waves take key groups in turn, each with its own m, z and o, and join
+// in LDS at the end.  What bounds it for few rows is the stream of K and V:
+// no key passes through LDS, a wave's next keys are requested before this
+// group's weights are computed and its next values after they are used, and
+// rows that share a kv-head share every load.
+template <class E, int D, int RT>
+__global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
+    constexpr int KG = E::kKeys, NT = E::kTiles, DV = E::kDV;
+    constexpr int DP = D + 4;  // padded row of the joined sums
+    __shared__ float s_o[kWaves][16][DP];
+    __shared__ float s_m[kWaves][16], s_z[kWaves][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 15, g = lane >> 4;
+    const bool own = (int)blockIdx.x >= a.items0;
+    const Segment sg = own ? a.seg[1] : a.seg[0];
+    int item = blockIdx.x - (own ? a.items0 : 0);
+    const int rb = item % sg.nrb;
+    item /= sg.nrb;
+    const int split = item % sg.ns, unit = item / sg.ns;
+    const int len = unit_len(sg, unit, a.Hkv);
+    const int r0 = rb * 16 * RT;
+
+    typename E::Q q[RT];
+    int lim[RT];  // keys the lane's row sees
+    float m[RT], z[RT];
+    f32x4 o[RT][DV];
+    int most = 0;  // keys that any row of the item sees
+    dev::static_for<RT>([&](auto rc) {
+        constexpr int rt = decltype(rc)::value;
+        const int rr = r0 + 16 * rt + col;
+        const bool valid = rr < sg.rows;
+        const Row x = decode_row(a, unit, sg.seqs, valid ? rr : 0);
+        q[rt] = load_q<E, D>(a, x, valid, g);
+        lim[rt] = valid ? seen_by(a, sg, len, x.t) : 0x7fffffff;  // a row that is none masks nothing
+        most = max(most, valid ? lim[rt] : 0);
+        m[rt] = kLowest;
+        z[rt] = 0.f;
+        dev::static_for<DV>([&](auto dc) { o[rt][decltype(dc)::value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    });
+    int least = lim[0];
+    dev::static_for<RT>([&](auto rc) { least = min(least, lim[decltype(rc)::value]); });
+    for (int x = 1; x < 16; x <<= 1) {
+        most = max(most, dev::shfl_xor_i(most, x));
+        least = min(least, dev::shfl_xor_i(least, x));
+    }
+    const int k_lo = split * sg.chunk;
+    // with the logits kept, keys that no row sees are written too (as -inf)
+    const bool keep = a.logits != nullptr && own;
+    const int k_hi = min(k_lo + sg.chunk, keep ? len : most);
+    const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
+    const typename E::elem* V = static_cast<const typename E::elem*>(sg.V) + (long long)unit * sg.cap * D;
+    float* lrow[RT];
+    if (keep)
+        dev::static_for<RT>([&](auto rc) {
+            constexpr int rt = decltype(rc)::value;
+            const int rr = r0 + 16 * rt + col;
+            lrow[rt] = rr < sg.rows ? a.logits + ((long long)unit * a.R + rr) * a.lstride : nullptr;
+        });
+
+    int k0 = k_lo + KG * wave;
+    if (k0 < k_hi) {
+        const int last = k_hi - 1;  // rows past it repeat it: nothing behind a sequence is read
+        typename E::K kr;
+        typename E::V vr;
+        E::load_k(kr, K, k0, last, lane);
+        E::load_v(vr, V, k0, last, lane);
+        for (; k0 < k_hi; k0 += KG * kWaves) {
+            f32x4 p[RT][NT];
+            dev::static_for<RT>([&](auto rc) {
+                constexpr int rt = decltype(rc)::value;
+                E::logits(p[rt], kr, q[rt]);
+            });
+            E::load_k(kr, K, k0 + KG * kWaves, last, lane);
+            const bool edge = k0 + KG > min(least, k_hi);
+            dev::static_for<RT>([&](auto rc) {
+                constexpr int rt = decltype(rc)::value;
+                float top = kLowest;
+                dev::static_for<NT * 4>([&](auto ic) {
+                    constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                    float l = p[rt][ti][i] * a.scale2;
+                    if (edge && k0 + 16 * ti + 4 * g + i >= min(lim[rt], k_hi)) l = -INFINITY;
+                    p[rt][ti][i] = l;
+                    top = fmaxf(top, l);
+                });
+                if (keep && lrow[rt])
+                    dev::static_for<NT>([&](auto tc) {
+                        constexpr int ti = decltype(tc)::value;
+                        *reinterpret_cast<f32x4*>(lrow[rt] + k0 + 16 * ti + 4 * g) = p[rt][ti];
+                    });
+                top = fmaxf(top, dev::shfl_xor_f(top, 16));
+                top = fmaxf(top, dev::shfl_xor_f(top, 32));
+                if (__any(top > m[rt])) {
+                    const float mn = fmaxf(m[rt], top), f = exp2_hw(m[rt] - mn);
+                    m[rt] = mn;
+                    z[rt] *= f;
+                    dev::static_for<DV>([&](auto dc) { o[rt][decltype(dc)::value] *= f; });
+                }
+                dev::static_for<NT * 4>([&](auto ic) {
+                    constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                    const float e = exp2_hw(p[rt][ti][i] - m[rt]);
+                    p[rt][ti][i] = e;
+                    z[rt] += e;
+                });
+            });
+            E::template values<RT>(o, vr, p);
+            E::load_v(vr, V, k0 + KG * kWaves, last, lane);
+        }
+    }
+
+    // join the waves, one row tile at a time
+    dev::static_for<RT>([&](auto rc) {
+        constexpr int rt = decltype(rc)::value;
+        float zz = z[rt];
+        zz += dev::shfl_xor_f(zz, 16);
+        zz += dev::shfl_xor_f(zz, 32);
+        if (g == 0) {
+            s_m[wave][col] = m[rt];
+            s_z[wave][col] = zz;
+        }
+        dev::static_for<4>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            dev::static_for<DV / 4>([&](auto cc) {
+                constexpr int c = decltype(cc)::value;
+                *reinterpret_cast<f32x4*>(&s_o[wave][col][DV * (4 * g + i) + 4 * c]) =
+                    f32x4{o[rt][4 * c][i], o[rt][4 * c + 1][i], o[rt][4 * c + 2][i], o[rt][4 * c + 3][i]};
+            });
+        });
+        __syncthreads();
+        constexpr int VPR = D / 4;  // 16-byte vectors of a row
+        for (int e = threadIdx.x; e < 16 * VPR; e += kThreads) {
+            const int r = e / VPR, v = e % VPR;
+            const int rr = r0 + 16 * rt + r;
+            if (rr >= sg.rows) break;
+            float M = s_m[0][r];
+            for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            float Z = 0.f;
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = exp2_hw(s_m[w][r] - M);
+                Z += f * s_z[w][r];
+                sum += f * *reinterpret_cast<const f32x4*>(&s_o[w][r][4 * v]);
+            }
+            const Row x = decode_row(a, unit, sg.seqs, rr);
+            if (a.ns > 1) {
+                const long long at = x.gr * a.ns + sg.split0 + split;
+                *reinterpret_cast<f32x4*>(a.part_o + at * D + 4 * v) = sum;
+                if (v == 0) {
+                    a.part_ml[2 * at] = M;
+                    a.part_ml[2 * at + 1] = Z;
+                }
+            } else {
+                const float inv = Z > 0.f ? 1.f / Z : 0.f;
+                typename E::elem* out = static_cast<typename E::elem*>(a.out) + x.q + 4 * v;
+                dev::static_for<4>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * inv); });
+                if (v == 0) {
+                    const float l2 = M + log2f(Z);
+                    if (a.lse) a.lse[x.lse] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
+                    if (a.mass) a.row_lse2[x.gr] = Z > 0.f ? l2 : INFINITY;
+                }
+            }
+        }
+        __syncthreads();
+    });
+}
+
+// ---- joining the partials ----------------------------------------------------------
+// One wave per row: the splits' weights exp2(m_s - M) go to the lanes, the
+// sums are added split by split.  A split that saw nothing has z = 0 and is
+// passed over.
+template <class E, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(Args a) {
+    constexpr int PER = D / 64;
+    const int lane = threadIdx.x & 63;
+    const long long gr = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (gr >= a.rows) return;
+    const float* ml = a.part_ml + 2 * gr * a.ns;
+    const float* po = a.part_o + gr * a.ns * D;
+    float M = kLowest;
+    for (int s = lane; s < a.ns; s += 64)
+        if (ml[2 * s + 1] > 0.f) M = fmaxf(M, ml[2 * s]);
+    for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, dev::shfl_xor_f(M, x));
+    float Z = 0.f, sum[PER] = {};
+    for (int s0 = 0; s0 < a.ns; s0 += 64) {
+        const int s = s0 + lane;
+        float f = 0.f;
+        if (s < a.ns && ml[2 * s + 1] > 0.f) {
+            f = exp2_hw(ml[2 * s] - M);
+            Z += f * ml[2 * s + 1];
+        }
+        const int n = min(64, a.ns - s0);
+        for (int i = 0; i < n; ++i) {
+            const float w = __shfl(f, i, 64);
+            if (w == 0.f) continue;
+            dev::static_for<PER>([&](auto c) {
+                constexpr int e = decltype(c)::value;
+                sum[e] += w * po[(long long)(s0 + i) * D + PER * lane + e];
+            });
+        }
+    }
+    for (int x = 1; x < 64; x <<= 1) Z += dev::shfl_xor_f(Z, x);
+    const int r = (int)(gr % a.R);
+    const long long bh = gr / a.R;
+    const int t = r / a.G, g = r - t * a.G;
+    const long long at = (bh * a.G + g) * a.T + t;  // (b Hkv + h) G + g is the query head
+    const float inv = Z > 0.f ? 1.f / Z : 0.f;
+    typename E::elem* out = static_cast<typename E::elem*>(a.out) + at * D + PER * lane;
+    dev::static_for<PER>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * inv); });
+    if (lane == 0) {
+        const float l2 = M + log2f(Z);
+        if (a.lse) a.lse[at] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
+        if (a.mass) a.row_lse2[gr] = Z > 0.f ? l2 : INFINITY;
+    }
+}
+
+// ---- the weights' sums ----------------------------------------------------------------
+// mass_j += sum over the unit's rows of exp2(l2_rj - lse2_r), from the logits
+// that the streaming kernel kept: four keys a thread, rows in order, so the
+// sum does not depend on the launch.
+__global__ __launch_bounds__(kThreads) void kept_mass_kernel(Args a, int nchunk) {
+    const int unit = blockIdx.x / nchunk, ch = blockIdx.x % nchunk;
+    const Segment& sg = a.seg[1];
+    const int len = unit_len(sg, unit, a.Hkv);
+    const int j = (ch * kThreads + (int)threadIdx.x) * 4;
+    if (j >= len) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    const float* l = a.logits + (long long)unit * a.R * a.lstride + j;
+    for (int r = 0; r < a.R; ++r) {
+        const float norm = a.row_lse2[(long long)unit * a.R + r];
+        const f32x4 x = *reinterpret_cast<const f32x4*>(l + (long long)r * a.lstride);
+        dev::static_for<4>([&](auto c) { sum[decltype(c)::value] += exp2_hw(x[decltype(c)::value] - norm); });
+    }
+    float* mass = a.mass + (long long)unit * a.N_cap + j;
+    dev::static_for<4>([&](auto c) {
+        constexpr int i = decltype(c)::value;
+        if (j + i < len) mass[i] += sum[i];
+    });
+}
+
+// The same from the queries and keys, for more rows than the logits are kept
+// of: a workgroup holds 4 x 16 NT keys, streams the unit's rows past them, and
+// every lane sums its keys' weights over its rows (lane % 16) in order.
+template <class E, int D>
+__global__ __launch_bounds__(kThreads) void mass_kernel(Args a, int nchunk) {
+    constexpr int NT = E::kTiles, KG = E::kKeys;
+    const Segment& sg = a.seg[1];
+    const int unit = blockIdx.x / nchunk, ch = blockIdx.x % nchunk;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = lane & 15, g = lane >> 4;
+    const int len = unit_len(sg, unit, a.Hkv);
+    const int k0 = (ch * kWaves + wave) * KG;
+    if (k0 >= len) return;
+    const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
+    typename E::K kr;
+    E::load_k(kr, K, k0, len - 1, lane);
+    float sum[NT * 4] = {};
+    // the first query that sees key k0
+    const int t0 = sg.causal ? max(0, k0 - (len - a.T)) : 0;
+    for (int r0 = min(t0, a.T) * a.G / 16 * 16; r0 < a.R; r0 += 16) {
+        const int rr = r0 + col;
+        const bool valid = rr < a.R;
+        const Row x = decode_row(a, unit, 1, valid ? rr : 0);
+        const typename E::Q q = load_q<E, D>(a, x, valid, g);
+        const float norm = valid ? a.row_lse2[x.gr] : INFINITY;
+        const int lim = valid ? seen_by(a, sg, len, x.t) : 0;
+        f32x4 s[NT];
+        E::logits(s, kr, q);
+        dev::static_for<NT * 4>([&](auto ic) {
+            constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+            const float e = exp2_hw(s[ti][i] * a.scale2 - norm);
+            sum[decltype(ic)::value] += k0 + 16 * ti + 4 * g + i < lim ? e : 0.f;
+        });
+    }
+    float* mass = a.mass + (long long)unit * a.N_cap;
+    dev::static_for<NT * 4>([&](auto ic) {
+        constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+        const float v = dev::row16_sum(sum[decltype(ic)::value]);
+        const int j = k0 + 16 * ti + 4 * g + i;
+        if (col == 0 && j < len) mass[j] += v;
+    });
+}
+
+template <class E, int D>
+hipError_t stream(const Args& a, bool wide, hipStream_t s) {
+    const long long items = a.items0 + (long long)a.seg[1].units * a.seg[1].nrb * a.seg[1].ns;
+    if (items == 0) return hipSuccess;
+    if (wide)
+        hipLaunchKernelGGL((stream_kernel<E, D, 2>), dim3((unsigned)items), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((stream_kernel<E, D, 1>), dim3((unsigned)items), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <class E, int D>
+hipError_t join(const Args& a, hipStream_t s) {
+    if (a.ns > 1)
+        hipLaunchKernelGGL((join_kernel<E, D>), dim3((unsigned)((a.rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+    const Segment& sg = a.seg[1];
+    if (a.mass && a.logits && sg.n > 0 && sg.units > 0) {
+        const int nchunk = (sg.n + 4 * kThreads - 1) / (4 * kThreads);
+        hipLaunchKernelGGL(kept_mass_kernel, dim3((unsigned)(sg.units * nchunk)), dim3(kThreads), 0, s, a, nchunk);
+    }
+    return hipGetLastError();
+}
+
+template <class E, int D>
+hipError_t masses(const Args& a, hipStream_t s) {
+    const Segment& sg = a.seg[1];
+    if (sg.n == 0 || sg.units == 0) return hipSuccess;
+    const int nchunk = (sg.n + kWaves * E::kKeys - 1) / (kWaves * E::kKeys);
+    hipLaunchKernelGGL((mass_kernel<E, D>), dim3((unsigned)(sg.units * nchunk)), dim3(kThreads), 0, s, a, nchunk);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace attend
+
+hipError_t launch_attend_stream(const attend::Args& a, int dtype, bool wide, hipStream_t s) {
+    using namespace attend;
+    if (dtype == BKV_BF16) return a.D == 128 ? stream<Bf16<128>, 128>(a, wide, s) : stream<Bf16<64>, 64>(a, wide, s);
+    return a.D == 128 ? stream<F32<128>, 128>(a, wide, s) : stream<F32<64>, 64>(a, wide, s);
+}
+hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s) {
+    using namespace attend;
+    if (dtype == BKV_BF16) return a.D == 128 ? join<Bf16<128>, 128>(a, s) : join<Bf16<64>, 64>(a, s);
+    return a.D == 128 ? join<F32<128>, 128>(a, s) : join<F32<64>, 64>(a, s);
+}
+hipError_t launch_attend_mass(const attend::Args& a, int dtype, hipStream_t s) {
+    using namespace attend;
+    if (dtype == BKV_BF16) return a.D == 128 ? masses<Bf16<128>, 128>(a, s) : masses<Bf16<64>, 64>(a, s);
+    return a.D == 128 ? masses<F32<128>, 128>(a, s) : masses<F32<64>, 64>(a, s);
+}
+
+}  // namespace bkv

@@ -1,0 +1,189 @@
+// Entry points of the attention over the cache (bkv_attend,
+// bkv_attend_shared): argument checks, how the work is cut, the launches.
+#include <math.h>
+#include <string.h>
+
+#include "attend.h"
+
+namespace bkv {
+namespace attend {
+
+namespace {
+constexpr size_t kAlign = 256;
+inline size_t up(size_t x, size_t n) { return (x + n - 1) / n * n; }
+
+constexpr int kItems = 1024;    // work items that fill the machine
+constexpr int kMinChunk = 128;  // keys: one group of 32 for each wave
+constexpr int kKeptRows = 32;   // rows per unit up to which the logits are kept for the mass
+
+int splits(long long base, int n) {
+    const long long want = base > 0 ? (kItems + base - 1) / base : 1;
+    const long long most = (n + kMinChunk - 1) / kMinChunk;
+    const long long k = want < most ? want : most;
+    return (int)(k > 1 ? k : 1);
+}
+int chunk_of(int n, int ns) { return (int)up((size_t)((n + ns - 1) / ns), kMinChunk); }
+}  // namespace
+
+Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap) {
+    Plan p;
+    memset(&p, 0, sizeof p);
+    const long long G = d.Hq / d.Hkv, R = G * T;
+    const long long rows = (long long)d.B * d.Hq * T;
+    const int tile = R > 16 || (groups > 0 && (d.B / groups) * R > 16) ? 32 : 16;
+    const long long own = (long long)d.B * d.Hkv * ((R + tile - 1) / tile);
+    const long long pre = groups > 0 ? (long long)groups * d.Hkv * (((d.B / groups) * R + tile - 1) / tile) : 0;
+    p.own_ns_cap = splits(own, d.N_cap);
+    p.own_chunk = chunk_of(d.N, splits(own, d.N));
+    p.own_ns = d.N > 0 ? (d.N + p.own_chunk - 1) / p.own_chunk : 1;
+    if (d.N == 0) p.own_chunk = kMinChunk;
+    if (groups > 0) {
+        p.pre_ns_cap = splits(pre, P_cap);
+        if (P > 0) {
+            p.pre_chunk = chunk_of(P, splits(pre, P));
+            p.pre_ns = (P + p.pre_chunk - 1) / p.pre_chunk;
+        }
+    }
+    p.lstride_cap = (int)up((size_t)d.N_cap, 32);
+    size_t off = 0;
+    const int ns_cap = p.own_ns_cap + p.pre_ns_cap;
+    p.part_o = off;
+    if (ns_cap > 1) off = up(off + sizeof(float) * (size_t)rows * ns_cap * d.D, kAlign);
+    p.part_ml = off;
+    if (ns_cap > 1) off = up(off + sizeof(float) * (size_t)rows * ns_cap * 2, kAlign);
+    p.row_lse2 = off;
+    if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
+    p.logits = off;
+    if (mass && R <= kKeptRows) off = up(off + sizeof(float) * (size_t)rows * p.lstride_cap, kAlign);
+    p.end = off;
+    return p;
+}
+
+}  // namespace attend
+}  // namespace bkv
+
+using namespace bkv;
+using namespace bkv::attend;
+
+namespace {
+
+bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Dimensions of a call; groups 0: no prefix.
+bkv_status check_shape(const bkv_dims* d, int32_t T, int32_t groups, int32_t P, int32_t P_cap) {
+    const bkv_status st = bkv_validate(d, BKV_OP_COMPACT);
+    if (st != BKV_OK) return st;
+    if (T < 0 || groups < 0 || (long long)d->B * d->Hq * T > 0x7fffffffLL) return BKV_ERR_SHAPE;
+    if (groups > 0) {
+        if (d->B % groups != 0 || P_cap < 1 || P < 0 || P > P_cap) return BKV_ERR_SHAPE;
+        if ((long long)groups * d->Hkv * P_cap > 0x7fffffffLL) return BKV_ERR_SHAPE;
+    }
+    return BKV_OK;
+}
+
+bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32_t groups, const void* PK,
+               const void* PV, int32_t P, int32_t P_cap, const int32_t* p_lens, const void* K, const void* V,
+               const int32_t* lens, float scale, void* out, float* lse, float* mass, void* ws, size_t ws_bytes,
+               hipStream_t stream) {
+    if (flags & ~BKV_ATTEND_CAUSAL) return BKV_ERR_INVALID;
+    const bkv_status st = check_shape(d, T, groups, P, P_cap);
+    if (st != BKV_OK) return st;
+    if (d->B == 0 || T == 0) return BKV_OK;
+    if (!q || !out || !aligned(q) || !aligned(out)) return BKV_ERR_INVALID;
+    if (d->N > 0 && (!K || !V || !aligned(K) || !aligned(V))) return BKV_ERR_INVALID;
+    if (groups > 0 && P > 0 && (!PK || !PV || !aligned(PK) || !aligned(PV))) return BKV_ERR_INVALID;
+    if (!(scale >= 0.0f) || isinf(scale)) return BKV_ERR_INVALID;
+    const Plan p = make_plan(*d, T, mass != nullptr, groups, P, P_cap);
+    if (p.end > 0 && (!ws || ws_bytes < p.end || !aligned(ws))) return BKV_ERR_WORKSPACE;
+    char* w = static_cast<char*>(ws);
+    Args a;
+    memset(&a, 0, sizeof a);
+    a.Hq = d->Hq;
+    a.Hkv = d->Hkv;
+    a.G = d->Hq / d->Hkv;
+    a.T = T;
+    a.R = a.G * T;
+    a.D = d->D;
+    a.N = d->N;
+    a.N_cap = d->N_cap;
+    a.rows = d->B * d->Hq * T;
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.mass = mass;
+    a.scale2 = (scale == 0.0f ? 1.0f / sqrtf((float)d->D) : scale) * 1.4426950408889634f;
+    const int S = groups > 0 ? d->B / groups : 1;
+    const bool wide = a.R > 16 || (groups > 0 && (long long)S * a.R > 16);
+    const int tile = wide ? 32 : 16;
+    Segment& own = a.seg[1];
+    own.K = K;
+    own.V = V;
+    own.lens = lens;
+    own.n = d->N;
+    own.cap = d->N_cap;
+    own.units = d->B * d->Hkv;
+    own.seqs = 1;
+    own.rows = a.R;
+    own.nrb = (a.R + tile - 1) / tile;
+    own.ns = p.own_ns;
+    own.chunk = p.own_chunk;
+    own.split0 = p.pre_ns;
+    own.causal = flags & BKV_ATTEND_CAUSAL;
+    Segment& pre = a.seg[0];
+    pre.nrb = pre.ns = pre.seqs = 1;
+    if (groups > 0 && P > 0) {
+        pre.K = PK;
+        pre.V = PV;
+        pre.lens = p_lens;
+        pre.n = P;
+        pre.cap = P_cap;
+        pre.units = groups * d->Hkv;
+        pre.seqs = S;
+        pre.rows = S * a.R;
+        pre.nrb = (pre.rows + tile - 1) / tile;
+        pre.ns = p.pre_ns;
+        pre.chunk = p.pre_chunk;
+    }
+    const long long items0 = (long long)pre.units * pre.nrb * pre.ns;
+    const long long items1 = (long long)own.units * own.nrb * own.ns;
+    if (items0 + items1 > 0x7fffffffLL) return BKV_ERR_SHAPE;
+    a.items0 = (int)items0;
+    a.ns = p.own_ns + p.pre_ns;
+    a.part_o = reinterpret_cast<float*>(w + p.part_o);
+    a.part_ml = reinterpret_cast<float*>(w + p.part_ml);
+    a.row_lse2 = reinterpret_cast<float*>(w + p.row_lse2);
+    const bool keep = mass && a.R <= kKeptRows;
+    a.logits = keep ? reinterpret_cast<float*>(w + p.logits) : nullptr;
+    a.lstride = (int)up((size_t)d->N, 32);
+    if (launch_attend_stream(a, d->dtype, wide, stream) != hipSuccess) return BKV_ERR_HIP;
+    if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
+    if (mass && !keep && launch_attend_mass(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
+    return BKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t bkv_attend_workspace_bytes(const bkv_dims* d, int32_t T, int32_t mass, int32_t groups, int32_t P_cap) {
+    if (check_shape(d, T, groups, 0, P_cap) != BKV_OK || d->B == 0 || T == 0) return 0;
+    return make_plan(*d, T, mass != 0, groups, 0, P_cap).end;
+}
+
+bkv_status bkv_attend(const bkv_dims* d, int32_t flags, const void* q, int32_t T, const void* K, const void* V,
+                      const int32_t* lens, float scale, void* out, float* lse, float* mass, void* ws, size_t ws_bytes,
+                      hipStream_t stream) {
+    return run(d, flags, q, T, 0, nullptr, nullptr, 0, 0, nullptr, K, V, lens, scale, out, lse, mass, ws, ws_bytes,
+               stream);
+}
+
+bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32_t groups, const void* PK,
+                             const void* PV, int32_t P, int32_t P_cap, const int32_t* p_lens, const void* K,
+                             const void* V, const int32_t* lens, float scale, void* out, float* lse, float* mass,
+                             void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (groups < 1) return d ? BKV_ERR_SHAPE : BKV_ERR_INVALID;
+    return run(d, flags, q, T, groups, PK, PV, P, P_cap, p_lens, K, V, lens, scale, out, lse, mass, ws, ws_bytes,
+               stream);
+}
+
+}  // extern "C"
