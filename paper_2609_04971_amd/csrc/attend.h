@@ -48,11 +48,12 @@ struct Args {
 // only, and the splits are at most those of the capacities, so a workspace
 // serves every N <= N_cap and P <= P_cap.
 struct Plan {
-    bool own_tile, pre_tile;  // which kernel takes the segment
+    bool own_tile, pre_tile;  // the tile kernel takes the segment
+    bool wide;                // the streaming kernel takes 32 rows an item, else 16
+    int own_nrb, pre_nrb;
     int own_ns, own_chunk, pre_ns, pre_chunk;
-    int own_ns_cap, pre_ns_cap;
+    bool keep;                // the logits are kept for the mass
     size_t part_o, part_ml, row_lse2, logits, end;
-    int lstride_cap;
 };
 Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap);
 
@@ -81,11 +82,14 @@ constexpr float kLowest = -3.402823466e38f;
 
 }  // namespace attend
 
-// Segments (bit 0: prefix, bit 1: own) that the streaming kernel takes, in one launch.
+// Both segments in one launch (wide: 32 rows an item, else 16); a segment without units takes no part.
 hipError_t launch_attend_stream(const attend::Args& a, int dtype, bool wide, hipStream_t s);
+// One segment of a bf16 cache, 128 rows an item.
+hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, hipStream_t s);
 // Joins the partials and, where the logits were kept, adds the weights to the mass.
 hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s);
-// Adds the weights to the mass from the queries and keys (R > 32).
+// Adds the weights to the mass from the queries and keys: any type, and bf16 queries of less than 2 GB per unit.
 hipError_t launch_attend_mass(const attend::Args& a, int dtype, hipStream_t s);
+hipError_t launch_attend_tile_mass(const attend::Args& a, hipStream_t s);
 
 }  // namespace bkv

@@ -12,17 +12,23 @@ namespace {
 constexpr size_t kAlign = 256;
 inline size_t up(size_t x, size_t n) { return (x + n - 1) / n * n; }
 
-constexpr int kItems = 1024;    // work items that fill the machine
-constexpr int kMinChunk = 128;  // keys: one group of 32 for each wave
-constexpr int kKeptRows = 32;   // rows per unit up to which the logits are kept for the mass
+constexpr int kStreamItems = 1024;  // streaming work items that fill the machine
+constexpr int kTileItems = 512;     // tile work items: two per compute unit
+constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a streaming item, two tiles
+constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
-int splits(long long base, int n) {
-    const long long want = base > 0 ? (kItems + base - 1) / base : 1;
+int splits(long long base, int items, int n) {
+    const long long want = base > 0 ? (items + base - 1) / base : 1;
     const long long most = (n + kMinChunk - 1) / kMinChunk;
     const long long k = want < most ? want : most;
     return (int)(k > 1 ? k : 1);
 }
-int chunk_of(int n, int ns) { return (int)up((size_t)((n + ns - 1) / ns), kMinChunk); }
+
+// Splits of n keys (at most those of the capacity) and their length.
+void cut(int n, int ns, int* out_ns, int* chunk) {
+    *chunk = n > 0 ? (int)up((size_t)((n + ns - 1) / ns), kMinChunk) : kMinChunk;
+    *out_ns = n > 0 ? (n + *chunk - 1) / *chunk : 1;
+}
 }  // namespace
 
 Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap) {
@@ -30,23 +36,24 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     memset(&p, 0, sizeof p);
     const long long G = d.Hq / d.Hkv, R = G * T;
     const long long rows = (long long)d.B * d.Hq * T;
-    const int tile = R > 16 || (groups > 0 && (d.B / groups) * R > 16) ? 32 : 16;
-    const long long own = (long long)d.B * d.Hkv * ((R + tile - 1) / tile);
-    const long long pre = groups > 0 ? (long long)groups * d.Hkv * (((d.B / groups) * R + tile - 1) / tile) : 0;
-    p.own_ns_cap = splits(own, d.N_cap);
-    p.own_chunk = chunk_of(d.N, splits(own, d.N));
-    p.own_ns = d.N > 0 ? (d.N + p.own_chunk - 1) / p.own_chunk : 1;
-    if (d.N == 0) p.own_chunk = kMinChunk;
+    const long long pre_rows = groups > 0 ? d.B / groups * R : 0;
+    const bool tiles = d.dtype == BKV_BF16;
+    p.own_tile = tiles && R > kFewRows;
+    p.pre_tile = tiles && pre_rows > kFewRows;
+    p.wide = (!p.own_tile && R > 16) || (!p.pre_tile && pre_rows > 16);
+    const int own_rb = p.own_tile ? 128 : p.wide ? 32 : 16, pre_rb = p.pre_tile ? 128 : p.wide ? 32 : 16;
+    p.own_nrb = (int)((R + own_rb - 1) / own_rb);
+    p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
+    const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
+    const int own_items = p.own_tile ? kTileItems : kStreamItems, pre_items = p.pre_tile ? kTileItems : kStreamItems;
+    int ns_cap = splits(own, own_items, d.N_cap);
+    cut(d.N, splits(own, own_items, d.N), &p.own_ns, &p.own_chunk);
     if (groups > 0) {
-        p.pre_ns_cap = splits(pre, P_cap);
-        if (P > 0) {
-            p.pre_chunk = chunk_of(P, splits(pre, P));
-            p.pre_ns = (P + p.pre_chunk - 1) / p.pre_chunk;
-        }
+        ns_cap += splits(pre, pre_items, P_cap);
+        if (P > 0) cut(P, splits(pre, pre_items, P), &p.pre_ns, &p.pre_chunk);
     }
-    p.lstride_cap = (int)up((size_t)d.N_cap, 32);
+    p.keep = mass && R <= kFewRows;
     size_t off = 0;
-    const int ns_cap = p.own_ns_cap + p.pre_ns_cap;
     p.part_o = off;
     if (ns_cap > 1) off = up(off + sizeof(float) * (size_t)rows * ns_cap * d.D, kAlign);
     p.part_ml = off;
@@ -54,7 +61,7 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     p.row_lse2 = off;
     if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
     p.logits = off;
-    if (mass && R <= kKeptRows) off = up(off + sizeof(float) * (size_t)rows * p.lstride_cap, kAlign);
+    if (p.keep) off = up(off + sizeof(float) * (size_t)rows * up((size_t)d.N_cap, 32), kAlign);
     p.end = off;
     return p;
 }
@@ -112,9 +119,6 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     a.lse = lse;
     a.mass = mass;
     a.scale2 = (scale == 0.0f ? 1.0f / sqrtf((float)d->D) : scale) * 1.4426950408889634f;
-    const int S = groups > 0 ? d->B / groups : 1;
-    const bool wide = a.R > 16 || (groups > 0 && (long long)S * a.R > 16);
-    const int tile = wide ? 32 : 16;
     Segment& own = a.seg[1];
     own.K = K;
     own.V = V;
@@ -124,7 +128,7 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     own.units = d->B * d->Hkv;
     own.seqs = 1;
     own.rows = a.R;
-    own.nrb = (a.R + tile - 1) / tile;
+    own.nrb = p.own_nrb;
     own.ns = p.own_ns;
     own.chunk = p.own_chunk;
     own.split0 = p.pre_ns;
@@ -138,26 +142,33 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
         pre.n = P;
         pre.cap = P_cap;
         pre.units = groups * d->Hkv;
-        pre.seqs = S;
-        pre.rows = S * a.R;
-        pre.nrb = (pre.rows + tile - 1) / tile;
+        pre.seqs = d->B / groups;
+        pre.rows = pre.seqs * a.R;
+        pre.nrb = p.pre_nrb;
         pre.ns = p.pre_ns;
         pre.chunk = p.pre_chunk;
     }
     const long long items0 = (long long)pre.units * pre.nrb * pre.ns;
     const long long items1 = (long long)own.units * own.nrb * own.ns;
     if (items0 + items1 > 0x7fffffffLL) return BKV_ERR_SHAPE;
-    a.items0 = (int)items0;
     a.ns = p.own_ns + p.pre_ns;
     a.part_o = reinterpret_cast<float*>(w + p.part_o);
     a.part_ml = reinterpret_cast<float*>(w + p.part_ml);
     a.row_lse2 = reinterpret_cast<float*>(w + p.row_lse2);
-    const bool keep = mass && a.R <= kKeptRows;
-    a.logits = keep ? reinterpret_cast<float*>(w + p.logits) : nullptr;
+    a.logits = p.keep ? reinterpret_cast<float*>(w + p.logits) : nullptr;
     a.lstride = (int)up((size_t)d->N, 32);
-    if (launch_attend_stream(a, d->dtype, wide, stream) != hipSuccess) return BKV_ERR_HIP;
+    if (p.pre_tile && launch_attend_tile(a, pre, stream) != hipSuccess) return BKV_ERR_HIP;
+    if (p.own_tile && launch_attend_tile(a, own, stream) != hipSuccess) return BKV_ERR_HIP;
+    if (!p.own_tile) {  // rows of the prefix are no fewer than a sequence's own
+        a.items0 = p.pre_tile ? 0 : (int)items0;
+        if (launch_attend_stream(a, d->dtype, p.wide, stream) != hipSuccess) return BKV_ERR_HIP;
+    }
     if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
-    if (mass && !keep && launch_attend_mass(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
+    if (mass && !p.keep) {
+        const bool tile = p.own_tile && (long long)a.R * a.D * 2 < 0x7fffffffLL;
+        if ((tile ? launch_attend_tile_mass(a, stream) : launch_attend_mass(a, d->dtype, stream)) != hipSuccess)
+            return BKV_ERR_HIP;
+    }
     return BKV_OK;
 }
 
