@@ -7,8 +7,9 @@ queries keep coming back to (the thought-revisiting tokens of Section 3.1),
 between local queries on recent keys.  Each policy runs the trace through
 the periodic eviction driver: BeaconKV's Continual FPS beacons ("beacon"),
 running-mean beacons ("ns", row a1), the prompt's first queries frozen
-("initial", Table 3's Initial+Recent) and recent queries only ("rpc").  At
-every eviction:
+("initial", Table 3's Initial+Recent), recent queries only ("rpc") and the
+accumulated attention weight ("mass", which has no observation set, so no
+coverage).  At every eviction:
   * retention: the fraction of the planted keys still cached;
   * coverage: the mean, over the queries of the next `horizon` steps, of
     their largest cosine similarity to the pre-RoPE observation set the
@@ -67,7 +68,8 @@ def run(trace, mode: str, B_max: int, n_beacon: int = 16, n_recent: int = 16, pr
     T0 = B_max // 2 if prompt is None else prompt
     drv = PeriodicEviction(1, LB, Hq, Hkv, D, B_max, _identity_rope(D, K.device), n_beacon=n_beacon,
                            n_recent=n_recent, mode=mode, device=K.device, compaction=compaction)
-    drv.prefill(K[:, :, :T0].contiguous(), V[:, :, :T0].contiguous(), q[:, :, :T0].contiguous())
+    drv.prefill(K[:, :, :T0].contiguous(), V[:, :, :T0].contiguous(), q[:, :, :T0].contiguous(),
+                q_rope=q[:, :, :T0] if mode == "mass" else None)
     pos = torch.arange(T0, device=K.device).view(1, 1, T0).expand(LB, Hkv, T0).clone()
     out = {"retention": [], "coverage": [], "coverage_global": [], "steps": []}
     rec = []
@@ -77,6 +79,12 @@ def run(trace, mode: str, B_max: int, n_beacon: int = 16, n_recent: int = 16, pr
         if not ev:
             continue
         pos = torch.gather(pos, 2, drv.kept.long())
+        if mode == "mass":
+            out["retention"].append(retention(pos, trace["n_plant"]))
+            out["steps"].append(t)
+            if record:
+                rec.append({"pos": pos.clone()})
+            continue
         # the observation set of each kv-head: its beacons and its query heads' recent queries
         rec_q = drv.recent_pre[:, :, :n_recent].reshape(LB, Hkv, G * n_recent, D).float()
         if mode == "rpc":

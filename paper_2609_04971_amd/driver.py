@@ -31,6 +31,17 @@ step's pre-RoPE queries join the nearest of G * n_beacon slots per kv-head
 mode "initial" is the Initial+Recent baseline of Table 3: the first
 n_beacon queries of each query head (the prompt's) are frozen as its
 beacons for good, next to the same recent window.
+mode "mass" ranks by what tokens were attended to: the prompt's and every
+step's attention (bkv_attend) adds its weights to the tokens' mass, and
+evictions keep the prefix, the last n_recent tokens and the largest masses
+(bkv_evict_mass).  It needs no query buffers; prefill takes the prompt's
+post-RoPE queries.
+
+attention=True has step() compute the step's attention over the cache, in
+every mode and before any eviction, into `out` [LB, Hq, D] (and `lse`); mode
+"mass" always does.  share_prefix gives the sequences of each layer a prefix
+that is held once and never evicted (bkv_attend_shared): the B sequences are
+samples of one prompt, and what each of them writes is its own cache.
 
 compaction "fill" evicts with bkv_score, bkv_topk and bkv_compact_fill
 instead of bkv_evict_ex: the cache keeps the same rows but only the kept
@@ -53,24 +64,26 @@ import paper_2609_04971_amd as bkv
 class PeriodicEviction:
     def __init__(self, layers: int, B: int, Hq: int, Hkv: int, D: int, B_max: int, rope_table, n_beacon: int = 16,
                  n_recent: int = 16, n_prefix: int = 0, mode: str = "beacon", dtype=torch.bfloat16,
-                 device="cuda", record: bool = False, timing: bool = False, compaction: str = "order"):
+                 device="cuda", record: bool = False, timing: bool = False, compaction: str = "order",
+                 attention: bool = False):
         """rope_table(t) -> (cos, sin), fp32 [D/2] device tensors of the
         model's rotate-half RoPE at absolute position t (the beacons are
         rotated to the step at which eviction runs).  record keeps every
         call's inputs and outputs in `events`; timing brackets every library
         call with HIP events on the current stream, in `times`."""
-        if mode not in ("beacon", "rpc", "ns", "initial"):
-            raise ValueError("mode is 'beacon', 'rpc', 'ns' or 'initial'")
+        if mode not in ("beacon", "rpc", "ns", "initial", "mass"):
+            raise ValueError("mode is 'beacon', 'rpc', 'ns', 'initial' or 'mass'")
         if B_max % 8:
             raise ValueError("B_max must be a multiple of 8 (B_min = 7/8 B_max)")
         if compaction not in ("order", "fill"):
             raise ValueError("compaction is 'order' or 'fill'")
         self.compaction = compaction
         self.mode = mode
+        self.layers = layers
         self.LB, self.Hq, self.Hkv, self.D = layers * B, Hq, Hkv, D
         self.G = Hq // Hkv
         self.B_max, self.B_min = B_max, 7 * B_max // 8
-        self.nb = 0 if mode == "rpc" else n_beacon
+        self.nb = 0 if mode in ("rpc", "mass") else n_beacon
         self.nr = n_recent
         if self.B_max - self.nr <= self.B_min:
             raise ValueError("the recent window must fit between B_min and B_max")
@@ -93,10 +106,20 @@ class PeriodicEviction:
         self.n_rec = 0
         self.dims = bkv.dims(B=LB, Hq=Hq, Hkv=Hkv, D=D, N=B_max, N_cap=B_max, W=nr, C=self.G * nb,
                              budget=self.B_min, n_prefix=n_prefix, dtype="bf16" if dt == torch.bfloat16 else "fp32")
-        self.ws = bkv.workspace(self.dims, bkv.OP_EVICT, device=dev)
+        self.mass = torch.zeros(LB, Hkv, B_max, dtype=torch.float32, device=dev) if mode == "mass" else None
+        self.ws = bkv.mass_workspace(self.dims, device=dev) if mode == "mass" else \
+            bkv.workspace(self.dims, bkv.OP_EVICT, device=dev)
         self.kept = torch.empty(LB, Hkv, self.B_min, dtype=torch.int32, device=dev)
-        self.sel = torch.empty_like(self.kept) if compaction == "fill" else None  # top-k output before filling
-        self.scores = torch.empty(LB, Hkv, B_max, dtype=torch.float32, device=dev)
+        # top-k output before filling
+        self.sel = torch.empty_like(self.kept) if compaction == "fill" and mode != "mass" else None
+        self.scores = None if mode == "mass" else torch.empty(LB, Hkv, B_max, dtype=torch.float32, device=dev)
+        self.attention = attention or mode == "mass"
+        self.prefix = None  # (keys, values) of share_prefix
+        if self.attention:
+            self.adims = self.dims.replace(N=0)  # the cache as it stands
+            self.out = torch.zeros(LB, Hq, D, dtype=dt, device=dev)
+            self.lse = torch.zeros(LB, Hq, dtype=torch.float32, device=dev)
+            self.aws = bkv.attend_workspace(self.dims, 1, mode == "mass", device=dev)
         self.events = []  # (kind, details) of the calls made, when recording
         self.timing = timing
         self.times = []   # (kind, start event, end event), when timing
@@ -123,15 +146,54 @@ class PeriodicEviction:
         self.obs_len = min(self.nb, n)
         self._log("fps", why=why, src=src, picks=picks)
 
+    # ---- attention over the cache --------------------------------------------------
+    def share_prefix(self, K, V):
+        """Keys and values [layers, Hkv, P, D] of a prompt that the B sequences of
+        every layer share: held once, seen by every query, never evicted.  Before
+        prefill; the sequences' own tokens start at position P."""
+        if not self.attention:
+            raise ValueError("a shared prefix needs attention=True or mode 'mass'")
+        if self.t != 0:
+            raise ValueError("the prefix comes before every other token")
+        if K.shape != V.shape or K.dim() != 4 or tuple(K.shape[:2]) != (self.layers, self.Hkv) or K.shape[3] != self.D:
+            raise ValueError(f"the prefix is [layers, Hkv, P, D], got {tuple(K.shape)} and {tuple(V.shape)}")
+        self.t = K.shape[2]
+        if self.t:
+            self.prefix = (K.contiguous(), V.contiguous())
+            self.aws = bkv.attend_workspace(self.dims, 1, self.mass is not None, self.layers, self.t, device=K.device)
+
+    def _attend(self, q, out, lse, ws):
+        self.adims.N = self.L
+        kw = {"lse": lse, "mass": self.mass, "causal": True}
+        if self.prefix is None:
+            self._call("attend", lambda: bkv.attend(self.adims, q, self.K, self.V, out, ws, **kw))
+        else:
+            self._call("attend", lambda: bkv.attend_shared(self.adims, q, *self.prefix, self.K, self.V, out, ws, **kw))
+
     # ---- the phase machine -----------------------------------------------------
-    def prefill(self, K, V, q_pre):
-        """Prompt keys/values [LB, Hkv, T, D] and pre-RoPE queries [LB, Hq, T, D]."""
+    def prefill(self, K, V, q_pre, q_rope=None):
+        """Prompt keys/values [LB, Hkv, T, D] and pre-RoPE queries [LB, Hq, T, D].
+        With attention, and where the post-RoPE queries q_rope [LB, Hq, T, D]
+        are given (mode "mass" needs them), returns the prompt's causal
+        attention [LB, Hq, T, D]."""
         T = K.shape[2]
         if T > self.B_max - self.nr:
             raise ValueError("the prompt must end before the recent window")
+        if self.mode == "mass" and q_rope is None:
+            raise ValueError("mode 'mass' needs the prompt's post-RoPE queries")
         self.K[:, :, :T] = K
         self.V[:, :, :T] = V
-        self.L = self.t = T
+        self.L = T
+        self.t = T + (self.prefix[0].shape[2] if self.prefix else 0)
+        if self.mass is not None:
+            self.mass.zero_()
+        out = None
+        if self.attention and q_rope is not None:
+            q = q_rope.contiguous()
+            out = torch.empty_like(q)
+            groups, P = (self.layers, self.prefix[0].shape[2]) if self.prefix else (0, 0)
+            ws = bkv.attend_workspace(self.dims, T, self.mass is not None, groups, P, device=q.device)
+            self._attend(q, out, None, ws)
         if self.mode == "ns":
             # bkv_beacon_update takes queries t-major, so consecutive prompt
             # chunks give the same running means as one call; chunks keep
@@ -151,6 +213,7 @@ class PeriodicEviction:
             self._call("fps_prefill", lambda: bkv.fps_gather(q_pre, self.nb, dst=self.obs, picks=picks))
             self.obs_len = min(self.nb, T)
             self._log("fps", why="prefill", src=q_pre.clone() if self.record else None, picks=picks)
+        return out
 
     def step(self, k, v, q_pre, q_rope):
         """One decoding step: k, v [LB, Hkv, D]; q_pre, q_rope [LB, Hq, D].
@@ -159,7 +222,7 @@ class PeriodicEviction:
         # buffer (up to the freeze) or into the recent set (after it)
         L, nb, nr = self.L + 1, self.nb, self.nr
         writes = [(self.K, self.L, k), (self.V, self.L, v)]
-        recent = self.B_max - nr < L <= self.B_max
+        recent = self.B_max - nr < L <= self.B_max and self.mode != "mass"
         if recent:
             writes += [(self.recent_rope, self.n_rec, q_rope), (self.recent_pre, self.n_rec, q_pre)]
         elif self.mode == "beacon":
@@ -167,6 +230,9 @@ class PeriodicEviction:
         bkv.append_rows(writes)
         self.L = L
         self.t += 1
+        if self.attention:
+            q = q_rope.reshape(self.LB, self.Hq, 1, self.D).contiguous()
+            self._attend(q, self.out.unsqueeze(2), self.lse.unsqueeze(2), self.aws)
         if self.mode == "ns":
             q_new = q_pre.reshape(self.LB, self.Hq, 1, self.D).contiguous()
             self._call("beacon_update", lambda: bkv.beacon_update(self.dims, q_new, self.beacons, self.counts))
@@ -191,8 +257,15 @@ class PeriodicEviction:
         return False
 
     def _evict(self):
-        rc, rs = self.rope_table(self.t - 1)  # beacons rotated to the current step
         pre = (self.K.clone(), self.V.clone()) if self.record else None
+        if self.mode == "mass":
+            mass = self.mass.clone() if self.record else None
+            self._call("evict", lambda: bkv.evict_mass(self.dims, self.K, self.V, self.mass, self.ws, kept=self.kept,
+                                                       fill=self.compaction == "fill"))
+            self._log("evict", before=pre, mass=mass, kept=self.kept.clone())
+            self.L = self.B_min
+            return
+        rc, rs = self.rope_table(self.t - 1)  # beacons rotated to the current step
         if self.compaction == "order":
             self._call("evict", lambda: bkv.evict(self.dims, self.K, self.V, self.recent_rope, self.beacons,
                                                   self.counts, self.ws, kept=self.kept, scores=self.scores,
