@@ -314,11 +314,29 @@ def evict_noalloc(d: Dims, K, V, q_win, beacons, counts, kept=None, scores=None,
 
 
 # ---- attention over the cache, eviction by accumulated weight ----------------------
-def _here(t, name):
-    """Tensors of another GPU than the current one are refused: work goes to
-    the current device's stream."""
-    if t is not None and t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on GPU {t.get_device()}, the current device is {torch.cuda.current_device()}")
+def _arg(t, shape, dtype, name, dev, optional=False):
+    """Address of a contiguous tensor of this shape and type on GPU `dev`, the
+    current device: its stream is where the work goes.  One test decides the
+    usual case; what is wrong is found out only where it fails."""
+    if t is None and optional:
+        return None
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _ptr(t, shape, dtype, name)
+    raise ValueError(f"{name} is on GPU {t.get_device()}, the current device is {dev}")
+
+
+def _device_of(t, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    return torch.cuda.current_device()
+
+
+def _arg_ws(ws, dev):
+    if ws is not None and (not isinstance(ws, torch.Tensor) or ws.get_device() != dev or not ws.is_contiguous()):
+        raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)
 
 
 def attend_workspace(d: Dims, T: int = 1, mass: bool = False, groups: int = 0, P_cap: int = 0, device="cuda"):
@@ -329,19 +347,17 @@ def attend_workspace(d: Dims, T: int = 1, mass: bool = False, groups: int = 0, P
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
-def _attend_args(d, q, K, V, out, lens, lse, mass):
-    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+def _attend_args(d, q, K, V, out, lens, lse, mass, dev):
+    if q.dim() != 4:
         raise ValueError("q must be a tensor [B, Hq, T, D]")
-    T = q.shape[2]
-    cache = (d.B, d.Hkv, d.N_cap, d.D)
-    p = (_ptr(q, (d.B, d.Hq, T, d.D), _tdtype(d), "q"), _ptr(K, cache, _tdtype(d), "K"), _ptr(V, cache, _tdtype(d), "V"),
-         _ptr(lens, (d.B,), torch.int32, "lens", optional=True),
-         _ptr(out, (d.B, d.Hq, T, d.D), _tdtype(d), "out"),
-         _ptr(lse, (d.B, d.Hq, T), torch.float32, "lse", optional=True),
-         _ptr(mass, cache[:3], torch.float32, "mass", optional=True))
-    for t, name in ((q, "q"), (K, "K"), (V, "V"), (lens, "lens"), (out, "out"), (lse, "lse"), (mass, "mass")):
-        _here(t, name)
-    return T, p
+    B, Hq, T, D = rows = q.shape
+    dt, cache = _tdtype(d), (d.B, d.Hkv, d.N_cap, d.D)
+    if (B, Hq, D) != (d.B, d.Hq, d.D):
+        raise ValueError(f"q must have shape {(d.B, d.Hq, T, d.D)}, got {tuple(q.shape)}")
+    return T, dt, (_arg(q, rows, dt, "q", dev), _arg(K, cache, dt, "K", dev), _arg(V, cache, dt, "V", dev),
+                   _arg(lens, (B,), torch.int32, "lens", dev, True), _arg(out, rows, dt, "out", dev),
+                   _arg(lse, (B, Hq, T), torch.float32, "lse", dev, True),
+                   _arg(mass, cache[:3], torch.float32, "mass", dev, True))
 
 
 def attend(d: Dims, q, K, V, out, ws, lens=None, lse=None, mass=None, scale: float = 0.0, causal: bool = False):
@@ -349,11 +365,11 @@ def attend(d: Dims, q, K, V, out, ws, lens=None, lse=None, mass=None, scale: flo
     cache: out [B,Hq,T,D] and, where given, lse [B,Hq,T] written, and every
     cached token's weights added to mass [B,Hkv,N_cap].  lens [B] int32:
     ragged lengths.  causal: query t sees the tokens up to its own."""
-    T, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass)
-    wp, wn = _ws(ws)
-    _here(ws, "workspace")
-    st = lib().bkv_attend(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, kp, vp, lp, float(scale), op, ep, mp,
-                          wp, wn, _stream())
+    dev = _device_of(q, "q")
+    T, _, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass, dev)
+    wp, wn = _arg_ws(ws, dev)
+    st = lib().bkv_attend(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, kp, vp, lp, scale, op, ep, mp, wp, wn,
+                          torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend")
 
 
@@ -362,19 +378,18 @@ def attend_shared(d: Dims, q, PK, PV, K, V, out, ws, P: int | None = None, p_len
     """attend() for groups of consecutive sequences that share a prefix PK, PV
     [groups,Hkv,P_cap,D], of which the first P tokens are valid (default: all;
     p_lens [groups] int32: ragged).  mass collects the own tokens' weights."""
+    dev = _device_of(q, "q")
     if not isinstance(PK, torch.Tensor) or PK.dim() != 4:
         raise ValueError("PK must be a tensor [groups, Hkv, P_cap, D]")
     groups, P_cap = PK.shape[0], PK.shape[2]
-    T, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass)
+    T, dt, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass, dev)
     shape = (groups, d.Hkv, P_cap, d.D)
-    pk, pv = _ptr(PK, shape, _tdtype(d), "PK"), _ptr(PV, shape, _tdtype(d), "PV")
-    pl = _ptr(p_lens, (groups,), torch.int32, "p_lens", optional=True)
-    wp, wn = _ws(ws)
-    for t, name in ((PK, "PK"), (PV, "PV"), (p_lens, "p_lens"), (ws, "workspace")):
-        _here(t, name)
+    pk, pv = _arg(PK, shape, dt, "PK", dev), _arg(PV, shape, dt, "PV", dev)
+    pl = _arg(p_lens, (groups,), torch.int32, "p_lens", dev, True)
+    wp, wn = _arg_ws(ws, dev)
     st = lib().bkv_attend_shared(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, groups, pk, pv,
-                                 P_cap if P is None else int(P), P_cap, pl, kp, vp, lp, float(scale), op, ep, mp, wp, wn,
-                                 _stream())
+                                 P_cap if P is None else int(P), P_cap, pl, kp, vp, lp, scale, op, ep, mp, wp, wn,
+                                 torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_shared")
 
 
@@ -391,14 +406,14 @@ def evict_mass(d: Dims, K, V, mass, ws, kept=None, fill: bool = False):
     K, V and mass [B,Hkv,N_cap] compacted in place (fill: the layout of
     compact_fill), mass 0 from the budget to N.  kept [B,Hkv,min(budget,N)]
     int32, optional, receives the old row now at each row."""
-    cache = (d.B, d.Hkv, d.N_cap, d.D)
-    kp, vp = _ptr(K, cache, _tdtype(d), "K"), _ptr(V, cache, _tdtype(d), "V")
-    mp = _ptr(mass, cache[:3], torch.float32, "mass")
-    op = _ptr(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", optional=True)
-    wp, wn = _ws(ws)
-    for t, name in ((K, "K"), (V, "V"), (mass, "mass"), (kept, "kept"), (ws, "workspace")):
-        _here(t, name)
-    st = lib().bkv_evict_mass(ctypes.byref(d), EVICT_FILL if fill else 0, kp, vp, mp, op, wp, wn, _stream())
+    dev = _device_of(K, "K")
+    dt, cache = _tdtype(d), (d.B, d.Hkv, d.N_cap, d.D)
+    kp, vp = _arg(K, cache, dt, "K", dev), _arg(V, cache, dt, "V", dev)
+    mp = _arg(mass, cache[:3], torch.float32, "mass", dev)
+    op = _arg(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", dev, True)
+    wp, wn = _arg_ws(ws, dev)
+    st = lib().bkv_evict_mass(ctypes.byref(d), EVICT_FILL if fill else 0, kp, vp, mp, op, wp, wn,
+                              torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_evict_mass")
 
 

@@ -76,6 +76,28 @@ __device__ __forceinline__ Row decode_row(const Args& a, int unit, int seqs, int
     return x;
 }
 
+// Workgroups of 256 threads that one launch holds: its threads are counted in
+// 32 bits.
+constexpr long long kMaxBlocks = 0xffffffffLL / 256;
+
+// Blocks of the launches below.
+struct JoinGrid {
+    int wpr;  // waves per row
+    int njoin, nchunk;
+    long long blocks;
+};
+inline JoinGrid join_grid(const Args& a) {
+    // a wave per row, or four where there are so many splits that one would walk them for long
+    constexpr int kManySplits = 12, kWaves = 4, kTokens = 1024;
+    JoinGrid g;
+    g.wpr = a.ns >= kManySplits ? kWaves : 1;
+    const int rpb = kWaves / g.wpr;
+    g.njoin = a.ns > 1 ? (int)(((long long)a.rows + rpb - 1) / rpb) : 0;
+    g.nchunk = a.mass && a.logits ? (a.seg[1].n + kTokens - 1) / kTokens : 0;
+    g.blocks = g.njoin + (long long)a.seg[1].units * g.nchunk;
+    return g;
+}
+
 // Lowest running maximum: finite, so that exp2(-inf - m) is 0 and not NaN in
 // a row that has seen nothing yet.
 constexpr float kLowest = -3.402823466e38f;

@@ -369,18 +369,26 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     });
 }
 
-// ---- joining the partials ----------------------------------------------------------
-// One wave per row: the splits' weights exp2(m_s - M) go to the lanes, the
-// sums are added split by split.  A split that saw nothing has z = 0 and is
-// passed over.
-template <class E, int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(Args a) {
-    constexpr int PER = D / 64;
-    const int lane = threadIdx.x & 63;
-    const long long gr = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (gr >= a.rows) return;
+// ---- joining the partials, and the weights of kept logits --------------------------
+// One launch.  The first blocks join: WPR waves per row take the row's splits
+// in turn, the weights exp2(m_s - M) in their lanes, eight splits' sums
+// requested at a time.  A split that saw nothing has z = 0 and weight 0; its
+// sums are never used.
+// The other blocks add the kept logits' weights to the masses, four tokens a
+// thread, rows in order, so that no sum depends on the launch:
+//   mass_j += sum over the unit's rows of exp2(l2_rj - lse2_r).
+// They take the rows' normalisers from the partials themselves.
+template <class E, int D, int WPR>
+__device__ __forceinline__ void join_rows(const Args& a) {
+    constexpr int PER = D / 64, RPB = kWaves / WPR;
+    __shared__ float s_sum[WPR > 1 ? kWaves : 1][D];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int sub = wave % WPR;
+    const long long row = (long long)blockIdx.x * RPB + wave / WPR;
+    const bool valid = row < a.rows;
+    const long long gr = valid ? row : 0;
     const float* ml = a.part_ml + 2 * gr * a.ns;
-    const float* po = a.part_o + gr * a.ns * D;
+    const float* po = a.part_o + gr * a.ns * D + PER * lane;
     float M = kLowest;
     for (int s = lane; s < a.ns; s += 64)
         if (ml[2 * s + 1] > 0.f) M = fmaxf(M, ml[2 * s]);
@@ -394,16 +402,33 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Args a) {
             Z += f * ml[2 * s + 1];
         }
         const int n = min(64, a.ns - s0);
-        for (int i = 0; i < n; ++i) {
-            const float w = __shfl(f, i, 64);
-            if (w == 0.f) continue;
-            dev::static_for<PER>([&](auto c) {
-                constexpr int e = decltype(c)::value;
-                sum[e] += w * po[(long long)(s0 + i) * D + PER * lane + e];
+        for (int i0 = sub; i0 < n; i0 += 8 * WPR) {
+            float v[8][PER];
+            dev::static_for<8>([&](auto kc) {
+                constexpr int k = decltype(kc)::value;
+                const int i = s0 + min(i0 + k * WPR, n - 1);
+                dev::static_for<PER>([&](auto c) { v[k][decltype(c)::value] = po[(long long)i * D + decltype(c)::value]; });
+            });
+            dev::static_for<8>([&](auto kc) {
+                constexpr int k = decltype(kc)::value;
+                const int i = i0 + k * WPR;
+                const float w = i < n ? __shfl(f, i, 64) : 0.f;
+                dev::static_for<PER>([&](auto c) {
+                    constexpr int e = decltype(c)::value;
+                    sum[e] += w > 0.f ? w * v[k][e] : 0.f;
+                });
             });
         }
     }
     for (int x = 1; x < 64; x <<= 1) Z += dev::shfl_xor_f(Z, x);
+    if constexpr (WPR > 1) {
+        dev::static_for<PER>([&](auto c) { s_sum[wave][PER * lane + decltype(c)::value] = sum[decltype(c)::value]; });
+        __syncthreads();
+        if (sub != 0) return;
+        for (int w = 1; w < WPR; ++w)
+            dev::static_for<PER>([&](auto c) { sum[decltype(c)::value] += s_sum[wave + w][PER * lane + decltype(c)::value]; });
+    }
+    if (!valid) return;
     const int r = (int)(gr % a.R);
     const long long bh = gr / a.R;
     const int t = r / a.G, g = r - t * a.G;
@@ -414,32 +439,72 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Args a) {
     if (lane == 0) {
         const float l2 = M + log2f(Z);
         if (a.lse) a.lse[at] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-        if (a.mass) a.row_lse2[gr] = Z > 0.f ? l2 : INFINITY;
+        if (a.mass && !a.logits) a.row_lse2[gr] = Z > 0.f ? l2 : INFINITY;
     }
 }
 
-// ---- the weights' sums ----------------------------------------------------------------
-// mass_j += sum over the unit's rows of exp2(l2_rj - lse2_r), from the logits
-// that the streaming kernel kept: four keys a thread, rows in order, so the
-// sum does not depend on the launch.
-__global__ __launch_bounds__(kThreads) void kept_mass_kernel(Args a, int nchunk) {
-    const int unit = blockIdx.x / nchunk, ch = blockIdx.x % nchunk;
+constexpr int kKeptRows = 32;  // rows per unit of kept logits, at most
+
+__device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
+    __shared__ float s_m[kThreads], s_z[kThreads], s_norm[kKeptRows];
+    const int unit = item / nchunk, ch = item % nchunk;
     const Segment& sg = a.seg[1];
     const int len = unit_len(sg, unit, a.Hkv);
+    if (ch * kThreads * 4 >= len) return;
+    const long long row0 = (long long)unit * a.R;
+    if (a.ns > 1) {  // eight threads a row
+        const int r = threadIdx.x % kKeptRows;
+        float m = kLowest, z = 0.f;
+        if (r < a.R) {
+            const float* ml = a.part_ml + 2 * (row0 + r) * a.ns;
+            for (int s = threadIdx.x / kKeptRows; s < a.ns; s += kThreads / kKeptRows) {
+                if (!(ml[2 * s + 1] > 0.f)) continue;
+                const float mn = fmaxf(m, ml[2 * s]);
+                z = z * exp2_hw(m - mn) + ml[2 * s + 1] * exp2_hw(ml[2 * s] - mn);
+                m = mn;
+            }
+        }
+        s_m[threadIdx.x] = m;
+        s_z[threadIdx.x] = z;
+        __syncthreads();
+        if (threadIdx.x < kKeptRows) {
+            for (int w = 1; w < kThreads / kKeptRows; ++w) m = fmaxf(m, s_m[threadIdx.x + w * kKeptRows]);
+            z = 0.f;
+            for (int w = 0; w < kThreads / kKeptRows; ++w)
+                z += s_z[threadIdx.x + w * kKeptRows] * exp2_hw(s_m[threadIdx.x + w * kKeptRows] - m);
+            s_norm[threadIdx.x] = z > 0.f ? m + log2f(z) : INFINITY;
+        }
+    } else if ((int)threadIdx.x < a.R) {
+        s_norm[threadIdx.x] = a.row_lse2[row0 + threadIdx.x];
+    }
+    __syncthreads();
     const int j = (ch * kThreads + (int)threadIdx.x) * 4;
     if (j >= len) return;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    const float* l = a.logits + (long long)unit * a.R * a.lstride + j;
+    const float* l = a.logits + row0 * a.lstride + j;
+#pragma unroll 4
     for (int r = 0; r < a.R; ++r) {
-        const float norm = a.row_lse2[(long long)unit * a.R + r];
         const f32x4 x = *reinterpret_cast<const f32x4*>(l + (long long)r * a.lstride);
+        const float norm = s_norm[r];
         dev::static_for<4>([&](auto c) { sum[decltype(c)::value] += exp2_hw(x[decltype(c)::value] - norm); });
     }
     float* mass = a.mass + (long long)unit * a.N_cap + j;
+    if (j + 4 <= len && (reinterpret_cast<uintptr_t>(mass) & 15u) == 0) {
+        *reinterpret_cast<f32x4*>(mass) += sum;
+        return;
+    }
     dev::static_for<4>([&](auto c) {
         constexpr int i = decltype(c)::value;
         if (j + i < len) mass[i] += sum[i];
     });
+}
+
+template <class E, int D, int WPR>
+__global__ __launch_bounds__(kThreads) void join_kernel(Args a, int njoin, int nchunk) {
+    if ((int)blockIdx.x < njoin)
+        join_rows<E, D, WPR>(a);
+    else
+        kept_mass(a, blockIdx.x - njoin, nchunk);
 }
 
 // The same from the queries and keys, for more rows than the logits are kept
@@ -498,13 +563,13 @@ hipError_t stream(const Args& a, bool wide, hipStream_t s) {
 
 template <class E, int D>
 hipError_t join(const Args& a, hipStream_t s) {
-    if (a.ns > 1)
-        hipLaunchKernelGGL((join_kernel<E, D>), dim3((unsigned)((a.rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
-    const Segment& sg = a.seg[1];
-    if (a.mass && a.logits && sg.n > 0 && sg.units > 0) {
-        const int nchunk = (sg.n + 4 * kThreads - 1) / (4 * kThreads);
-        hipLaunchKernelGGL(kept_mass_kernel, dim3((unsigned)(sg.units * nchunk)), dim3(kThreads), 0, s, a, nchunk);
-    }
+    const JoinGrid g = join_grid(a);
+    if (g.blocks == 0) return hipSuccess;
+    const dim3 grid((unsigned)g.blocks), block(kThreads);
+    if (g.wpr > 1)
+        hipLaunchKernelGGL((join_kernel<E, D, kWaves>), grid, block, 0, s, a, g.njoin, g.nchunk);
+    else
+        hipLaunchKernelGGL((join_kernel<E, D, 1>), grid, block, 0, s, a, g.njoin, g.nchunk);
     return hipGetLastError();
 }
 

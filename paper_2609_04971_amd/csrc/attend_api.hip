@@ -150,13 +150,16 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     }
     const long long items0 = (long long)pre.units * pre.nrb * pre.ns;
     const long long items1 = (long long)own.units * own.nrb * own.ns;
-    if (items0 + items1 > 0x7fffffffLL) return BKV_ERR_SHAPE;
+    // every launch's grid; the weights' sums take at most one block per 64 tokens
+    if (items0 + items1 > kMaxBlocks || (mass && !p.keep && own.units * ((d->N + 63LL) / 64) > kMaxBlocks))
+        return BKV_ERR_SHAPE;
     a.ns = p.own_ns + p.pre_ns;
     a.part_o = reinterpret_cast<float*>(w + p.part_o);
     a.part_ml = reinterpret_cast<float*>(w + p.part_ml);
     a.row_lse2 = reinterpret_cast<float*>(w + p.row_lse2);
     a.logits = p.keep ? reinterpret_cast<float*>(w + p.logits) : nullptr;
     a.lstride = (int)up((size_t)d->N, 32);
+    if (join_grid(a).blocks > kMaxBlocks) return BKV_ERR_SHAPE;
     if (p.pre_tile && launch_attend_tile(a, pre, stream) != hipSuccess) return BKV_ERR_HIP;
     if (p.own_tile && launch_attend_tile(a, own, stream) != hipSuccess) return BKV_ERR_HIP;
     if (!p.own_tile) {  // rows of the prefix are no fewer than a sequence's own

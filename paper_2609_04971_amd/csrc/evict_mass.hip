@@ -363,6 +363,8 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     if (d->B == 0 || d->N == 0) return BKV_OK;
     if (!K || !V || !mass || ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15u))
         return BKV_ERR_INVALID;
+    // every launch's threads are counted in 32 bits
+    if ((long long)d->B * d->Hkv > 0xffffffffLL / kThreads) return BKV_ERR_SHAPE;
     const MassLayout m = mass_layout(*d);
     if (!ws || ws_bytes < m.end || (reinterpret_cast<uintptr_t>(ws) & 15u)) return BKV_ERR_WORKSPACE;
     char* w = static_cast<char*>(ws);
@@ -370,7 +372,7 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     const int n = d->N < d->budget ? d->N : d->budget;
     if (d->N <= d->budget) {
         if (!kept) return BKV_OK;
-        const long long total = (long long)P * n;
+        const long long total = (long long)P * n;  // at most 2^31
         hipLaunchKernelGGL(mass_identity_kernel, dim3((unsigned)((total + kCopyThreads - 1) / kCopyThreads)),
                            dim3(kCopyThreads), 0, stream, kept, n, total);
         return hipGetLastError() == hipSuccess ? BKV_OK : BKV_ERR_HIP;
@@ -391,6 +393,9 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     a.W = d->W;
     a.n_prefix = d->n_prefix;
     a.fill = flags & BKV_EVICT_FILL;
+    const int most = n < a.N - n ? n : a.N - n;
+    const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
+    if (a.fill && (long long)P * nchunk > 0xffffffffLL / kCopyThreads) return BKV_ERR_SHAPE;
     const dim3 grid((unsigned)P), block(kThreads);
     if (a.N <= 4 * kThreads)
         hipLaunchKernelGGL(mass_select_kernel<4>, grid, block, 0, stream, a);
@@ -404,9 +409,6 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     if (!a.fill) {
         return launch_compact(*d, ws_layout(*d), K, V, a.kept, ws, stream) == hipSuccess ? BKV_OK : BKV_ERR_HIP;
     }
-    const int most = n < a.N - n ? n : a.N - n;
-    const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
-    if ((long long)P * nchunk > 0x7fffffffLL) return BKV_ERR_SHAPE;
     const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
     const size_t hs = (size_t)d->N_cap * rb;
     char* k = static_cast<char*>(K);
