@@ -34,7 +34,7 @@ struct Args {
     float* mass;          // or null
     float* part_o;        // [row][ns][D] unnormalised sums of exp2(l2 - m) v
     float* part_ml;       // [row][ns][2] m and z = sum of exp2(l2 - m)
-    float* row_lse2;      // [row] log2-normaliser, +inf for a row that sees nothing
+    float* row_lse2;      // [B, Hq, T] log2-normalisers, +inf for a row that sees nothing
     float* logits;        // [own unit][R][lstride] l2 = l log2(e), -inf where not seen
     int lstride;
     int Hq, Hkv, G, T, R, D;
@@ -53,7 +53,8 @@ struct Plan {
     int own_nrb, pre_nrb;
     int own_ns, own_chunk, pre_ns, pre_chunk;
     bool keep;                // the logits are kept for the mass
-    size_t part_o, part_ml, row_lse2, logits, end;
+    int parts;                // else: workgroups that share a block of keys (bf16)
+    size_t part_o, part_ml, row_lse2, logits, parts_at, end;
 };
 Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap);
 
@@ -110,8 +111,9 @@ hipError_t launch_attend_stream(const attend::Args& a, int dtype, bool wide, hip
 hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, hipStream_t s);
 // Joins the partials and, where the logits were kept, adds the weights to the mass.
 hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s);
-// Adds the weights to the mass from the queries and keys: any type, and bf16 queries of less than 2 GB per unit.
-hipError_t launch_attend_mass(const attend::Args& a, int dtype, hipStream_t s);
-hipError_t launch_attend_tile_mass(const attend::Args& a, hipStream_t s);
+// Adds the weights to the mass from the queries and keys: fp32 caches, and bf16 ones (part: parts * units * n floats
+// where parts > 1).
+hipError_t launch_attend_mass(const attend::Args& a, hipStream_t s);
+hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s);
 
 }  // namespace bkv

@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                 if (v == 0) {
                     const float l2 = M + log2f(Z);
                     if (a.lse) a.lse[x.lse] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-                    if (a.mass) a.row_lse2[x.gr] = Z > 0.f ? l2 : INFINITY;
+                    if (a.mass) a.row_lse2[x.lse] = Z > 0.f ? l2 : INFINITY;
                 }
             }
         }
@@ -439,7 +439,7 @@ __device__ __forceinline__ void join_rows(const Args& a) {
     if (lane == 0) {
         const float l2 = M + log2f(Z);
         if (a.lse) a.lse[at] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-        if (a.mass && !a.logits) a.row_lse2[gr] = Z > 0.f ? l2 : INFINITY;
+        if (a.mass && !a.logits) a.row_lse2[at] = Z > 0.f ? l2 : INFINITY;
     }
 }
 
@@ -475,7 +475,8 @@ __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
             s_norm[threadIdx.x] = z > 0.f ? m + log2f(z) : INFINITY;
         }
     } else if ((int)threadIdx.x < a.R) {
-        s_norm[threadIdx.x] = a.row_lse2[row0 + threadIdx.x];
+        const int t = threadIdx.x / a.G, g = threadIdx.x - t * a.G;
+        s_norm[threadIdx.x] = a.row_lse2[row0 + g * a.T + t];
     }
     __syncthreads();
     const int j = (ch * kThreads + (int)threadIdx.x) * 4;
@@ -531,7 +532,7 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(Args a, int nchunk) {
         const bool valid = rr < a.R;
         const Row x = decode_row(a, unit, 1, valid ? rr : 0);
         const typename E::Q q = load_q<E, D>(a, x, valid, g);
-        const float norm = valid ? a.row_lse2[x.gr] : INFINITY;
+        const float norm = valid ? a.row_lse2[x.lse] : INFINITY;
         const int lim = valid ? seen_by(a, sg, len, x.t) : 0;
         f32x4 s[NT];
         E::logits(s, kr, q);
@@ -595,9 +596,8 @@ hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s) {
     if (dtype == BKV_BF16) return a.D == 128 ? join<Bf16<128>, 128>(a, s) : join<Bf16<64>, 64>(a, s);
     return a.D == 128 ? join<F32<128>, 128>(a, s) : join<F32<64>, 64>(a, s);
 }
-hipError_t launch_attend_mass(const attend::Args& a, int dtype, hipStream_t s) {
+hipError_t launch_attend_mass(const attend::Args& a, hipStream_t s) {
     using namespace attend;
-    if (dtype == BKV_BF16) return a.D == 128 ? masses<Bf16<128>, 128>(a, s) : masses<Bf16<64>, 64>(a, s);
     return a.D == 128 ? masses<F32<128>, 128>(a, s) : masses<F32<64>, 64>(a, s);
 }
 

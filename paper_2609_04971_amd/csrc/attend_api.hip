@@ -17,6 +17,10 @@ constexpr int kTileItems = 512;     // tile work items: two per compute unit
 constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a streaming item, two tiles
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
+constexpr int kMassItems = 2048;    // workgroups that sum the weights of many rows, at least
+constexpr int kMassRows = 1024;     // rows that make such a workgroup worth its own sums
+constexpr int kMassBlock = 128;     // keys of one
+
 int splits(long long base, int items, int n) {
     const long long want = base > 0 ? (items + base - 1) / base : 1;
     const long long most = (n + kMinChunk - 1) / kMinChunk;
@@ -62,6 +66,18 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
     p.logits = off;
     if (p.keep) off = up(off + sizeof(float) * (size_t)rows * up((size_t)d.N_cap, 32), kAlign);
+    // the heads of a group share a block of keys where there are few blocks and
+    // each head has many rows; parts > 1 means fewer blocks than kMassItems, so
+    // their sums never pass kMassItems blocks and as many again
+    p.parts = 1;
+    p.parts_at = off;
+    const long long most = G < R / kMassRows ? G : R / kMassRows;
+    if (mass && p.own_tile && most > 1) {
+        const long long blocks = (long long)d.B * d.Hkv * ((d.N + kMassBlock - 1) / kMassBlock);
+        const long long want = blocks > 0 ? (kMassItems + blocks - 1) / blocks : 1;
+        p.parts = (int)(want < most ? want : most);
+        off = up(off + sizeof(float) * 2 * kMassItems * kMassBlock, kAlign);
+    }
     p.end = off;
     return p;
 }
@@ -168,9 +184,10 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     }
     if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
     if (mass && !p.keep) {
-        const bool tile = p.own_tile && (long long)a.R * a.D * 2 < 0x7fffffffLL;
-        if ((tile ? launch_attend_tile_mass(a, stream) : launch_attend_mass(a, d->dtype, stream)) != hipSuccess)
-            return BKV_ERR_HIP;
+        const hipError_t e = p.own_tile
+                                 ? launch_attend_tile_mass(a, reinterpret_cast<float*>(w + p.parts_at), p.parts, stream)
+                                 : launch_attend_mass(a, stream);
+        if (e != hipSuccess) return BKV_ERR_HIP;
     }
     return BKV_OK;
 }

@@ -14,9 +14,12 @@
 // rows through the transposing LDS read (4 keys of a coordinate per lane).
 //
 // Tiles lie in LDS row by row, the 16-byte chunks of row r permuted by
-// chunk ^ f(r), f the bit reversal of r % 8: eight consecutive rows put one
-// chunk into eight different bank groups (K), and the transposing read's four
-// rows put a pair of chunks into four (V).
+// chunk ^ f(r).  LDS serves 256 bytes a cycle: 16 lanes of a 16-byte read (one
+// chunk of 16 consecutive rows, K) or 32 lanes of an 8-byte one (four chunks
+// of four rows, V).  f takes the low bits of r to the chunk's high bits, so
+// that four rows put their four chunks into four different blocks of 64
+// bytes, and is a permutation over 16 rows (over the 8 pairs of rows that
+// share 256 bytes, D = 64).
 #include "attend.h"
 
 namespace bkv {
@@ -44,7 +47,12 @@ __device__ __forceinline__ void turn() {
     __syncthreads();
 }
 
-__device__ __forceinline__ int swz(int r) { return ((r & 1) << 2) | (r & 2) | ((r >> 2) & 1); }
+// Position of chunk c of row r is c ^ swz(r).
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+    if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    return ((r & 2) << 1) | ((r >> 2) & 3);
+}
 
 template <int D>
 struct Tile {
@@ -67,34 +75,57 @@ __device__ __forceinline__ void load_tile(const uint16_t* base, int rows, uint16
         constexpr int jj = decltype(jc)::value;
         const int j = jj * kWaves + wave;
         const int r = j * T::RPI + lane / T::CPR;
-        const int off = r * D * 2 + (((lane % T::CPR) ^ swz(r)) * 16);
+        const int off = r * D * 2 + (((lane % T::CPR) ^ swz<D>(r)) * 16);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(stage + j * 512), 16,
                                                  off, 0, 0, 0);
     });
 #endif
 }
 
-// A operand of S^T: keys 32 kt + lane % 32, chunk 2 kk + h.
+// Where a lane finds its operands in a tile: the swizzle depends on r % 16
+// alone, so that every read is one of these offsets and a constant.
 template <int D>
-__device__ __forceinline__ bf16x8_t key_frag(const uint16_t* stage, int kt, int kk, int lane) {
-    const int r = 32 * kt + (lane & 31), c = 2 * kk + (lane >> 5);
-    return *reinterpret_cast<const bf16x8_t*>(stage + r * D + ((c ^ swz(r)) * 8));
+struct Offsets {
+    int k[D / 16];     // A operand of S^T: key lane % 32, chunk 2 kk + h
+    int v[D / 32][2];  // A operand of out^T: coordinates 32 dt + lane % 32, keys 4 h + L / 4 and 8 more
+};
+
+template <int D>
+__device__ __forceinline__ void row_offsets(int (&k)[D / 16], int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    dev::static_for<D / 16>([&](auto kc) {
+        constexpr int kk = decltype(kc)::value;
+        k[kk] = r * D + ((2 * kk + h) ^ swz<D>(r)) * 8;
+    });
+}
+template <int D>
+__device__ __forceinline__ Offsets<D> offsets(int lane) {
+    Offsets<D> o;
+    row_offsets<D>(o.k, lane);
+    // lanes 4 i .. 4 i + 3 of a group of 16 read 16 coordinates of key i, and
+    // lane i of the group ends up with coordinate i of the four keys
+    const int L = lane & 15, gg = lane >> 4;
+    dev::static_for<D / 16>([&](auto dc) {
+        constexpr int dt = decltype(dc)::value / 2, jh = decltype(dc)::value % 2;
+        const int r = 8 * jh + 4 * (gg >> 1) + (L >> 2);
+        o.v[dt][jh] = r * D + ((4 * dt + 2 * (gg & 1) + ((L & 3) >> 1)) ^ swz<D>(r)) * 8 + (L & 1) * 4;
+    });
+    return o;
 }
 
-// A operand of out^T: coordinates 32 dt + lane % 32, keys 16 c + 8 (j / 4) + 4 h + j % 4.
+__device__ __forceinline__ bf16x8_t row_frag(const uint16_t* stage, int off) {
+    return *reinterpret_cast<const bf16x8_t*>(stage + off);
+}
+
+// Keys 16 c + 8 (j / 4) + 4 h + j % 4 of a coordinate, j = 0..7.
 template <int D>
-__device__ __forceinline__ bf16x8_t value_frag(const uint16_t* stage, int dt, int c, int lane) {
-    s16x4 half[2];
-    dev::static_for<2>([&](auto jc) {
-        constexpr int jh = decltype(jc)::value;
-        const int L = lane & 15, gg = lane >> 4;
-        const int r = 16 * c + 8 * jh + 4 * (gg >> 1) + (L >> 2);
-        const int chunk = 4 * dt + 2 * (gg & 1) + ((L & 3) >> 1);
-        const uint16_t* p = stage + r * D + ((chunk ^ swz(r)) * 8) + (L & 1) * 4;
-        half[jh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(const_cast<uint16_t*>(p)));
-    });
-    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+__device__ __forceinline__ bf16x8_t value_frag(const uint16_t* stage, const int (&off)[2], int c) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4*)(const_cast<uint16_t*>(stage + off[0] + 16 * c * D)));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4*)(const_cast<uint16_t*>(stage + off[1] + 16 * c * D)));
+    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // The larger of the lane's value and that of lane ^ 32.
@@ -115,22 +146,40 @@ struct State {
 // to 2^8 do.
 constexpr float kSlack = 8.f;
 
-// One tile of keys [k0, k0 + 64) against the wave's rows.  edge: some row
-// does not see some key (lim: keys that the lane's row sees).
+// Kinds of instructions for the scheduler.
+constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100;
+
 template <int D>
-__device__ __forceinline__ void tile_step(State<D>& st, const uint16_t* ks, const uint16_t* vs, int k0, int lim,
-                                          bool edge, float scale2, int lane) {
-    using T = Tile<D>;
-    f32x16 s[2];
+__device__ __forceinline__ void tile_logits(f32x16 (&s)[2], const State<D>& st, const Offsets<D>& at,
+                                            const uint16_t* ks) {
     dev::static_for<2>([&](auto tc) {
         constexpr int kt = decltype(tc)::value;
         f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        dev::static_for<T::KK>([&](auto kc) {
+        dev::static_for<D / 16>([&](auto kc) {
             constexpr int kk = decltype(kc)::value;
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag<D>(ks, kt, kk, lane), st.q[kk], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag(ks, at.k[kk] + 32 * kt * D), st.q[kk], acc, 0, 0, 0);
         });
         s[kt] = acc;
     });
+    // six key operands ahead of the products: without it the compiler reads
+    // each one right before its product and waits for LDS every time
+    constexpr int N = 2 * (D / 16), AHEAD = 6;
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, AHEAD, 0);
+    dev::static_for<N - AHEAD>([&](auto) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+    });
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, AHEAD, 0);
+}
+
+// One tile of keys [k0, k0 + 64) against the wave's rows.  edge: some row
+// does not see some key (lim: keys that the lane's row sees).
+template <int D>
+__device__ __forceinline__ void tile_step(State<D>& st, const Offsets<D>& at, const uint16_t* ks, const uint16_t* vs,
+                                          int k0, int lim, bool edge, float scale2, int lane) {
+    constexpr int DT = D / 32;
+    f32x16 s[2];
+    tile_logits<D>(s, st, at, ks);
     if (edge) {
         const int h4 = 4 * (lane >> 5);
         dev::static_for<32>([&](auto ic) {
@@ -148,7 +197,7 @@ __device__ __forceinline__ void tile_step(State<D>& st, const uint16_t* ks, cons
         const float mn = fmaxf(st.m, top), f = exp2_hw(st.m - mn);
         st.m = mn;
         st.z *= f;
-        dev::static_for<T::DT>([&](auto dc) { st.o[decltype(dc)::value] *= f; });
+        dev::static_for<DT>([&](auto dc) { st.o[decltype(dc)::value] *= f; });
     }
     bf16x8_t p[4];
     float z = 0.f;
@@ -161,11 +210,22 @@ __device__ __forceinline__ void tile_step(State<D>& st, const uint16_t* ks, cons
     st.z += z;
     dev::static_for<4>([&](auto cc) {
         constexpr int c = decltype(cc)::value;
-        dev::static_for<T::DT>([&](auto dc) {
+        dev::static_for<DT>([&](auto dc) {
             constexpr int dt = decltype(dc)::value;
-            st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_frag<D>(vs, dt, c, lane), p[c], st.o[dt], 0, 0, 0);
+            st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_frag<D>(vs, at.v[dt], c), p[c], st.o[dt], 0, 0, 0);
         });
     });
+    // the first values are requested before the exponentials, the others
+    // between the products, and so are the exponentials of the later keys
+    constexpr int kFirst = 28, kRest = (112 - kFirst + 3 * DT - 1) / (3 * DT);
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, 2 * DT, 1);
+    __builtin_amdgcn_sched_group_barrier(kSchedValu, kFirst, 1);
+    dev::static_for<3 * DT>([&](auto) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 1);
+        __builtin_amdgcn_sched_group_barrier(kSchedValu, kRest, 1);
+    });
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, DT, 1);
 }
 
 template <int D>
@@ -224,9 +284,10 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
             load_tile<D>(V + (long long)k0 * D, k_hi - k0, vs, wave, lane);
         }
     };
+    const Offsets<D> at = offsets<D>(lane);
     auto step = [&](int k0, const uint16_t* ks, const uint16_t* vs) {
         if (k0 < most)
-            tile_step<D>(st, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
+            tile_step<D>(st, at, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
     };
     load(k_lo, k_a, v_a);
     for (int k0 = k_lo; k0 < k_hi; k0 += 2 * kKeys) {
@@ -265,125 +326,153 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
         if (h == 0) {
             const float l2 = st.m + log2f(z);
             if (a.lse) a.lse[x.lse] = z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-            if (a.mass) a.row_lse2[x.gr] = z > 0.f ? l2 : INFINITY;
+            if (a.mass) a.row_lse2[x.lse] = z > 0.f ? l2 : INFINITY;
         }
     }
 }
 
 // ---- the weights' sums -----------------------------------------------------------
 // mass_j += sum over the unit's rows of exp2(l2_rj - lse2_r).  A workgroup
-// holds 64 keys in operand registers (two waves of 32, twice) and walks the
-// unit's rows in tiles of 64 through LDS; waves 0, 1 take a tile's first 32
-// rows and 2, 3 the others.  A lane sums its 16 keys over its rows in order.
-template <int D>
-__device__ __forceinline__ void load_rows(const Args& a, const uint16_t* q, int r0, unsigned magic, uint16_t* stage,
-                                          int wave, int lane) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    using T = Tile<D>;
-    // the unit's queries: row r = t G + g lies at (g T + t) D
-    const __amdgpu_buffer_rsrc_t rsrc =
-        __builtin_amdgcn_make_buffer_rsrc((void*)q, (short)0, a.R * D * 2, 0x00020000);
-    dev::static_for<T::NI>([&](auto jc) {
-        constexpr int jj = decltype(jc)::value;
-        const int j = jj * kWaves + wave;
-        const int i = j * T::RPI + lane / T::CPR, r = r0 + i;
-        const int t = a.G == 1 ? r : (int)__umulhi((unsigned)r, magic), g = r - t * a.G;
-        const int off = (g * a.T + t) * D * 2 + (((lane % T::CPR) ^ swz(i)) * 16);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(stage + j * 512), 16,
-                                                 r < a.R ? off : 0x7fffffff, 0, 0, 0);
-    });
-#endif
-}
+// holds 128 keys in operand registers and walks the unit's rows in tiles of 64
+// through LDS: waves 0, 1 take a tile's first 32 rows and 2, 3 the others,
+// each for 64 of the keys.  A lane sums its 32 keys over its rows in order.
+// Rows are taken as they lie, head by head (g T + t).  With few units the
+// heads of the group go to `parts` workgroups, whose sums are added by
+// add_parts_kernel.
+constexpr int kMassKeys = 128;
 
 template <int D>
-__global__ __launch_bounds__(kThreads) void tile_mass_kernel(Args a, unsigned magic) {
+__global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* part, int parts) {
     using T = Tile<D>;
     __shared__ __attribute__((aligned(16))) uint16_t q_a[T::ELEMS], q_b[T::ELEMS];
-    __shared__ float s_sum[kKeys];
+    __shared__ float s_sum[kMassKeys];
     const Segment& sg = a.seg[1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, kw = wave & 1, rw = wave >> 1;
     // chunks of keys slowest: the first ones are seen by the most rows
-    const int unit = blockIdx.x % sg.units, k0 = blockIdx.x / sg.units * kKeys;
+    int item = blockIdx.x;
+    const int unit = item % sg.units;
+    item /= sg.units;
+    const int pt = item % parts, k0 = item / parts * kMassKeys;
     const int len = sg.lens ? min(max(sg.lens[unit / a.Hkv], 0), sg.n) : sg.n;
     if (k0 >= len) return;
-    const int key0 = k0 + 32 * kw;
+    const int key0 = k0 + 64 * kw;
     const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
-    const uint16_t* kp = K + (long long)min(key0 + (lane & 31), len - 1) * D + 8 * h;
-    bf16x8_t kr[T::KK];
-    dev::static_for<T::KK>([&](auto kc) {
-        constexpr int kk = decltype(kc)::value;
-        kr[kk] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * kk);
-    });
-    f32x16 sum = {};
-    const int lead = len - a.T;  // key j is seen by queries t >= j - lead
-    const int t0 = sg.causal ? min(max(0, k0 - lead), a.T) : 0;
-    const int start = t0 * a.G / kKeys * kKeys;
-    // rows from here on see all 64 keys
-    const int full = sg.causal ? (int)min((long long)a.R, (long long)max(0, k0 + kKeys - 1 - lead) * a.G) : 0;
-    const uint16_t* q = static_cast<const uint16_t*>(a.q) + (long long)unit * a.R * D;
-    const float* norms = a.row_lse2 + (long long)unit * a.R;
-    auto load = [&](int r, uint16_t* stage) {
-        if (r < a.R) load_rows<D>(a, q, r, magic, stage, wave, lane);
-    };
-    auto norm_at = [&](int r) {
-        const int i = r + 32 * rw + (lane & 31);
-        return i < a.R ? norms[i] : INFINITY;
-    };
-    auto step = [&](int r, const uint16_t* stage, float norm) {
-        f32x16 s = {};
+    bf16x8_t kr[2][T::KK];
+    dev::static_for<2>([&](auto tc) {
+        constexpr int kt = decltype(tc)::value;
+        const uint16_t* kp = K + (long long)min(key0 + 32 * kt + (lane & 31), len - 1) * D + 8 * h;
         dev::static_for<T::KK>([&](auto kc) {
             constexpr int kk = decltype(kc)::value;
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[kk], key_frag<D>(stage, rw, kk, lane), s, 0, 0, 0);
+            kr[kt][kk] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * kk);
         });
-        if (r < full) {
-            const int i = r + 32 * rw + (lane & 31);
-            const int t = a.G == 1 ? i : (int)__umulhi((unsigned)i, magic);
-            const int lim = lead + 1 + t;  // keys that the row sees
-            dev::static_for<16>([&](auto ic) {
-                constexpr int e = decltype(ic)::value;
-                const float w = exp2_hw(__builtin_fmaf(s[e], a.scale2, -norm));
-                sum[e] += key0 + 8 * (e / 4) + 4 * h + e % 4 < lim ? w : 0.f;
+    });
+    f32x16 sum[2] = {};
+    // heads [g0, g1) of the group, rows [r, r1) of them; key j is seen by the
+    // queries t >= j - lead
+    const int g0 = pt * a.G / parts, g1 = (pt + 1) * a.G / parts, r1 = g1 * a.T;
+    const int lead = len - a.T;
+    const int t0 = sg.causal ? max(0, k0 - lead) : 0;
+    const int full = sg.causal ? k0 + kMassKeys - 1 - lead : 0;  // queries from here on see all the keys
+    int r = g0 * a.T, t = 0;  // the tile's first row and its query
+    auto skip = [&]() {       // to the head's first query that sees anything
+        if (t < t0) {
+            r += t0 - t;
+            t = t0;
+        }
+    };
+    if (t0 >= a.T) r = r1;
+    skip();
+    auto load = [&](int row, uint16_t* stage) {
+        if (row < r1)
+            load_tile<D>(static_cast<const uint16_t*>(a.q) + ((long long)unit * a.R + row) * D, r1 - row, stage, wave, lane);
+    };
+    const float* norms = a.row_lse2 + (long long)unit * a.R + 32 * rw + (lane & 31);
+    auto norm_at = [&](int row) { return row + 32 * rw + (lane & 31) < r1 ? norms[row] : INFINITY; };
+    int at[T::KK];
+    row_offsets<D>(at, lane);
+    auto step = [&](int row, int query, const uint16_t* stage, float norm) {
+        f32x16 s[2] = {};
+        dev::static_for<T::KK>([&](auto kc) {
+            constexpr int kk = decltype(kc)::value;
+            const bf16x8_t q = row_frag(stage, at[kk] + 32 * rw * D);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[0][kk], q, s[0], 0, 0, 0);
+            s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[1][kk], q, s[1], 0, 0, 0);
+        });
+        if (query < full || (sg.causal && query + kKeys > a.T && row + a.T - query < r1)) {
+            // some row may not see some key, or a later head's first queries are in the tile
+            const int qt = (row + 32 * rw + (lane & 31)) % a.T;
+            const int lim = lead + 1 + qt - key0 - 4 * h;  // keys that the row sees, from the lane's first
+            dev::static_for<32>([&](auto ic) {
+                constexpr int kt = decltype(ic)::value / 16, e = decltype(ic)::value % 16;
+                const float w = exp2_hw(__builtin_fmaf(s[kt][e], a.scale2, -norm));
+                sum[kt][e] += 32 * kt + 8 * (e / 4) + e % 4 < lim ? w : 0.f;
             });
         } else {
-            dev::static_for<16>([&](auto ic) {
-                constexpr int e = decltype(ic)::value;
-                sum[e] += exp2_hw(__builtin_fmaf(s[e], a.scale2, -norm));
+            dev::static_for<32>([&](auto ic) {
+                constexpr int kt = decltype(ic)::value / 16, e = decltype(ic)::value % 16;
+                sum[kt][e] += exp2_hw(__builtin_fmaf(s[kt][e], a.scale2, -norm));
             });
         }
     };
-    load(start, q_a);
-    float norm = norm_at(start);
-    for (int r = start; r < a.R; r += 2 * kKeys) {
+    // the tile after (r, t)
+    auto advance = [&]() {
+        r += kKeys;
+        t += kKeys;
+        if (t >= a.T) {
+            t %= a.T;
+            skip();
+        }
+    };
+    load(r, q_a);
+    float norm = norm_at(r);
+    while (r < r1) {
+        const int ra = r, ta = t;
+        advance();
         turn();
-        load(r + kKeys, q_b);
-        const float next = norm_at(r + kKeys);
-        step(r, q_a, norm);
-        if (r + kKeys >= a.R) break;
+        load(r, q_b);
+        const float next = norm_at(r);
+        step(ra, ta, q_a, norm);
+        if (r >= r1) break;
+        const int rb = r, tb = t;
+        advance();
         turn();
-        load(r + 2 * kKeys, q_a);
-        norm = norm_at(r + 2 * kKeys);
-        step(r + kKeys, q_b, next);
+        load(r, q_a);
+        norm = norm_at(r);
+        step(rb, tb, q_b, next);
     }
     // over the 32 rows of the lanes, then the two row halves
-    dev::static_for<16>([&](auto ic) {
-        constexpr int e = decltype(ic)::value;
-        float v = dev::row16_sum(sum[e]);
+    dev::static_for<32>([&](auto ic) {
+        constexpr int kt = decltype(ic)::value / 16, e = decltype(ic)::value % 16;
+        float v = dev::row16_sum(sum[kt][e]);
         v += dev::shfl_xor_f(v, 16);
-        sum[e] = v;
+        sum[kt][e] = v;
+        if (rw == 1 && (lane & 31) == 0) s_sum[64 * kw + 32 * kt + 8 * (e / 4) + 4 * h + e % 4] = v;
     });
-    if (rw == 1 && (lane & 31) == 0)
-        dev::static_for<16>([&](auto ic) {
-            constexpr int e = decltype(ic)::value;
-            s_sum[32 * kw + 8 * (e / 4) + 4 * h + e % 4] = sum[e];
-        });
     __syncthreads();
     if (rw == 0 && (lane & 31) == 0)
-        dev::static_for<16>([&](auto ic) {
-            constexpr int e = decltype(ic)::value;
-            const int at = 32 * kw + 8 * (e / 4) + 4 * h + e % 4;
-            if (k0 + at < len) a.mass[(long long)unit * a.N_cap + k0 + at] += sum[e] + s_sum[at];
+        dev::static_for<32>([&](auto ic) {
+            constexpr int kt = decltype(ic)::value / 16, e = decltype(ic)::value % 16;
+            const int i = 64 * kw + 32 * kt + 8 * (e / 4) + 4 * h + e % 4;
+            if (k0 + i >= len) return;
+            const float v = sum[kt][e] + s_sum[i];
+            if (parts > 1)
+                part[((long long)pt * sg.units + unit) * sg.n + k0 + i] = v;
+            else
+                a.mass[(long long)unit * a.N_cap + k0 + i] += v;
         });
+}
+
+__global__ __launch_bounds__(kThreads) void add_parts_kernel(Args a, const float* part, int parts) {
+    const Segment& sg = a.seg[1];
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x, n = (long long)sg.units * sg.n;
+    if (i >= n) return;
+    const int unit = (int)(i / sg.n), j = (int)(i - (long long)unit * sg.n);
+    const int len = sg.lens ? min(max(sg.lens[unit / a.Hkv], 0), sg.n) : sg.n;
+    if (j >= len) return;
+    float v = 0.f;
+    for (int p = 0; p < parts; ++p) v += part[p * n + i];
+    a.mass[(long long)unit * a.N_cap + j] += v;
 }
 
 }  // namespace
@@ -400,16 +489,19 @@ hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, 
     return hipGetLastError();
 }
 
-hipError_t launch_attend_tile_mass(const attend::Args& a, hipStream_t s) {
+hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s) {
     using namespace attend;
     const Segment& sg = a.seg[1];
     if (sg.n == 0 || sg.units == 0) return hipSuccess;
-    const unsigned items = (unsigned)sg.units * (unsigned)((sg.n + kKeys - 1) / kKeys);
-    const unsigned magic = (unsigned)(((1ull << 32) + a.G - 1) / a.G);  // ceil(2^32 / G): r / G for r G < 2^32
+    const dim3 grid((unsigned)((long long)sg.units * parts * ((sg.n + kMassKeys - 1) / kMassKeys))), block(kThreads);
     if (a.D == 128)
-        hipLaunchKernelGGL(tile_mass_kernel<128>, dim3(items), dim3(kThreads), 0, s, a, magic);
+        hipLaunchKernelGGL(tile_mass_kernel<128>, grid, block, 0, s, a, part, parts);
     else
-        hipLaunchKernelGGL(tile_mass_kernel<64>, dim3(items), dim3(kThreads), 0, s, a, magic);
+        hipLaunchKernelGGL(tile_mass_kernel<64>, grid, block, 0, s, a, part, parts);
+    if (parts > 1) {
+        const long long n = (long long)sg.units * sg.n;
+        hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), block, 0, s, a, part, parts);
+    }
     return hipGetLastError();
 }
 
