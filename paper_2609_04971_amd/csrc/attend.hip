@@ -55,7 +55,7 @@ struct Bf16 {
             const elem* p = base + (long long)min(k0 + 16 * a + m, last) * D;
             dev::static_for<kKK>([&](auto c) {
                 constexpr int kk = decltype(c)::value;
-                k.v[a][kk] = *reinterpret_cast<const dev::u32x4*>(p + chunk(kk, g));
+                k.v[a][kk] = __builtin_nontemporal_load(reinterpret_cast<const dev::u32x4*>(p + chunk(kk, g)));
             });
         });
     }
@@ -65,7 +65,7 @@ struct Bf16 {
             constexpr int j = decltype(jc)::value;
             const elem* p = base + (long long)min(k0 + 16 * (j / 4) + 4 * g + j % 4, last) * D + kDV * m;
             if constexpr (kDV == 8) {
-                const dev::u32x4 x = *reinterpret_cast<const dev::u32x4*>(p);
+                const dev::u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const dev::u32x4*>(p));
                 dev::static_for<4>([&](auto c) { v.v[j][decltype(c)::value] = x[decltype(c)::value]; });
             } else {
                 const u32x2 x = *reinterpret_cast<const u32x2*>(p);

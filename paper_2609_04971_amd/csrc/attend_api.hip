@@ -12,20 +12,53 @@ namespace {
 constexpr size_t kAlign = 256;
 inline size_t up(size_t x, size_t n) { return (x + n - 1) / n * n; }
 
-constexpr int kStreamItems = 1024;  // streaming work items that fill the machine
-constexpr int kTileItems = 512;     // tile work items: two per compute unit
+constexpr int kStreamItems = 768;   // streaming work items: three per compute unit are resident
 constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a streaming item, two tiles
+constexpr int kWhole = 512;         // keys that one streaming item takes rather than a join
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
 constexpr int kMassItems = 2048;    // workgroups that sum the weights of many rows, at least
 constexpr int kMassRows = 1024;     // rows that make such a workgroup worth its own sums
 constexpr int kMassBlock = 128;     // keys of one
 
-int splits(long long base, int items, int n) {
-    const long long want = base > 0 ? (items + base - 1) / base : 1;
+// Splits of n keys for the streaming kernel: as many items as are resident.
+int stream_splits(long long base, int n) {
+    const long long want = base > 0 ? (kStreamItems + base - 1) / base : 1;
     const long long most = (n + kMinChunk - 1) / kMinChunk;
     const long long k = want < most ? want : most;
     return (int)(k > 1 ? k : 1);
+}
+
+int most_tile_splits(long long base, int n) {
+    constexpr int kMost = 64, kItems = 1024;
+    const long long k = base > 0 ? kItems / base + 1 : 1, by_keys = (n + kMinChunk - 1) / kMinChunk;
+    const long long least = k < by_keys ? k : by_keys;
+    return (int)(least > kMost ? kMost : least > 1 ? least : 1);
+}
+
+// Splits of n keys for the tile kernel, `base` items each, by what they cost
+// in keys of one item that has a compute unit to itself: the rounds of items
+// times their keys and what an item costs around them (kItemKeys), and the
+// partials' way through memory.  With 2 or 3 items on a compute unit a round
+// takes 1.7 or 2.4 times as long.
+int tile_splits(long long base, int n, long long rows, int D) {
+    constexpr int kCus = 256;
+    constexpr float kItemKeys = 100.f, kRound[4] = {0.f, 1.f, 1.7f, 2.4f};
+    constexpr float kJoinKeys = 43.f * 8.f / 4e6f;  // keys in the time that 8 bytes take at 4 TB/s
+    const int resident = D == 128 ? 2 : 3;          // items per compute unit
+    const int most = most_tile_splits(base, n);
+    int best = 1;
+    float least = 0.f;
+    for (int k = 1; k <= most; ++k) {
+        const long long items = base * k, full = items / (resident * kCus), rest = items % (resident * kCus);
+        const float rounds = (float)full * kRound[resident] + kRound[(rest + kCus - 1) / kCus];
+        const float cost = rounds * ((float)n / (float)k + kItemKeys) + (k > 1 ? (float)rows * (float)(k * D) * kJoinKeys : 0.f);
+        if (k == 1 || cost < least) {
+            least = cost;
+            best = k;
+        }
+    }
+    return best;
 }
 
 // Splits of n keys (at most those of the capacity) and their length.
@@ -49,12 +82,14 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
     const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
-    const int own_items = p.own_tile ? kTileItems : kStreamItems, pre_items = p.pre_tile ? kTileItems : kStreamItems;
-    int ns_cap = splits(own, own_items, d.N_cap);
-    cut(d.N, splits(own, own_items, d.N), &p.own_ns, &p.own_chunk);
+    // a short cache in one piece: joining splits would be a launch of its own.  Not by
+    // the mass: outputs do not depend on whether it is asked for
+    const bool whole = groups == 0 && !p.own_tile && d.N <= kWhole;
+    int ns_cap = p.own_tile ? most_tile_splits(own, d.N_cap) : stream_splits(own, d.N_cap);
+    cut(d.N, whole ? 1 : p.own_tile ? tile_splits(own, d.N, rows, d.D) : stream_splits(own, d.N), &p.own_ns, &p.own_chunk);
     if (groups > 0) {
-        ns_cap += splits(pre, pre_items, P_cap);
-        if (P > 0) cut(P, splits(pre, pre_items, P), &p.pre_ns, &p.pre_chunk);
+        ns_cap += p.pre_tile ? most_tile_splits(pre, P_cap) : stream_splits(pre, P_cap);
+        if (P > 0) cut(P, p.pre_tile ? tile_splits(pre, P, rows, d.D) : stream_splits(pre, P), &p.pre_ns, &p.pre_chunk);
     }
     p.keep = mass && R <= kFewRows;
     size_t off = 0;
