@@ -3,28 +3,41 @@
 // n_prefix - W of largest mass (ties to the lower index); K, V and the
 // masses themselves are compacted in place.
 //
-// One 1024-thread workgroup per head selects.  Masses are heavy-tailed (a
-// few sinks hold most of the weight), so they are cut by their order-preserving
-// bit pattern, which is about logarithmic: the candidates' range [lo, hi] is
-// split into 4096 equal bins, a histogram in LDS finds the bin that holds the
-// last one kept, and that bin becomes the range, 12 bits a round and at most
-// three rounds.  A round ends the search when its bin is taken whole.  Up to
-// 32768 tokens a head's masses stay in registers (token tid + 1024 i), so they
-// are read once and moved without a hazard; longer heads read them again on
-// every pass.  Kept tokens are ranked with ballots over runs of 64 tokens and
-// one scan of the runs' counts.
+// One workgroup per head selects.  Masses are heavy-tailed (a few sinks hold
+// most of the weight), so they are cut by their order-preserving bit pattern,
+// which is about logarithmic: the candidates' range [lo, hi] is split into
+// 4096 equal bins, a histogram in LDS finds the bin that holds the last one
+// kept, and that bin becomes the range, 12 bits a round and at most three
+// rounds.  Usually the first bin holds a few candidates, which one wave ranks
+// directly; a bin that is taken whole, or whose masses are all equal, ends the
+// search too.  What comes out is a (mass, token) pair: a candidate is kept if
+// its mass is larger, or equal with a token at or below.
+//
+// Up to 32768 tokens a head's masses stay in registers (token tid + NT i), so
+// they are read once and moved without a hazard; longer heads read them again
+// on every pass.  Kept tokens are ranked from the ballots of runs of 64 tokens
+// and one scan of the runs' counts.
+//
+// The rest is moving rows.  Order preserved, compact.hip does it.  Filling
+// holes, the moves are a list, which the selecting workgroup works off itself
+// where there are many heads (one's selection then overlaps another's copies)
+// and a second launch otherwise.
 #include "device_common.h"
 #include "internal.h"
 
 namespace bkv {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 4096;
-constexpr int kPerMax = 32;  // tokens per thread in registers
+constexpr int kPerMax = 32;    // tokens per thread in registers
+constexpr int kLongThreads = 1024;  // threads per head, and few where heads are many and short
+constexpr int kShortThreads = 256;
+constexpr int kManyHeads = 256;
+constexpr int kOwnMoves = kBins / 2;  // moves that the selecting workgroup's lists hold
 constexpr int kCopyThreads = 256;
 constexpr int kCopyMoves = 64;  // rows per copy item
+
+enum Mode { kOrder, kFill, kFillCopy };
 
 struct MassArgs {
     float* mass;
@@ -32,15 +45,24 @@ struct MassArgs {
     // moves of the hole-filling layout, [P][max_moves], and their number [P]
     int32_t* mv_src;
     int32_t* mv_dst;
-    float* mv_val;
+    int32_t* mv_val;
     int32_t* mv_n;
-    int32_t* runs;  // [P][2][nruns], heads longer than the registers hold
+    // heads longer than the registers hold: [P][nruns] ballots and [P][nruns] counts
+    unsigned long long* ballots;
+    int32_t* runs;
     int nruns, max_moves;
-    int N, N_cap, n_keep, W, n_prefix, fill;
+    int N, N_cap, n_keep, W, n_prefix;
+    // the rows, for workgroups that move them themselves
+    char* K;
+    char* V;
+    size_t head_stride;  // bytes between heads
+    int vec_shift;       // log2 of 16-byte vectors per row
 };
 
 // Exclusive scan of one int per thread over the workgroup; *total is the sum.
+template <int NT>
 __device__ __forceinline__ int block_scan(int v, int* buf, int* total) {
+    constexpr int NW = NT / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int x = v;
 #pragma unroll
@@ -51,103 +73,151 @@ __device__ __forceinline__ int block_scan(int v, int* buf, int* total) {
     if (lane == 63) buf[wave] = x;
     __syncthreads();
     int before = x - v, all = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) before += all;
-        all += buf[w];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const int t = buf[w];
+        if (w < wave) before += t;
+        all += t;
     }
     *total = all;
     __syncthreads();
     return before;
 }
 
-__device__ __forceinline__ unsigned block_min(unsigned v, unsigned* buf) {
-    v = dev::wave_min_u32(v);
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-    __syncthreads();
-    unsigned m = buf[0];
-    for (int w = 1; w < kWaves; ++w) m = min(m, buf[w]);
-    __syncthreads();
-    return m;
-}
-
 // Exclusive scan of n counts in place.
+template <int NT>
 __device__ __forceinline__ void scan_runs(int* runs, int n, int* buf) {
     int base = 0;
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
+    for (int i0 = 0; i0 < n; i0 += NT) {
         const int i = i0 + threadIdx.x;
         int total;
-        const int before = block_scan(i < n ? runs[i] : 0, buf, &total);
+        const int before = block_scan<NT>(i < n ? runs[i] : 0, buf, &total);
         if (i < n) runs[i] = base + before;
         base += total;
     }
     __syncthreads();
 }
 
-// PER tokens per thread in registers; 0: read from memory on every pass.
-template <int PER>
-__global__ __launch_bounds__(kThreads) void mass_select_kernel(MassArgs a) {
-    __shared__ int hist[kBins];
-    __shared__ int s_runs[2][PER ? PER * kWaves : 1];
-    __shared__ int buf[kWaves];
-    __shared__ unsigned ubuf[kWaves];
-    __shared__ int s_bin, s_above, s_count, s_c;
+// Rows src[m] -> dst[m] of K and V for moves [0, n): sources lie at or above
+// the budget and destinations below it, so no move can read what another
+// writes.  Threads [0, NT) of one workgroup, eight vectors each in flight.
+template <int NT>
+__device__ __forceinline__ void move_rows(char* K, char* V, const int* src, const int* dst, int n, int vec_shift) {
+    if (n <= 0) return;
+    const int vpr = 1 << vec_shift, total = n << (vec_shift + 1);  // K and V
+    for (int e0 = threadIdx.x; e0 < total; e0 += 8 * NT) {
+        dev::u32x4 b[8];
+        dev::static_for<8>([&](auto kc) {
+            const int e = min(e0 + decltype(kc)::value * NT, total - 1);
+            const int r = e >> (vec_shift + 1), v = e & (2 * vpr - 1);  // a move's K row, then its V row
+            const char* from = (v < vpr ? K : V) + ((size_t)src[r] << (vec_shift + 4)) + (v & (vpr - 1)) * 16;
+            b[decltype(kc)::value] = __builtin_nontemporal_load(reinterpret_cast<const dev::u32x4*>(from));
+        });
+        dev::static_for<8>([&](auto kc) {
+            const int e = e0 + decltype(kc)::value * NT;
+            const int r = e >> (vec_shift + 1), v = e & (2 * vpr - 1);
+            if (e < total) {
+                char* to = (v < vpr ? K : V) + ((size_t)dst[r] << (vec_shift + 4)) + (v & (vpr - 1)) * 16;
+                __builtin_nontemporal_store(b[decltype(kc)::value], reinterpret_cast<dev::u32x4*>(to));
+            }
+        });
+    }
+}
+
+// NT threads, PER tokens each in registers; PER 0: masses, ballots and counts
+// stay in memory.
+template <int NT, int PER, int MODE>
+__global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
+    constexpr int NW = NT / 64, BPT = kBins / NT;
+    __shared__ int hist[kBins];  // later the moves' two lists
+    __shared__ unsigned long long s_ballots[PER ? PER * NW : 1];
+    __shared__ int s_runs[PER ? PER * NW : 1];
+    __shared__ int buf[NW];
+    __shared__ unsigned s_min[NW], s_max[NW], s_cand[64];
+    __shared__ int s_cand_j[64];
+    __shared__ int s_bin, s_above, s_count, s_n, s_j;
+    __shared__ unsigned s_theta;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = blockIdx.x, N = a.N, n = a.n_keep;
     float* mass = a.mass + (size_t)h * a.N_cap;
     int32_t* kept = a.kept + (size_t)h * n;
     const int lo_t = a.n_prefix, hi_t = N - a.W;  // candidates [lo_t, hi_t)
-    const int NI = PER ? PER : (N + kThreads - 1) / kThreads;
-    const int nruns = NI * kWaves;
-    int* runs_eq = PER ? s_runs[0] : a.runs + (size_t)h * 2 * a.nruns;
-    int* runs_keep = PER ? s_runs[1] : runs_eq + a.nruns;
+    const int NI = PER ? PER : (N + NT - 1) / NT;
+    unsigned long long* ballots = PER ? s_ballots : a.ballots + (size_t)h * a.nruns;
+    int* runs = PER ? s_runs : a.runs + (size_t)h * a.nruns;
 
     float val[PER ? PER : 1];
     if constexpr (PER > 0) {
         dev::static_for<PER>([&](auto ic) {
             constexpr int i = decltype(ic)::value;
-            val[i] = mass[min(tid + i * kThreads, N - 1)];
+            val[i] = mass[min(tid + i * NT, N - 1)];
         });
     }
-    // f(i, token, value) for every token of this thread, whole waves at a time
+    // f(run, token, value) for every token of this thread, whole waves at a time
     auto each = [&](auto&& f) {
         if constexpr (PER > 0) {
             dev::static_for<PER>([&](auto ic) {
                 constexpr int i = decltype(ic)::value;
-                f(i, tid + i * kThreads, val[i]);
+                float v = val[i];
+                asm volatile("" : "+v"(v));  // or every pass's keys would be kept in registers
+                f(i * NW + wave, tid + i * NT, v);
             });
         } else {
             for (int i = 0; i < NI; ++i) {
-                const int j = tid + i * kThreads;
-                f(i, j, mass[min(j, N - 1)]);
+                const int j = tid + i * NT;
+                f(i * NW + wave, j, mass[min(j, N - 1)]);
             }
         }
     };
+    const unsigned long long below = (1ull << lane) - 1ull;
 
-    // the last candidate kept: its order key theta, and how many equal to it
-    // are taken
+    // the last candidate kept: mass order key theta, token last
     unsigned theta = 0xffffffffu;
-    int take = n - a.n_prefix - a.W;  // > 0 places, or none but the forced ones
-    bool ties = false;                // some equal to theta are left out
+    int last = -1;
+    int take = n - a.n_prefix - a.W;  // places for candidates; 0: none but the forced tokens
     if (take > 0) {
-        unsigned kmin = 0xffffffffu, kmaxn = 0xffffffffu;
+        unsigned kmin = 0xffffffffu, kmax = 0u;
         each([&](int, int j, float v) {
             if (j >= lo_t && j < hi_t) {
                 const unsigned u = dev::ord_key(v);
                 kmin = min(kmin, u);
-                kmaxn = min(kmaxn, ~u);
+                kmax = max(kmax, u);
             }
         });
-        unsigned lo = block_min(kmin, ubuf), hi = ~block_min(kmaxn, ubuf);
+        kmin = dev::wave_min_u32(kmin);
+        kmax = ~dev::wave_min_u32(~kmax);
+        if (lane == 0) {
+            s_min[wave] = kmin;
+            s_max[wave] = kmax;
+        }
+        for (int i = tid; i < kBins; i += NT) hist[i] = 0;
+        __syncthreads();
+        unsigned lo = s_min[0], hi = s_max[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            lo = min(lo, s_min[w]);
+            hi = max(hi, s_max[w]);
+        }
         for (;;) {
             const unsigned span = hi - lo;
-            if (span == 0) {  // every candidate of the range is equal
+            if (span == 0) {  // the candidates left are equal: the first `take` of them in order
                 theta = lo;
-                ties = true;
+                each([&](int run, int j, float v) {
+                    const unsigned long long eq = __ballot(j >= lo_t && j < hi_t && dev::ord_key(v) == theta);
+                    if (lane == 0) runs[run] = __builtin_popcountll(eq);
+                });
+                __syncthreads();
+                scan_runs<NT>(runs, NI * NW, buf);
+                each([&](int run, int j, float v) {
+                    const bool e = j >= lo_t && j < hi_t && dev::ord_key(v) == theta;
+                    const unsigned long long eq = __ballot(e);
+                    if (e && runs[run] + __builtin_popcountll(eq & below) == take - 1) s_j = j;
+                });
+                __syncthreads();
+                last = s_j;
                 break;
             }
             const int shift = max(0, 20 - __builtin_clz(span));  // bins 0..4095
-            for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
-            __syncthreads();
             each([&](int, int j, float v) {
                 const unsigned u = dev::ord_key(v);
                 const bool in = j >= lo_t && j < hi_t && u >= lo && u <= hi;
@@ -161,114 +231,126 @@ __global__ __launch_bounds__(kThreads) void mass_select_kernel(MassArgs a) {
                     if (in && bin != first) atomicAdd(&hist[bin], 1);
                 }
             });
+            if (tid == 0) s_n = 0;
             __syncthreads();
-            // the bin at which the count from the top reaches `take`
-            const int b0 = 4 * (kThreads - 1 - tid);
-            const int c3 = hist[b0 + 3], c2 = hist[b0 + 2], c1 = hist[b0 + 1], c0 = hist[b0];
-            int total;
-            int above = block_scan(c0 + c1 + c2 + c3, buf, &total);
-            const int c[4] = {c3, c2, c1, c0};
+            // the bin at which the count from the top reaches `take`; thread t
+            // owns the bins from BPT (NT - 1 - t), the highest first
+            const int b0 = BPT * (NT - 1 - tid);
+            int c[BPT], mine = 0, total;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < BPT; ++k) {
+                c[k] = hist[b0 + BPT - 1 - k];
+                mine += c[k];
+            }
+            int above = block_scan<NT>(mine, buf, &total);
+#pragma unroll
+            for (int k = 0; k < BPT; ++k) {
                 if (above < take && above + c[k] >= take) {
-                    s_bin = b0 + 3 - k;
+                    s_bin = b0 + BPT - 1 - k;
                     s_above = above;
                     s_count = c[k];
                 }
                 above += c[k];
             }
             __syncthreads();
-            const int bin = s_bin, count = s_count;
+            const int count = s_count;
             take -= s_above;
-            __syncthreads();
-            lo += (unsigned)bin << shift;
+            lo += (unsigned)s_bin << shift;
+            hi = min(hi, lo + ((1u << shift) - 1u));
             if (take == count) {  // the whole bin
                 theta = lo;
+                last = 0x7fffffff;
                 break;
             }
-            hi = min(hi, lo + ((1u << shift) - 1u));
+            if (count <= 64) {  // one wave ranks them
+                each([&](int, int j, float v) {
+                    const unsigned u = dev::ord_key(v);
+                    if (j >= lo_t && j < hi_t && u >= lo && u <= hi) {
+                        const int at = atomicAdd(&s_n, 1);
+                        s_cand[at] = u;
+                        s_cand_j[at] = j;
+                    }
+                });
+                __syncthreads();
+                if (tid < count) {
+                    const unsigned u = s_cand[tid];
+                    const int j = s_cand_j[tid];
+                    int rank = 0;
+                    for (int k = 0; k < count; ++k) rank += s_cand[k] > u || (s_cand[k] == u && s_cand_j[k] < j);
+                    if (rank == take - 1) {
+                        s_theta = u;
+                        s_j = j;
+                    }
+                }
+                __syncthreads();
+                theta = s_theta;
+                last = s_j;
+                break;
+            }
+            for (int i = tid; i < kBins; i += NT) hist[i] = 0;
+            __syncthreads();
         }
     }
-    // kept: forced, above theta, or one of the first `take` equal to it
-    // (without ties, everything from theta on)
-    auto forced = [&](int j) { return j < lo_t || j >= hi_t; };
-    const bool some = n > a.n_prefix + a.W;
-    if (ties) {
-        each([&](int i, int j, float v) {
-            const unsigned long long eq = __ballot(j < N && !forced(j) && dev::ord_key(v) == theta);
-            if (lane == 0) runs_eq[i * kWaves + wave] = __builtin_popcountll(eq);
-        });
-        __syncthreads();
-        scan_runs(runs_eq, nruns, buf);
-    }
-    const unsigned long long below = (1ull << lane) - 1ull;
-    auto is_kept = [&](int i, int j, float v) {
+    // ballots of the kept tokens and their counts, run by run
+    each([&](int run, int j, float v) {
         const unsigned u = dev::ord_key(v);
-        bool k = j < N && (forced(j) || (some && (ties ? u > theta : u >= theta)));
-        if (ties) {
-            const bool e = j < N && !forced(j) && u == theta;
-            const unsigned long long eq = __ballot(e);
-            if (e) k = runs_eq[i * kWaves + wave] + __builtin_popcountll(eq & below) < take;
+        const bool forced = j < lo_t || j >= hi_t;
+        const unsigned long long k =
+            __ballot(j < N && (forced || (last >= 0 && (u > theta || (u == theta && j <= last)))));
+        if (lane == 0) {
+            ballots[run] = k;
+            runs[run] = __builtin_popcountll(k);
         }
-        return k;
-    };
-    each([&](int i, int j, float v) {
-        const unsigned long long k = __ballot(is_kept(i, j, v));
-        if (lane == 0) runs_keep[i * kWaves + wave] = __builtin_popcountll(k);
     });
     __syncthreads();
-    scan_runs(runs_keep, nruns, buf);
+    scan_runs<NT>(runs, NI * NW, buf);
 
-    if (!a.fill) {
-        // rank <= token, so a pass writes masses at or below the tokens it has read
-        each([&](int i, int j, float v) {
-            const bool k = is_kept(i, j, v);
-            const int rank = runs_keep[i * kWaves + wave] + __builtin_popcountll(__ballot(k) & below);
-            if (PER == 0) __syncthreads();
-            if (k) {
+    if constexpr (MODE == kOrder) {
+        each([&](int run, int j, float v) {
+            const unsigned long long k = ballots[run];
+            const int rank = runs[run] + __builtin_popcountll(k & below);
+            if (PER == 0) __syncthreads();  // rank <= j: what a pass writes, it and the ones before it have read
+            if ((k >> lane) & 1) {
                 kept[rank] = j;
                 mass[rank] = v;
             }
         });
     } else {
         // kept rows from n on, in order, go to the holes below n, in order
-        int32_t* src = a.mv_src + (size_t)h * a.max_moves;
-        int32_t* dst = a.mv_dst + (size_t)h * a.max_moves;
-        float* mv = a.mv_val + (size_t)h * a.max_moves;
-        each([&](int i, int j, float v) {
-            const bool k = is_kept(i, j, v);
-            const int rank = runs_keep[i * kWaves + wave] + __builtin_popcountll(__ballot(k) & below);
-            if (j == n) s_c = rank;  // kept tokens below n (n < N)
-        });
-        __syncthreads();
-        const int c = s_c;
-        each([&](int i, int j, float v) {
-            const bool k = is_kept(i, j, v);
-            const int rank = runs_keep[i * kWaves + wave] + __builtin_popcountll(__ballot(k) & below);
-            if (k && j >= n) {
-                src[rank - c] = j;
-                mv[rank - c] = v;
+        const int c = runs[n >> 6] + __builtin_popcountll(ballots[n >> 6] & ((1ull << (n & 63)) - 1ull));  // kept below n
+        int* src = MODE == kFillCopy ? hist : a.mv_src + (size_t)h * a.max_moves;
+        int* dst = MODE == kFillCopy ? hist + kOwnMoves : a.mv_dst + (size_t)h * a.max_moves;
+        // a moved mass waits in its move's slot of dst until its hole's thread takes it
+        int* mv = MODE == kFillCopy ? dst : a.mv_val + (size_t)h * a.max_moves;
+        each([&](int run, int j, float v) {
+            const unsigned long long k = ballots[run];
+            if (j >= n && ((k >> lane) & 1)) {
+                const int m = runs[run] + __builtin_popcountll(k & below) - c;
+                src[m] = j;
+                mv[m] = __float_as_int(v);
             }
         });
         __syncthreads();
-        each([&](int i, int j, float v) {
-            const bool k = is_kept(i, j, v);
-            const int rank = runs_keep[i * kWaves + wave] + __builtin_popcountll(__ballot(k) & below);
-            if (j < n) {
-                int from = j;
-                if (!k) {
-                    const int m = j - rank;
-                    from = src[m];
-                    dst[m] = j;
-                    mass[j] = mv[m];
-                }
-                kept[j] = from;
+        each([&](int run, int j, float v) {
+            if (j >= n) return;
+            const unsigned long long k = ballots[run];
+            int from = j;
+            if (!((k >> lane) & 1)) {
+                const int m = j - (runs[run] + __builtin_popcountll(k & below));
+                from = src[m];
+                mass[j] = __int_as_float(mv[m]);
+                dst[m] = j;
             }
+            kept[j] = from;
         });
-        if (tid == 0) a.mv_n[h] = n - c;
+        if (MODE == kFill && tid == 0) a.mv_n[h] = n - c;
+        if constexpr (MODE == kFillCopy) {
+            __syncthreads();
+            move_rows<NT>(a.K + (size_t)h * a.head_stride, a.V + (size_t)h * a.head_stride, src, dst, n - c, a.vec_shift);
+        }
     }
-    __syncthreads();
-    for (int j = n + tid; j < N; j += kThreads) mass[j] = 0.f;  // the rows that the next tokens take
+    if (PER == 0) __syncthreads();  // every mass has been read
+    for (int j = n + tid; j < N; j += NT) mass[j] = 0.f;  // the rows that the next tokens take
 }
 
 // N <= budget: everything stays.
@@ -277,43 +359,29 @@ __global__ void mass_identity_kernel(int32_t* kept, int n, long long total) {
     if (i < total) kept[i] = (int)(i % n);
 }
 
-// The moves of the hole-filling layout: sources lie at or above n and
-// destinations below it, so no move can read what another writes.
-template <int RB>
-__global__ __launch_bounds__(kCopyThreads) void mass_copy_kernel(char* K, char* V, MassArgs a, int nchunk,
-                                                                 size_t head_stride) {
-    constexpr int VPR = RB / 16;
-    constexpr int NV = 2 * kCopyMoves * VPR / kCopyThreads;
+// The moves of the hole-filling layout where there are few heads: kCopyMoves
+// of a head's list a workgroup.
+__global__ __launch_bounds__(kCopyThreads) void mass_copy_kernel(MassArgs a, int nchunk) {
     const int h = blockIdx.x / nchunk, m0 = (blockIdx.x - h * nchunk) * kCopyMoves;
-    const int moves = min(kCopyMoves, a.mv_n[h] - m0);
-    if (moves <= 0) return;
-    const int32_t* src = a.mv_src + (size_t)h * a.max_moves + m0;
-    const int32_t* dst = a.mv_dst + (size_t)h * a.max_moves + m0;
-    char* Kh = K + (size_t)h * head_stride;
-    char* Vh = V + (size_t)h * head_stride;
-    dev::u32x4 b[NV];
-    dev::static_for<NV>([&](auto kc) {
-        constexpr int k = decltype(kc)::value;
-        const int e = threadIdx.x + k * kCopyThreads;
-        const int which = e / (kCopyMoves * VPR), r = e / VPR % kCopyMoves, v = e % VPR;
-        if (r < moves)
-            b[k] = __builtin_nontemporal_load(
-                reinterpret_cast<const dev::u32x4*>((which ? Vh : Kh) + (size_t)src[r] * RB) + v);
-    });
-    dev::static_for<NV>([&](auto kc) {
-        constexpr int k = decltype(kc)::value;
-        const int e = threadIdx.x + k * kCopyThreads;
-        const int which = e / (kCopyMoves * VPR), r = e / VPR % kCopyMoves, v = e % VPR;
-        if (r < moves)
-            __builtin_nontemporal_store(b[k],
-                                        reinterpret_cast<dev::u32x4*>((which ? Vh : Kh) + (size_t)dst[r] * RB) + v);
-    });
+    const size_t at = (size_t)h * a.max_moves + m0;
+    move_rows<kCopyThreads>(a.K + (size_t)h * a.head_stride, a.V + (size_t)h * a.head_stride, a.mv_src + at,
+                            a.mv_dst + at, min(kCopyMoves, a.mv_n[h] - m0), a.vec_shift);
+}
+
+template <int NT, int PER>
+hipError_t select(const MassArgs& a, int P, int mode, hipStream_t s) {
+    constexpr int kFilling = NT == kShortThreads ? kFillCopy : kFill;
+    if (mode == kOrder)
+        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kOrder>), dim3((unsigned)P), dim3(NT), 0, s, a);
+    else
+        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kFilling>), dim3((unsigned)P), dim3(NT), 0, s, a);
+    return hipGetLastError();
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct MassLayout {
-    size_t kept, src, dst, val, n, runs, end;
+    size_t kept, src, dst, val, n, ballots, runs, end;
     int max_moves, nruns;
 };
 
@@ -336,9 +404,11 @@ MassLayout mass_layout(const bkv_dims& d) {
     off = up256(off + 4 * P * m.max_moves);
     m.n = off;
     off = up256(off + 4 * P);
-    m.nruns = d.N_cap > kPerMax * kThreads ? (d.N_cap + kThreads - 1) / kThreads * kWaves : 0;
+    m.nruns = d.N_cap > kPerMax * kLongThreads ? (d.N_cap + kLongThreads - 1) / kLongThreads * (kLongThreads / 64) : 0;
+    m.ballots = off;
+    off = up256(off + 8 * P * (size_t)m.nruns);
     m.runs = off;
-    off = up256(off + 4 * 2 * P * (size_t)m.nruns);
+    off = up256(off + 4 * P * (size_t)m.nruns);
     m.end = off;
     return m;
 }
@@ -364,7 +434,7 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     if (!K || !V || !mass || ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15u))
         return BKV_ERR_INVALID;
     // every launch's threads are counted in 32 bits
-    if ((long long)d->B * d->Hkv > 0xffffffffLL / kThreads) return BKV_ERR_SHAPE;
+    if ((long long)d->B * d->Hkv > 0xffffffffLL / kLongThreads) return BKV_ERR_SHAPE;
     const MassLayout m = mass_layout(*d);
     if (!ws || ws_bytes < m.end || (reinterpret_cast<uintptr_t>(ws) & 15u)) return BKV_ERR_WORKSPACE;
     char* w = static_cast<char*>(ws);
@@ -382,8 +452,9 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     a.kept = kept ? kept : reinterpret_cast<int32_t*>(w + m.kept);
     a.mv_src = reinterpret_cast<int32_t*>(w + m.src);
     a.mv_dst = reinterpret_cast<int32_t*>(w + m.dst);
-    a.mv_val = reinterpret_cast<float*>(w + m.val);
+    a.mv_val = reinterpret_cast<int32_t*>(w + m.val);
     a.mv_n = reinterpret_cast<int32_t*>(w + m.n);
+    a.ballots = reinterpret_cast<unsigned long long*>(w + m.ballots);
     a.runs = reinterpret_cast<int32_t*>(w + m.runs);
     a.nruns = m.nruns;
     a.max_moves = m.max_moves;
@@ -392,33 +463,32 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     a.n_keep = n;
     a.W = d->W;
     a.n_prefix = d->n_prefix;
-    a.fill = flags & BKV_EVICT_FILL;
-    const int most = n < a.N - n ? n : a.N - n;
-    const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
-    if (a.fill && (long long)P * nchunk > 0xffffffffLL / kCopyThreads) return BKV_ERR_SHAPE;
-    const dim3 grid((unsigned)P), block(kThreads);
-    if (a.N <= 4 * kThreads)
-        hipLaunchKernelGGL(mass_select_kernel<4>, grid, block, 0, stream, a);
-    else if (a.N <= 16 * kThreads)
-        hipLaunchKernelGGL(mass_select_kernel<16>, grid, block, 0, stream, a);
-    else if (a.N <= kPerMax * kThreads)
-        hipLaunchKernelGGL(mass_select_kernel<kPerMax>, grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL(mass_select_kernel<0>, grid, block, 0, stream, a);
-    if (hipGetLastError() != hipSuccess) return BKV_ERR_HIP;
-    if (!a.fill) {
-        return launch_compact(*d, ws_layout(*d), K, V, a.kept, ws, stream) == hipSuccess ? BKV_OK : BKV_ERR_HIP;
-    }
     const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
-    const size_t hs = (size_t)d->N_cap * rb;
-    char* k = static_cast<char*>(K);
-    char* v = static_cast<char*>(V);
-    const dim3 cgrid((unsigned)(P * nchunk)), cblock(kCopyThreads);
-    switch (rb) {
-        case 128: hipLaunchKernelGGL(mass_copy_kernel<128>, cgrid, cblock, 0, stream, k, v, a, nchunk, hs); break;
-        case 256: hipLaunchKernelGGL(mass_copy_kernel<256>, cgrid, cblock, 0, stream, k, v, a, nchunk, hs); break;
-        default: hipLaunchKernelGGL(mass_copy_kernel<512>, cgrid, cblock, 0, stream, k, v, a, nchunk, hs); break;
-    }
+    a.K = static_cast<char*>(K);
+    a.V = static_cast<char*>(V);
+    a.head_stride = (size_t)d->N_cap * rb;
+    a.vec_shift = rb == 128 ? 3 : rb == 256 ? 4 : 5;
+    const bool fill = flags & BKV_EVICT_FILL;
+    const int most = n < a.N - n ? n : a.N - n;  // moves of a head at most
+    const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
+    const bool many = P >= kManyHeads && a.N <= kPerMax * kShortThreads && (!fill || most <= kOwnMoves);
+    if (fill && !many && (long long)P * nchunk > 0xffffffffLL / kCopyThreads) return BKV_ERR_SHAPE;
+    const int mode = !fill ? kOrder : many ? kFillCopy : kFill;
+    hipError_t e;
+    if (many)
+        e = a.N <= 16 * kShortThreads ? select<kShortThreads, 16>(a, P, mode, stream)
+                                      : select<kShortThreads, kPerMax>(a, P, mode, stream);
+    else if (a.N <= 8 * kLongThreads)
+        e = select<kLongThreads, 8>(a, P, mode, stream);
+    else if (a.N <= kPerMax * kLongThreads)
+        e = select<kLongThreads, kPerMax>(a, P, mode, stream);
+    else
+        e = select<kLongThreads, 0>(a, P, mode, stream);
+    if (e != hipSuccess) return BKV_ERR_HIP;
+    if (mode == kOrder)
+        return launch_compact(*d, ws_layout(*d), K, V, a.kept, ws, stream) == hipSuccess ? BKV_OK : BKV_ERR_HIP;
+    if (mode == kFill)
+        hipLaunchKernelGGL(mass_copy_kernel, dim3((unsigned)(P * nchunk)), dim3(kCopyThreads), 0, stream, a, nchunk);
     return hipGetLastError() == hipSuccess ? BKV_OK : BKV_ERR_HIP;
 }
 

@@ -93,6 +93,13 @@ def test_many_heads_no_indices_asked_for():
 
 
 @pytest.mark.parametrize("fill", [False, True])
+@pytest.mark.parametrize("Hkv,N,budget", [(255, 700, 600), (256, 700, 600), (256, 5000, 4600), (256, 5000, 2400), (256, 8193, 8000)])
+def test_heads_around_the_many(Hkv, N, budget, fill):
+    # one workgroup moves a head's rows itself from 256 heads on, up to 8192 tokens and 2048 moves
+    run_case(1, Hkv, 64, N, N + 1, budget, 8, 1, "bf16", "exponential", fill)
+
+
+@pytest.mark.parametrize("fill", [False, True])
 def test_within_the_budget_nothing_changes(fill):
     run_case(2, 2, 64, 100, 128, 100, 8, 2, "bf16", "exponential", fill)
     run_case(2, 2, 64, 50, 128, 100, 8, 2, "bf16", "exponential", fill)
