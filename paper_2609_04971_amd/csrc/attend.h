@@ -35,8 +35,10 @@ struct Args {
     float* part_o;        // [row][ns][D] unnormalised sums of exp2(l2 - m) v
     float* part_ml;       // [row][ns][2] m and z = sum of exp2(l2 - m)
     float* row_lse2;      // [B, Hq, T] log2-normalisers, +inf for a row that sees nothing
-    float* logits;        // [own unit][R][lstride] l2 = l log2(e), -inf where not seen
+    float* logits;        // [own unit][R][lstride] l2 = l log2(e), -inf where not seen; null unless kept
     int lstride;
+    int keep;             // Keep: whether and where an item keeps its logits
+    int o_rows;           // rows of a 16-row tile that any item has
     int Hq, Hkv, G, T, R, D;
     int N, N_cap;
     int rows;             // B * Hq * T
@@ -77,6 +79,18 @@ __device__ __forceinline__ Row decode_row(const Args& a, int unit, int seqs, int
     return x;
 }
 
+// The logits of the sequences' own tokens, for the mass: none kept; in LDS
+// until the item ends (stores among the key loads would have to be waited for
+// with them); written as they come, where they do not fit.
+enum Keep { kKeepNone, kKeepLds, kKeepStore };
+constexpr int kPadO = 4, kPadL = 16;  // floats that keep the rows of the LDS arrays apart
+constexpr size_t kLdsRoom = 79 * 1024;  // two workgroups a compute unit
+inline size_t stream_lds(const Args& a) {
+    size_t n = (size_t)4 * a.o_rows * (a.D + kPadO);
+    if (a.keep == kKeepLds) n += (size_t)a.R * (a.seg[1].chunk + kPadL);
+    return n * sizeof(float);
+}
+
 // Workgroups of 256 threads that one launch holds: its threads are counted in
 // 32 bits.
 constexpr long long kMaxBlocks = 0xffffffffLL / 256;
@@ -94,7 +108,8 @@ inline JoinGrid join_grid(const Args& a) {
     g.wpr = a.ns >= kManySplits ? kWaves : 1;
     const int rpb = kWaves / g.wpr;
     g.njoin = a.ns > 1 ? (int)(((long long)a.rows + rpb - 1) / rpb) : 0;
-    g.nchunk = a.mass && a.logits ? (a.seg[1].n + kTokens - 1) / kTokens : 0;
+    // (one split with its logits in LDS has added its weights itself)
+    g.nchunk = a.keep && (a.ns > 1 || a.keep == kKeepStore) ? (a.seg[1].n + kTokens - 1) / kTokens : 0;
     g.blocks = g.njoin + (long long)a.seg[1].units * g.nchunk;
     return g;
 }

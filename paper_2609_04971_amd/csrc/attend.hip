@@ -202,6 +202,25 @@ __device__ __forceinline__ typename E::Q load_q(const Args& a, const Row& x, boo
     return q;
 }
 
+constexpr int kKeptRows = 32;  // rows per unit of kept logits, at most
+
+// Four tokens' weights of one row; what a row that sees nothing has (norm
+// +inf) is 0.
+__device__ __forceinline__ void add_weights(f32x4& sum, f32x4 l2, float norm) {
+    dev::static_for<4>([&](auto c) { sum[decltype(c)::value] += exp2_hw(l2[decltype(c)::value] - norm); });
+}
+
+// mass[0..4) += sum, of which `n` are there.
+__device__ __forceinline__ void add_mass(float* mass, f32x4 sum, int n) {
+    if (n >= 4 && (reinterpret_cast<uintptr_t>(mass) & 15u) == 0) {
+        *reinterpret_cast<f32x4*>(mass) += sum;
+        return;
+    }
+    dev::static_for<4>([&](auto c) {
+        if (decltype(c)::value < n) mass[decltype(c)::value] += sum[decltype(c)::value];
+    });
+}
+
 // ---- streaming kernel ------------------------------------------------------------
 // One work item: up to 16 RT rows of a unit against a chunk of its keys.  The
 // four waves take key groups in turn, each with its own m, z and o, and join
@@ -212,9 +231,12 @@ __device__ __forceinline__ typename E::Q load_q(const Args& a, const Row& x, boo
 template <class E, int D, int RT>
 __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     constexpr int KG = E::kKeys, NT = E::kTiles, DV = E::kDV;
-    constexpr int DP = D + 4;  // padded row of the joined sums
-    __shared__ float s_o[kWaves][16][DP];
-    __shared__ float s_m[kWaves][16], s_z[kWaves][16];
+    constexpr int DP = D + kPadO;  // padded row of the joined sums
+    // the waves' sums, [wave][a.o_rows][DP], and with the logits kept in LDS
+    // those of the item's keys, [R][chunk + kPadL]
+    extern __shared__ __attribute__((aligned(16))) float dyn[];
+    __shared__ float s_m[kWaves][16], s_z[kWaves][16], s_norm[kKeptRows];
+    float* const s_o = dyn;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, g = lane >> 4;
     const bool own = (int)blockIdx.x >= a.items0;
@@ -251,17 +273,13 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     }
     const int k_lo = split * sg.chunk;
     // with the logits kept, keys that no row sees are written too (as -inf)
-    const bool keep = a.logits != nullptr && own;
+    const int keep = own ? a.keep : kKeepNone;
     const int k_hi = min(k_lo + sg.chunk, keep ? len : most);
     const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
     const typename E::elem* V = static_cast<const typename E::elem*>(sg.V) + (long long)unit * sg.cap * D;
-    float* lrow[RT];
-    if (keep)
-        dev::static_for<RT>([&](auto rc) {
-            constexpr int rt = decltype(rc)::value;
-            const int rr = r0 + 16 * rt + col;
-            lrow[rt] = rr < sg.rows ? a.logits + ((long long)unit * a.R + rr) * a.lstride : nullptr;
-        });
+    float* const s_l = dyn + kWaves * a.o_rows * DP;
+    const int lds_stride = sg.chunk + kPadL;
+    float* const glob = keep ? a.logits + (long long)unit * a.R * a.lstride : nullptr;
 
     int k0 = k_lo + KG * wave;
     if (k0 < k_hi) {
@@ -288,10 +306,14 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     p[rt][ti][i] = l;
                     top = fmaxf(top, l);
                 });
-                if (keep && lrow[rt])
+                if (keep && 16 * rt + col < sg.rows)  // a kept unit is one row block
                     dev::static_for<NT>([&](auto tc) {
                         constexpr int ti = decltype(tc)::value;
-                        *reinterpret_cast<f32x4*>(lrow[rt] + k0 + 16 * ti + 4 * g) = p[rt][ti];
+                        const int at = k0 + 16 * ti + 4 * g;
+                        if (keep == kKeepLds)
+                            *reinterpret_cast<f32x4*>(s_l + (16 * rt + col) * lds_stride + at - k_lo) = p[rt][ti];
+                        else
+                            *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = p[rt][ti];
                     });
                 top = fmaxf(top, dev::shfl_xor_f(top, 16));
                 top = fmaxf(top, dev::shfl_xor_f(top, 32));
@@ -323,14 +345,15 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
             s_m[wave][col] = m[rt];
             s_z[wave][col] = zz;
         }
-        dev::static_for<4>([&](auto ic) {
-            constexpr int i = decltype(ic)::value;
-            dev::static_for<DV / 4>([&](auto cc) {
-                constexpr int c = decltype(cc)::value;
-                *reinterpret_cast<f32x4*>(&s_o[wave][col][DV * (4 * g + i) + 4 * c]) =
-                    f32x4{o[rt][4 * c][i], o[rt][4 * c + 1][i], o[rt][4 * c + 2][i], o[rt][4 * c + 3][i]};
+        if (col < a.o_rows)
+            dev::static_for<4>([&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                dev::static_for<DV / 4>([&](auto cc) {
+                    constexpr int c = decltype(cc)::value;
+                    *reinterpret_cast<f32x4*>(s_o + (wave * a.o_rows + col) * DP + DV * (4 * g + i) + 4 * c) =
+                        f32x4{o[rt][4 * c][i], o[rt][4 * c + 1][i], o[rt][4 * c + 2][i], o[rt][4 * c + 3][i]};
+                });
             });
-        });
         __syncthreads();
         constexpr int VPR = D / 4;  // 16-byte vectors of a row
         for (int e = threadIdx.x; e < 16 * VPR; e += kThreads) {
@@ -344,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
             for (int w = 0; w < kWaves; ++w) {
                 const float f = exp2_hw(s_m[w][r] - M);
                 Z += f * s_z[w][r];
-                sum += f * *reinterpret_cast<const f32x4*>(&s_o[w][r][4 * v]);
+                sum += f * *reinterpret_cast<const f32x4*>(s_o + (w * a.o_rows + r) * DP + 4 * v);
             }
             const Row x = decode_row(a, unit, sg.seqs, rr);
             if (a.ns > 1) {
@@ -362,11 +385,26 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     const float l2 = M + log2f(Z);
                     if (a.lse) a.lse[x.lse] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
                     if (a.mass) a.row_lse2[x.lse] = Z > 0.f ? l2 : INFINITY;
+                    if (keep) s_norm[16 * rt + r] = Z > 0.f ? l2 : INFINITY;
                 }
             }
         }
         __syncthreads();
     });
+    if (keep != kKeepLds) return;
+    // the kept logits: their weights, or on to the join where other splits
+    // have a say in the normalisers
+    for (int j = 4 * (int)threadIdx.x; j < k_hi - k_lo; j += 4 * kThreads) {
+        if (a.ns > 1) {
+            for (int r = 0; r < a.R; ++r)
+                *reinterpret_cast<f32x4*>(glob + (long long)r * a.lstride + k_lo + j) =
+                    *reinterpret_cast<const f32x4*>(s_l + r * lds_stride + j);
+        } else {
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < a.R; ++r) add_weights(sum, *reinterpret_cast<const f32x4*>(s_l + r * lds_stride + j), s_norm[r]);
+            add_mass(a.mass + (long long)unit * a.N_cap + k_lo + j, sum, k_hi - k_lo - j);
+        }
+    }
 }
 
 // ---- joining the partials, and the weights of kept logits --------------------------
@@ -443,8 +481,6 @@ __device__ __forceinline__ void join_rows(const Args& a) {
     }
 }
 
-constexpr int kKeptRows = 32;  // rows per unit of kept logits, at most
-
 __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
     __shared__ float s_m[kThreads], s_z[kThreads], s_norm[kKeptRows];
     const int unit = item / nchunk, ch = item % nchunk;
@@ -485,19 +521,9 @@ __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
     const float* l = a.logits + row0 * a.lstride + j;
 #pragma unroll 4
     for (int r = 0; r < a.R; ++r) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(l + (long long)r * a.lstride);
-        const float norm = s_norm[r];
-        dev::static_for<4>([&](auto c) { sum[decltype(c)::value] += exp2_hw(x[decltype(c)::value] - norm); });
+        add_weights(sum, *reinterpret_cast<const f32x4*>(l + (long long)r * a.lstride), s_norm[r]);
     }
-    float* mass = a.mass + (long long)unit * a.N_cap + j;
-    if (j + 4 <= len && (reinterpret_cast<uintptr_t>(mass) & 15u) == 0) {
-        *reinterpret_cast<f32x4*>(mass) += sum;
-        return;
-    }
-    dev::static_for<4>([&](auto c) {
-        constexpr int i = decltype(c)::value;
-        if (j + i < len) mass[i] += sum[i];
-    });
+    add_mass(a.mass + (long long)unit * a.N_cap + j, sum, len - j);
 }
 
 template <class E, int D, int WPR>
@@ -556,9 +582,9 @@ hipError_t stream(const Args& a, bool wide, hipStream_t s) {
     const long long items = a.items0 + (long long)a.seg[1].units * a.seg[1].nrb * a.seg[1].ns;
     if (items == 0) return hipSuccess;
     if (wide)
-        hipLaunchKernelGGL((stream_kernel<E, D, 2>), dim3((unsigned)items), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((stream_kernel<E, D, 2>), dim3((unsigned)items), dim3(kThreads), stream_lds(a), s, a);
     else
-        hipLaunchKernelGGL((stream_kernel<E, D, 1>), dim3((unsigned)items), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((stream_kernel<E, D, 1>), dim3((unsigned)items), dim3(kThreads), stream_lds(a), s, a);
     return hipGetLastError();
 }
 

@@ -210,6 +210,11 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     a.row_lse2 = reinterpret_cast<float*>(w + p.row_lse2);
     a.logits = p.keep ? reinterpret_cast<float*>(w + p.logits) : nullptr;
     a.lstride = (int)up((size_t)d->N, 32);
+    a.o_rows = a.R;
+    if (!p.pre_tile && pre.units > 0 && pre.rows > a.o_rows) a.o_rows = pre.rows;
+    if (a.o_rows > 16) a.o_rows = 16;
+    a.keep = p.keep ? kKeepLds : kKeepNone;
+    if (p.keep && stream_lds(a) > kLdsRoom) a.keep = kKeepStore;
     if (join_grid(a).blocks > kMaxBlocks) return BKV_ERR_SHAPE;
     if (p.pre_tile && launch_attend_tile(a, pre, stream) != hipSuccess) return BKV_ERR_HIP;
     if (p.own_tile && launch_attend_tile(a, own, stream) != hipSuccess) return BKV_ERR_HIP;
