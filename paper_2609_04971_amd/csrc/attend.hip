@@ -88,10 +88,10 @@ struct Bf16 {
     // o += V^T P^T.  The weights go in as two bf16 terms, high part and rest,
     // so that their rounding (2^-17) stays below the output's own: the
     // streaming kernel waits for memory, and the second product is free.
-    template <int RT>
+    template <int NR, int RT>
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
-        bf16x8_t hi[RT], lo[RT];
-        dev::static_for<RT>([&](auto rc) {
+        bf16x8_t hi[NR], lo[NR];
+        dev::static_for<NR>([&](auto rc) {
             constexpr int rt = decltype(rc)::value;
             dev::static_for<8>([&](auto jc) {
                 constexpr int j = decltype(jc)::value;
@@ -110,7 +110,7 @@ struct Bf16 {
                 t[i] = __builtin_amdgcn_perm(v.v[2 * i + 1][dd / 2], v.v[2 * i][dd / 2], sel);
             });
             const bf16x8_t a = __builtin_bit_cast(bf16x8_t, t);
-            dev::static_for<RT>([&](auto rc) {
+            dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[rt], o[rt][dd], 0, 0, 0);
                 o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[rt], o[rt][dd], 0, 0, 0);
@@ -163,13 +163,13 @@ struct F32 {
         });
         s[0] = acc;
     }
-    template <int RT>
+    template <int NR, int RT>
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][1]) {
         dev::static_for<4>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
             dev::static_for<kDV>([&](auto dc) {
                 constexpr int dd = decltype(dc)::value;
-                dev::static_for<RT>([&](auto rc) {
+                dev::static_for<NR>([&](auto rc) {
                     constexpr int rt = decltype(rc)::value;
                     o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.v[j][dd / 4][dd % 4], p[rt][0][j], o[rt][dd], 0,
                                                                      0, 0);
@@ -281,8 +281,11 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     const int lds_stride = sg.chunk + kPadL;
     float* const glob = keep ? a.logits + (long long)unit * a.R * a.lstride : nullptr;
 
-    int k0 = k_lo + KG * wave;
-    if (k0 < k_hi) {
+    // the keys, for the first NR row tiles
+    auto walk = [&](auto nc) __attribute__((always_inline)) {
+        constexpr int NR = decltype(nc)::value;
+        int k0 = k_lo + KG * wave;
+        if (k0 >= k_hi) return;
         const int last = k_hi - 1;  // rows past it repeat it: nothing behind a sequence is read
         typename E::K kr;
         typename E::V vr;
@@ -290,13 +293,13 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         E::load_v(vr, V, k0, last, lane);
         for (; k0 < k_hi; k0 += KG * kWaves) {
             f32x4 p[RT][NT];
-            dev::static_for<RT>([&](auto rc) {
+            dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 E::logits(p[rt], kr, q[rt]);
             });
             E::load_k(kr, K, k0 + KG * kWaves, last, lane);
             const bool edge = k0 + KG > min(least, k_hi);
-            dev::static_for<RT>([&](auto rc) {
+            dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 float top = kLowest;
                 dev::static_for<NT * 4>([&](auto ic) {
@@ -330,9 +333,17 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     z[rt] += e;
                 });
             });
-            E::template values<RT>(o, vr, p);
+            E::template values<NR>(o, vr, p);
             E::load_v(vr, V, k0 + KG * kWaves, last, lane);
         }
+    };
+    if constexpr (RT == 2) {
+        if (sg.rows - r0 <= 16)
+            walk(std::integral_constant<int, 1>{});
+        else
+            walk(std::integral_constant<int, 2>{});
+    } else {
+        walk(std::integral_constant<int, 1>{});
     }
 
     // join the waves, one row tile at a time

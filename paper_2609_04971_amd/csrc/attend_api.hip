@@ -12,7 +12,7 @@ namespace {
 constexpr size_t kAlign = 256;
 inline size_t up(size_t x, size_t n) { return (x + n - 1) / n * n; }
 
-constexpr int kStreamItems = 768;   // streaming work items: three per compute unit are resident
+constexpr int kCus = 256;
 constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a streaming item, two tiles
 constexpr int kWhole = 512;         // keys that one streaming item takes rather than a join
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
@@ -21,44 +21,51 @@ constexpr int kMassItems = 2048;    // workgroups that sum the weights of many r
 constexpr int kMassRows = 1024;     // rows that make such a workgroup worth its own sums
 constexpr int kMassBlock = 128;     // keys of one
 
-// Splits of n keys for the streaming kernel: as many items as are resident.
-int stream_splits(long long base, int n) {
-    const long long want = base > 0 ? (kStreamItems + base - 1) / base : 1;
-    const long long most = (n + kMinChunk - 1) / kMinChunk;
-    const long long k = want < most ? want : most;
-    return (int)(k > 1 ? k : 1);
-}
-
-int most_tile_splits(long long base, int n) {
-    constexpr int kMost = 64, kItems = 1024;
+// Splits of n keys at most, of `base` items each: what a workspace has room for.
+int most_splits(long long base, int n) {
+    constexpr int kMost = 256, kItems = 1024;
     const long long k = base > 0 ? kItems / base + 1 : 1, by_keys = (n + kMinChunk - 1) / kMinChunk;
     const long long least = k < by_keys ? k : by_keys;
     return (int)(least > kMost ? kMost : least > 1 ? least : 1);
 }
 
-// Splits of n keys for the tile kernel, `base` items each, by what they cost
-// in keys of one item that has a compute unit to itself: the rounds of items
-// times their keys and what an item costs around them (kItemKeys), and the
-// partials' way through memory.  With 2 or 3 items on a compute unit a round
-// takes 1.7 or 2.4 times as long.
-int tile_splits(long long base, int n, long long rows, int D) {
-    constexpr int kCus = 256;
-    constexpr float kItemKeys = 100.f, kRound[4] = {0.f, 1.f, 1.7f, 2.4f};
+// Splits of n keys, `base` items each, by what they cost in keys of one item
+// that has a compute unit to itself: the rounds of items times their keys and
+// what an item costs around them, and the partials' way through memory.
+// Streaming items share their compute unit's bandwidth, so that a round is as
+// many items as there are compute units; tile items share its matrix cores
+// only in part: 2 or 3 of them at once take 1.7 or 2.4 times as long as one.
+// us, splits as taken (*) and others, streaming: 8 heads x 65536 tokens 32* 49,
+// 64 50, 96 53, 256 57; 192 x 4000 1 78, 3 78, 4* 67, 6 76; 160 x 6000 (ragged)
+// 2 105, 3 79, 7 74, 8* 74; 296 x 2000 fp32 1 143, 2 127, 4 119; tile: 112
+// blocks of 500 x 7 queries against 24000 3 146, 4 119, 5 135, 9* 113, 19 138.
+int best_splits(bool tile, long long base, int n, long long rows, int D) {
+    constexpr float kRound[4] = {0.f, 1.f, 1.7f, 2.4f};
     constexpr float kJoinKeys = 43.f * 8.f / 4e6f;  // keys in the time that 8 bytes take at 4 TB/s
-    const int resident = D == 128 ? 2 : 3;          // items per compute unit
-    const int most = most_tile_splits(base, n);
+    const int resident = !tile ? 1 : D == 128 ? 2 : 3;
+    const float around = tile ? 100.f : 64.f;
+    const int most = most_splits(base, n);
     int best = 1;
     float least = 0.f;
     for (int k = 1; k <= most; ++k) {
         const long long items = base * k, full = items / (resident * kCus), rest = items % (resident * kCus);
         const float rounds = (float)full * kRound[resident] + kRound[(rest + kCus - 1) / kCus];
-        const float cost = rounds * ((float)n / (float)k + kItemKeys) + (k > 1 ? (float)rows * (float)(k * D) * kJoinKeys : 0.f);
+        const float cost = rounds * ((float)n / (float)k + around) + (k > 1 ? (float)rows * (float)(k * D) * kJoinKeys : 0.f);
         if (k == 1 || cost < least) {
             least = cost;
             best = k;
         }
     }
     return best;
+}
+
+// Splits of a segment of n keys that is streamed together with another: the
+// items of both fill one another's last rounds, so that none has to be
+// shorter than half of a compute unit's share of all keys.
+int shared_splits(long long base, int n, long long all_keys) {
+    const long long chunk = all_keys / (2 * kCus) > kMinChunk ? all_keys / (2 * kCus) : kMinChunk;
+    const long long k = (n + chunk - 1) / chunk, most = most_splits(base, n);
+    return (int)(k < 1 ? 1 : k < most ? k : most);
 }
 
 // Splits of n keys (at most those of the capacity) and their length.
@@ -82,15 +89,21 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
     const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
-    // a short cache in one piece: joining splits would be a launch of its own.  Not by
-    // the mass: outputs do not depend on whether it is asked for
-    const bool whole = groups == 0 && !p.own_tile && d.N <= kWhole;
-    int ns_cap = p.own_tile ? most_tile_splits(own, d.N_cap) : stream_splits(own, d.N_cap);
-    cut(d.N, whole ? 1 : p.own_tile ? tile_splits(own, d.N, rows, d.D) : stream_splits(own, d.N), &p.own_ns, &p.own_chunk);
-    if (groups > 0) {
-        ns_cap += p.pre_tile ? most_tile_splits(pre, P_cap) : stream_splits(pre, P_cap);
-        if (P > 0) cut(P, p.pre_tile ? tile_splits(pre, P, rows, d.D) : stream_splits(pre, P), &p.pre_ns, &p.pre_chunk);
+    int ns_cap = most_splits(own, d.N_cap), own_ns, pre_ns = 1;
+    if (groups > 0) ns_cap += most_splits(pre, P_cap);
+    if (groups > 0 && P > 0 && !p.own_tile && !p.pre_tile) {  // one launch takes both
+        const long long all = own * d.N + pre * P;
+        own_ns = shared_splits(own, d.N, all);
+        pre_ns = shared_splits(pre, P, all);
+    } else {
+        // a short cache goes in one piece: joining splits would be a launch of
+        // its own.  Not by the mass: outputs do not depend on whether it is asked for
+        const bool whole = groups == 0 && !p.own_tile && d.N <= kWhole;
+        own_ns = whole ? 1 : best_splits(p.own_tile, own, d.N, rows, d.D);
+        if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile, pre, P, rows, d.D);
     }
+    cut(d.N, own_ns, &p.own_ns, &p.own_chunk);
+    if (groups > 0 && P > 0) cut(P, pre_ns, &p.pre_ns, &p.pre_chunk);
     p.keep = mass && R <= kFewRows;
     size_t off = 0;
     p.part_o = off;
