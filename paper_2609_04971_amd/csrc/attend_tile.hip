@@ -141,10 +141,8 @@ struct State {
     float m, z;
 };
 
-// A row's maximum follows the logits only once they pass it by this much
-// (log2): rescaling the sums on every small rise cost more than weights of up
-// to 2^8 do.
-constexpr float kSlack = 8.f;
+// New weights of a lane that call for another maximum.
+constexpr float kMost = 16777216.f;
 
 // Kinds of instructions for the scheduler.
 constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100;
@@ -187,26 +185,36 @@ __device__ __forceinline__ void tile_step(State<D>& st, const Offsets<D>& at, co
             if (k0 + 32 * kt + 8 * (i / 4) + h4 + i % 4 >= lim) s[kt][i] = -INFINITY;
         });
     }
-    float top = s[0][0];
-    dev::static_for<31>([&](auto ic) {
-        constexpr int e = decltype(ic)::value + 1;
-        top = fmaxf(top, s[e / 16][e % 16]);
-    });
-    top = max_halves(top) * scale2;
-    if (__any(top > st.m + kSlack)) {
+    // The exponentials are taken against the running maximum as it stands: the
+    // sums are floats, so a weight may be far above 1, and only where a lane's
+    // new weights pass kMost (the first tile's, whose m is the lowest float,
+    // always do) is the maximum looked for and everything brought down to it.
+    // That spares the common tile the search and its wait for every logit.
+    bf16x8_t p[4];
+    float z;
+    auto weights = [&]() __attribute__((always_inline)) {
+        z = 0.f;
+        dev::static_for<32>([&](auto ic) {
+            constexpr int kt = decltype(ic)::value / 16, i = decltype(ic)::value % 16;
+            const float e = exp2_hw(__builtin_fmaf(s[kt][i], scale2, -st.m));
+            z += e;
+            p[2 * kt + i / 8][i % 8] = (__bf16)e;
+        });
+    };
+    weights();
+    if (__any(!(z <= kMost))) {
+        float top = s[0][0];
+        dev::static_for<31>([&](auto ic) {
+            constexpr int e = decltype(ic)::value + 1;
+            top = fmaxf(top, s[e / 16][e % 16]);
+        });
+        top = max_halves(top) * scale2;
         const float mn = fmaxf(st.m, top), f = exp2_hw(st.m - mn);
         st.m = mn;
         st.z *= f;
         dev::static_for<DT>([&](auto dc) { st.o[decltype(dc)::value] *= f; });
+        weights();
     }
-    bf16x8_t p[4];
-    float z = 0.f;
-    dev::static_for<32>([&](auto ic) {
-        constexpr int kt = decltype(ic)::value / 16, i = decltype(ic)::value % 16;
-        const float e = exp2_hw(__builtin_fmaf(s[kt][i], scale2, -st.m));
-        z += e;
-        p[2 * kt + i / 8][i % 8] = (__bf16)e;
-    });
     st.z += z;
     dev::static_for<4>([&](auto cc) {
         constexpr int c = decltype(cc)::value;
@@ -215,17 +223,12 @@ __device__ __forceinline__ void tile_step(State<D>& st, const Offsets<D>& at, co
             st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_frag<D>(vs, at.v[dt], c), p[c], st.o[dt], 0, 0, 0);
         });
     });
-    // the first values are requested before the exponentials, the others
-    // between the products, and so are the exponentials of the later keys
-    constexpr int kFirst = 28, kRest = (112 - kFirst + 3 * DT - 1) / (3 * DT);
-    __builtin_amdgcn_sched_group_barrier(kSchedLds, 2 * DT, 1);
-    __builtin_amdgcn_sched_group_barrier(kSchedValu, kFirst, 1);
-    dev::static_for<3 * DT>([&](auto) {
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, 8, 1);
+    dev::static_for<4 * DT - 4>([&](auto) {
         __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
         __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 1);
-        __builtin_amdgcn_sched_group_barrier(kSchedValu, kRest, 1);
     });
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, DT, 1);
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 1);
 }
 
 template <int D>

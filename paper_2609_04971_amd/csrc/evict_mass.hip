@@ -32,7 +32,10 @@ constexpr int kBins = 4096;
 constexpr int kPerMax = 32;    // tokens per thread in registers
 constexpr int kLongThreads = 1024;  // threads per head, and few where heads are many and short
 constexpr int kShortThreads = 256;
-constexpr int kManyHeads = 256;
+// Heads from which on a workgroup of kShortThreads selects and moves (us, that
+// and the other form, 4096 -> 3584 filling holes: 128 heads 31 26, 256 40 40, 512
+// 65 75, 2048 217 268; 8192 -> 7168: 256 73 67, 384 99 100, 768 167 183).
+constexpr int kManyHeads = 256, kManyLongHeads = 384;
 constexpr int kOwnMoves = kBins / 2;  // moves that the selecting workgroup's lists hold
 constexpr int kCopyThreads = 256;
 constexpr int kCopyMoves = 64;  // rows per copy item
@@ -163,9 +166,14 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
                 f(i * NW + wave, tid + i * NT, v);
             });
         } else {
-            for (int i = 0; i < NI; ++i) {
-                const int j = tid + i * NT;
-                f(i * NW + wave, j, mass[min(j, N - 1)]);
+            constexpr int kAhead = 8;  // loads in flight
+            for (int i0 = 0; i0 < NI; i0 += kAhead) {
+                float v[kAhead];
+                dev::static_for<kAhead>([&](auto kc) { v[decltype(kc)::value] = mass[min(tid + (i0 + decltype(kc)::value) * NT, N - 1)]; });
+                dev::static_for<kAhead>([&](auto kc) {
+                    const int i = i0 + decltype(kc)::value;
+                    if (i < NI) f(i * NW + wave, tid + i * NT, v[decltype(kc)::value]);
+                });
             }
         }
     };
@@ -309,7 +317,7 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
         each([&](int run, int j, float v) {
             const unsigned long long k = ballots[run];
             const int rank = runs[run] + __builtin_popcountll(k & below);
-            if (PER == 0) __syncthreads();  // rank <= j: what a pass writes, it and the ones before it have read
+            if (PER == 0) __syncthreads();  // rank <= j: what is written here, every thread has read
             if ((k >> lane) & 1) {
                 kept[rank] = j;
                 mass[rank] = v;
@@ -471,7 +479,8 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     const bool fill = flags & BKV_EVICT_FILL;
     const int most = n < a.N - n ? n : a.N - n;  // moves of a head at most
     const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
-    const bool many = P >= kManyHeads && a.N <= kPerMax * kShortThreads && (!fill || most <= kOwnMoves);
+    const bool many = P >= (a.N <= 16 * kShortThreads ? kManyHeads : kManyLongHeads) &&
+                      a.N <= kPerMax * kShortThreads && (!fill || most <= kOwnMoves);
     if (fill && !many && (long long)P * nchunk > 0xffffffffLL / kCopyThreads) return BKV_ERR_SHAPE;
     const int mode = !fill ? kOrder : many ? kFillCopy : kFill;
     hipError_t e;

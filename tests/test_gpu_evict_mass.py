@@ -93,9 +93,10 @@ def test_many_heads_no_indices_asked_for():
 
 
 @pytest.mark.parametrize("fill", [False, True])
-@pytest.mark.parametrize("Hkv,N,budget", [(255, 700, 600), (256, 700, 600), (256, 5000, 4600), (256, 5000, 2400), (256, 8193, 8000)])
+@pytest.mark.parametrize("Hkv,N,budget", [(255, 700, 600), (256, 700, 600), (256, 5000, 4600), (256, 5000, 2400), (256, 8193, 8000),
+                                          (383, 4097, 3900), (384, 4097, 3900), (384, 8192, 7500), (384, 5000, 2400)])
 def test_heads_around_the_many(Hkv, N, budget, fill):
-    # one workgroup moves a head's rows itself from 256 heads on, up to 8192 tokens and 2048 moves
+    # one workgroup moves a head's rows itself from 256 heads on (384 of more than 4096 tokens), up to 8192 tokens and 2048 moves
     run_case(1, Hkv, 64, N, N + 1, budget, 8, 1, "bf16", "exponential", fill)
 
 
