@@ -221,6 +221,12 @@ __device__ __forceinline__ void add_mass(float* mass, f32x4 sum, int n) {
     });
 }
 
+// Pointers into LDS keep their address space, and an index is whole before it
+// is added: an LDS address that wraps below its array's start on the way is
+// none any more once it is widened.
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
 // ---- streaming kernel ------------------------------------------------------------
 // One work item: up to 16 RT rows of a unit against a chunk of its keys.  The
 // four waves take key groups in turn, each with its own m, z and o, and join
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     // those of the item's keys, [R][chunk + kPadL]
     extern __shared__ __attribute__((aligned(16))) float dyn[];
     __shared__ float s_m[kWaves][16], s_z[kWaves][16], s_norm[kKeptRows];
-    float* const s_o = dyn;
+    lds_float* const s_o = (lds_float*)dyn;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, g = lane >> 4;
     const bool own = (int)blockIdx.x >= a.items0;
@@ -277,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     const int k_hi = min(k_lo + sg.chunk, keep ? len : most);
     const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
     const typename E::elem* V = static_cast<const typename E::elem*>(sg.V) + (long long)unit * sg.cap * D;
-    float* const s_l = dyn + kWaves * a.o_rows * DP;
+    lds_float* const s_l = s_o + kWaves * a.o_rows * DP;
     const int lds_stride = sg.chunk + kPadL;
     float* const glob = keep ? a.logits + (long long)unit * a.R * a.lstride : nullptr;
 
@@ -314,7 +320,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                         constexpr int ti = decltype(tc)::value;
                         const int at = k0 + 16 * ti + 4 * g;
                         if (keep == kKeepLds)
-                            *reinterpret_cast<f32x4*>(s_l + (16 * rt + col) * lds_stride + at - k_lo) = p[rt][ti];
+                            *(lds_f32x4*)(s_l + ((16 * rt + col) * lds_stride + (at - k_lo))) = p[rt][ti];
                         else
                             *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = p[rt][ti];
                     });
@@ -361,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                 constexpr int i = decltype(ic)::value;
                 dev::static_for<DV / 4>([&](auto cc) {
                     constexpr int c = decltype(cc)::value;
-                    *reinterpret_cast<f32x4*>(s_o + (wave * a.o_rows + col) * DP + DV * (4 * g + i) + 4 * c) =
+                    *(lds_f32x4*)(s_o + ((wave * a.o_rows + col) * DP + DV * (4 * g + i) + 4 * c)) =
                         f32x4{o[rt][4 * c][i], o[rt][4 * c + 1][i], o[rt][4 * c + 2][i], o[rt][4 * c + 3][i]};
                 });
             });
@@ -378,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
             for (int w = 0; w < kWaves; ++w) {
                 const float f = exp2_hw(s_m[w][r] - M);
                 Z += f * s_z[w][r];
-                sum += f * *reinterpret_cast<const f32x4*>(s_o + (w * a.o_rows + r) * DP + 4 * v);
+                sum += f * *(const lds_f32x4*)(s_o + ((w * a.o_rows + r) * DP + 4 * v));
             }
             const Row x = decode_row(a, unit, sg.seqs, rr);
             if (a.ns > 1) {
@@ -409,10 +415,10 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         if (a.ns > 1) {
             for (int r = 0; r < a.R; ++r)
                 *reinterpret_cast<f32x4*>(glob + (long long)r * a.lstride + k_lo + j) =
-                    *reinterpret_cast<const f32x4*>(s_l + r * lds_stride + j);
+                    *(const lds_f32x4*)(s_l + (r * lds_stride + j));
         } else {
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            for (int r = 0; r < a.R; ++r) add_weights(sum, *reinterpret_cast<const f32x4*>(s_l + r * lds_stride + j), s_norm[r]);
+            for (int r = 0; r < a.R; ++r) add_weights(sum, *(const lds_f32x4*)(s_l + (r * lds_stride + j)), s_norm[r]);
             add_mass(a.mass + (long long)unit * a.N_cap + k_lo + j, sum, k_hi - k_lo - j);
         }
     }
