@@ -14,7 +14,11 @@ inline size_t up(size_t x, size_t n) { return (x + n - 1) / n * n; }
 
 constexpr int kCus = 256;
 constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a streaming item, two tiles
-constexpr int kWhole = 512;         // keys that one streaming item takes rather than a join
+// Bytes of a unit's keys that one streaming item takes rather than splits and a
+// join: the second launch costs 3.2 us, a round of 32 bf16 or 16 fp32 keys a
+// wave 1.1 (us captured, in one piece and split, 8 heads of 128: bf16 256 tokens
+// 6.3 8.3, 512 8.4 8.4, 768 10.7 8.4; fp32 256 9.1 9.8, 400 12.4 10.0).
+constexpr long long kWhole = 128 << 10;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
 constexpr int kMassItems = 2048;    // workgroups that sum the weights of many rows, at least
@@ -98,7 +102,8 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     } else {
         // a short cache goes in one piece: joining splits would be a launch of
         // its own.  Not by the mass: outputs do not depend on whether it is asked for
-        const bool whole = groups == 0 && !p.own_tile && d.N <= kWhole;
+        const bool whole = groups == 0 && !p.own_tile &&
+                           (long long)d.N * d.D * (d.dtype == BKV_BF16 ? 2 : 4) <= kWhole;
         own_ns = whole ? 1 : best_splits(p.own_tile, own, d.N, rows, d.D);
         if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile, pre, P, rows, d.D);
     }
