@@ -51,11 +51,15 @@ int best_splits(bool tile, long long base, int n, long long rows, int D) {
     const int most = most_splits(base, n);
     int best = 1;
     float least = 0.f;
-    for (int k = 1; k <= most; ++k) {
+    // one piece, or as many as 1 to 4 items per compute unit take: in between
+    // a round is begun and not filled
+    for (int j = 0; j <= 4; ++j) {
+        const long long fills = j == 0 || base > j * kCus ? 1 : j * kCus / base;
+        const int k = fills < most ? (int)fills : most;
         const long long items = base * k, full = items / (resident * kCus), rest = items % (resident * kCus);
         const float rounds = (float)full * kRound[resident] + kRound[(rest + kCus - 1) / kCus];
         const float cost = rounds * ((float)n / (float)k + around) + (k > 1 ? (float)rows * (float)(k * D) * kJoinKeys : 0.f);
-        if (k == 1 || cost < least) {
+        if (j == 0 || cost < least) {
             least = cost;
             best = k;
         }
@@ -169,6 +173,9 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     if (d->N > 0 && (!K || !V || !aligned(K) || !aligned(V))) return BKV_ERR_INVALID;
     if (groups > 0 && P > 0 && (!PK || !PV || !aligned(PK) || !aligned(PV))) return BKV_ERR_INVALID;
     if (!(scale >= 0.0f) || isinf(scale)) return BKV_ERR_INVALID;
+    const size_t q_bytes = (size_t)d->B * d->Hq * T * d->D * (d->dtype == BKV_BF16 ? 2 : 4);
+    const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
+    if (q0 < o0 + q_bytes && o0 < q0 + q_bytes) return BKV_ERR_INVALID;  // queries are read after outputs are written
     const Plan p = make_plan(*d, T, mass != nullptr, groups, P, P_cap);
     if (p.end > 0 && (!ws || ws_bytes < p.end || !aligned(ws))) return BKV_ERR_WORKSPACE;
     char* w = static_cast<char*>(ws);

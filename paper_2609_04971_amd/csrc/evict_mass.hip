@@ -55,6 +55,8 @@ struct MassArgs {
     int32_t* runs;
     int nruns, max_moves;
     int N, N_cap, n_keep, W, n_prefix;
+    int* hdr;  // the workspace's stamp
+    int P, budget;
     // the rows, for workgroups that move them themselves
     char* K;
     char* V;
@@ -138,7 +140,7 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
     __shared__ int buf[NW];
     __shared__ unsigned s_min[NW], s_max[NW], s_cand[64];
     __shared__ int s_cand_j[64];
-    __shared__ int s_bin, s_above, s_count, s_n, s_j;
+    __shared__ int s_bin, s_above, s_count, s_n, s_j, s_ok;
     __shared__ unsigned s_theta;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = blockIdx.x, N = a.N, n = a.n_keep;
@@ -156,6 +158,12 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
             val[i] = mass[min(tid + i * NT, N - 1)];
         });
     }
+    if (tid == 0) {
+        s_ok = dev::stamp_ok(a.hdr, a.P, a.budget);
+        if (!s_ok) dev::raise_error(a.hdr, kErrStamp);
+    }
+    __syncthreads();
+    if (!s_ok) return;  // nothing has been written
     // f(run, token, value) for every token of this thread, whole waves at a time
     auto each = [&](auto&& f) {
         if constexpr (PER > 0) {
@@ -370,6 +378,7 @@ __global__ void mass_identity_kernel(int32_t* kept, int n, long long total) {
 // The moves of the hole-filling layout where there are few heads: kCopyMoves
 // of a head's list a workgroup.
 __global__ __launch_bounds__(kCopyThreads) void mass_copy_kernel(MassArgs a, int nchunk) {
+    if (!dev::stamp_ok(a.hdr, a.P, a.budget)) return;  // the lists were not written
     const int h = blockIdx.x / nchunk, m0 = (blockIdx.x - h * nchunk) * kCopyMoves;
     const size_t at = (size_t)h * a.max_moves + m0;
     move_rows<kCopyThreads>(a.K + (size_t)h * a.head_stride, a.V + (size_t)h * a.head_stride, a.mv_src + at,
@@ -471,6 +480,9 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     a.n_keep = n;
     a.W = d->W;
     a.n_prefix = d->n_prefix;
+    a.hdr = reinterpret_cast<int*>(w);
+    a.P = P;
+    a.budget = d->budget;
     const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
     a.K = static_cast<char*>(K);
     a.V = static_cast<char*>(V);

@@ -9,6 +9,7 @@ import torch
 import paper_2609_04971_amd as bkv
 
 P = ctypes.c_void_p(1 << 20)    # 16-byte aligned stand-ins, never dereferenced
+OUT = ctypes.c_void_p(1 << 28)
 ODD = ctypes.c_void_p((1 << 20) + 8)
 BIG = 1 << 40
 
@@ -17,12 +18,12 @@ def dims(**kw):
     return bkv.dims(B=4, Hq=8, Hkv=2, D=128, N=1000, N_cap=1100, W=8, C=0, budget=256, n_prefix=2).replace(**kw)
 
 
-def attend(d=None, flags=0, q=P, T=1, K=P, V=P, lens=None, scale=0.0, out=P, lse=None, mass=None, ws=P, n=BIG):
+def attend(d=None, flags=0, q=P, T=1, K=P, V=P, lens=None, scale=0.0, out=OUT, lse=None, mass=None, ws=P, n=BIG):
     d = dims() if d is None else d
     return bkv.lib().bkv_attend(ctypes.byref(d), flags, q, T, K, V, lens, scale, out, lse, mass, ws, n, None)
 
 
-def shared(d=None, flags=0, q=P, T=1, groups=2, PK=P, PV=P, n_pre=50, P_cap=60, p_lens=None, K=P, V=P, scale=0.0, out=P,
+def shared(d=None, flags=0, q=P, T=1, groups=2, PK=P, PV=P, n_pre=50, P_cap=60, p_lens=None, K=P, V=P, scale=0.0, out=OUT,
            mass=None, ws=P, n=BIG):
     d = dims() if d is None else d
     return bkv.lib().bkv_attend_shared(ctypes.byref(d), flags, q, T, groups, PK, PV, n_pre, P_cap, p_lens, K, V, None,
@@ -47,6 +48,8 @@ def evict(d=None, flags=0, K=P, V=P, mass=P, kept=P, ws=P, n=BIG):
     (dict(K=None), bkv.ERR_INVALID), (dict(K=ODD), bkv.ERR_INVALID),
     (dict(V=None), bkv.ERR_INVALID), (dict(V=ODD), bkv.ERR_INVALID),
     (dict(out=None), bkv.ERR_INVALID), (dict(out=ODD), bkv.ERR_INVALID),
+    (dict(out=P), bkv.ERR_INVALID),                  # over the queries
+    (dict(out=ctypes.c_void_p((1 << 20) + 4096)), bkv.ERR_INVALID),
     (dict(scale=-1.0), bkv.ERR_INVALID), (dict(scale=float("inf")), bkv.ERR_INVALID),
     (dict(scale=float("nan")), bkv.ERR_INVALID),
     (dict(ws=None), bkv.ERR_WORKSPACE), (dict(ws=ODD), bkv.ERR_WORKSPACE), (dict(n=16), bkv.ERR_WORKSPACE),

@@ -119,6 +119,29 @@ def test_nan_masses_keep_an_exact_count(fill):
 
 
 @pytest.mark.parametrize("fill", [False, True])
+@pytest.mark.parametrize("Hkv", [2, 300])
+def test_a_workspace_stamped_for_other_dims_moves_nothing(fill, Hkv):
+    d = bkv.dims(B=1, Hq=Hkv, Hkv=Hkv, D=64, N=700, W=8, C=0, budget=300, n_prefix=2)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    K, V = (torch.randn(1, Hkv, 700, 64, generator=g, device="cuda").bfloat16() for _ in "KV")
+    m = torch.rand(1, Hkv, 700, generator=g, device="cuda")
+    kept = torch.full((1, Hkv, 300), -1, dtype=torch.int32, device="cuda")
+    before = [t.clone() for t in (K, V, m, kept)]
+    ws = bkv.mass_workspace(d)
+    bkv.workspace_init(d.replace(budget=299), ws)
+    bkv.evict_mass(d, K, V, m, ws, kept=kept, fill=fill)
+    assert bkv.device_status(ws) == bkv.ERR_DEVICE
+    assert all(torch.equal(a, b) for a, b in zip((K, V, m, kept), before))
+    ws.zero_()  # never initialised
+    bkv.evict_mass(d, K, V, m, ws, kept=kept, fill=fill)
+    assert bkv.device_status(ws) == bkv.ERR_WORKSPACE
+    assert all(torch.equal(a, b) for a, b in zip((K, V, m, kept), before))
+    bkv.workspace_init(d, ws)
+    bkv.evict_mass(d, K, V, m, ws, kept=kept, fill=fill)
+    assert bkv.device_status(ws) == bkv.OK and not torch.equal(kept, before[3])
+
+
+@pytest.mark.parametrize("fill", [False, True])
 def test_captured_graph(fill):
     d = bkv.dims(B=2, Hq=4, Hkv=2, D=128, N=900, W=8, C=0, budget=600, n_prefix=2)
     g = torch.Generator(device="cuda").manual_seed(3)
