@@ -48,30 +48,62 @@ struct Bf16 {
     // Which 16-byte chunk of a row (in elements) load kk of lane group g takes.
     __device__ static int chunk(int kk, int g) { return 32 * kk + 8 * g; }
 
-    __device__ static void load_k(K& k, const elem* base, int k0, int last, int lane) {
-        const int m = lane & 15, g = lane >> 4;
-        dev::static_for<kTiles>([&](auto ac) {
-            constexpr int a = decltype(ac)::value;
-            const elem* p = base + (long long)min(k0 + 16 * a + m, last) * D;
-            dev::static_for<kKK>([&](auto c) {
-                constexpr int kk = decltype(c)::value;
-                k.v[a][kk] = __builtin_nontemporal_load(reinterpret_cast<const dev::u32x4*>(p + chunk(kk, g)));
-            });
-        });
+    // Keys [k0, k0 + kKeys) of the head at base; rows past `last` repeat it, so
+    // that nothing behind a sequence is read.  A whole group's addresses are a
+    // uniform base and lane offsets that never change (off): no arithmetic.
+    // Keys and values are read once, and go past the caches.
+    struct Off { unsigned k, v; };
+    __device__ static Off offsets(int lane) {
+        const unsigned m = lane & 15, g = lane >> 4;
+        return {m * D + 8 * g, 4 * g * D + kDV * m};
     }
-    __device__ static void load_v(V& v, const elem* base, int k0, int last, int lane) {
-        const int m = lane & 15, g = lane >> 4;
-        dev::static_for<8>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            const elem* p = base + (long long)min(k0 + 16 * (j / 4) + 4 * g + j % 4, last) * D + kDV * m;
-            if constexpr (kDV == 8) {
-                const dev::u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const dev::u32x4*>(p));
-                dev::static_for<4>([&](auto c) { v.v[j][decltype(c)::value] = x[decltype(c)::value]; });
-            } else {
-                const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-                dev::static_for<2>([&](auto c) { v.v[j][decltype(c)::value] = x[decltype(c)::value]; });
-            }
-        });
+    __device__ static void load_k(K& k, const elem* base, int k0, int last, Off off, int lane) {
+        if (k0 + kKeys - 1 <= last) {
+            const elem* p = base + (long long)k0 * D;
+            dev::static_for<kTiles>([&](auto ac) {
+                constexpr int a = decltype(ac)::value;
+                dev::static_for<kKK>([&](auto c) {
+                    constexpr int kk = decltype(c)::value;
+                    k.v[a][kk] = __builtin_nontemporal_load(
+                        reinterpret_cast<const dev::u32x4*>(p + 16 * a * D + 32 * kk + off.k));
+                });
+            });
+        } else {
+            const int m = lane & 15, g = lane >> 4;
+            dev::static_for<kTiles>([&](auto ac) {
+                constexpr int a = decltype(ac)::value;
+                const elem* p = base + (long long)min(k0 + 16 * a + m, last) * D;
+                dev::static_for<kKK>([&](auto c) {
+                    constexpr int kk = decltype(c)::value;
+                    k.v[a][kk] = *reinterpret_cast<const dev::u32x4*>(p + chunk(kk, g));
+                });
+            });
+        }
+    }
+    __device__ static void load_v(V& v, const elem* base, int k0, int last, Off off, int lane) {
+        if (k0 + kKeys - 1 <= last) {
+            const elem* p = base + (long long)k0 * D;
+            dev::static_for<8>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                take(v, decltype(jc){}, p + (16 * (j / 4) + j % 4) * D + off.v);
+            });
+        } else {
+            const int m = lane & 15, g = lane >> 4;
+            dev::static_for<8>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                take(v, decltype(jc){}, base + (long long)min(k0 + 16 * (j / 4) + 4 * g + j % 4, last) * D + kDV * m);
+            });
+        }
+    }
+    template <int J>
+    __device__ static void take(V& v, std::integral_constant<int, J>, const elem* p) {
+        if constexpr (kDV == 8) {
+            const dev::u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const dev::u32x4*>(p));
+            dev::static_for<4>([&](auto c) { v.v[J][decltype(c)::value] = x[decltype(c)::value]; });
+        } else {
+            const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+            dev::static_for<2>([&](auto c) { v.v[J][decltype(c)::value] = x[decltype(c)::value]; });
+        }
     }
     __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const Q& q) {
         dev::static_for<kTiles>([&](auto ac) {
@@ -133,24 +165,34 @@ struct F32 {
 
     __device__ static int chunk(int kk, int g) { return 16 * kk + 4 * g; }
 
-    __device__ static void load_k(K& k, const elem* base, int k0, int last, int lane) {
+    struct Off { unsigned k, v; };
+    __device__ static Off offsets(int lane) {
+        const unsigned m = lane & 15, g = lane >> 4;
+        return {m * D + 4 * g, 4 * g * D + kDV * m};
+    }
+    __device__ static void load_k(K& k, const elem* base, int k0, int last, Off off, int lane) {
         const int m = lane & 15, g = lane >> 4;
-        const elem* p = base + (long long)min(k0 + m, last) * D;
+        const elem* p = k0 + kKeys - 1 <= last ? base + (long long)k0 * D + off.k
+                                               : base + (long long)min(k0 + m, last) * D + 4 * g;
         dev::static_for<kKK>([&](auto c) {
             constexpr int kk = decltype(c)::value;
-            k.v[0][kk] = *reinterpret_cast<const f32x4*>(p + chunk(kk, g));
+            k.v[0][kk] = *reinterpret_cast<const f32x4*>(p + 16 * kk);
         });
     }
-    __device__ static void load_v(V& v, const elem* base, int k0, int last, int lane) {
-        const int m = lane & 15, g = lane >> 4;
-        dev::static_for<4>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            const elem* p = base + (long long)min(k0 + 4 * g + j, last) * D + kDV * m;
-            dev::static_for<kDV / 4>([&](auto c) {
-                constexpr int i = decltype(c)::value;
-                v.v[j][i] = *reinterpret_cast<const f32x4*>(p + 4 * i);
+    __device__ static void load_v(V& v, const elem* base, int k0, int last, Off off, int lane) {
+        if (k0 + kKeys - 1 <= last) {
+            const elem* p = base + (long long)k0 * D;
+            dev::static_for<kDV>([&](auto ic) {
+                constexpr int j = decltype(ic)::value / (kDV / 4), i = decltype(ic)::value % (kDV / 4);
+                v.v[j][i] = *reinterpret_cast<const f32x4*>(p + j * D + 4 * i + off.v);
             });
-        });
+        } else {
+            const int m = lane & 15, g = lane >> 4;
+            dev::static_for<kDV>([&](auto ic) {
+                constexpr int j = decltype(ic)::value / (kDV / 4), i = decltype(ic)::value % (kDV / 4);
+                v.v[j][i] = *reinterpret_cast<const f32x4*>(base + (long long)min(k0 + 4 * g + j, last) * D + kDV * m + 4 * i);
+            });
+        }
     }
     __device__ static void logits(f32x4 (&s)[1], const K& k, const Q& q) {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -243,7 +285,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     extern __shared__ __attribute__((aligned(16))) float dyn[];
     __shared__ float s_m[kWaves][16], s_z[kWaves][16], s_norm[kKeptRows];
     lds_float* const s_o = (lds_float*)dyn;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const bool own = (int)blockIdx.x >= a.items0;
     const Segment sg = own ? a.seg[1] : a.seg[0];
@@ -277,6 +319,8 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         most = max(most, dev::shfl_xor_i(most, x));
         least = min(least, dev::shfl_xor_i(least, x));
     }
+    most = __builtin_amdgcn_readfirstlane(most);  // (every lane has them)
+    least = __builtin_amdgcn_readfirstlane(least);
     const int k_lo = split * sg.chunk;
     // with the logits kept, keys that no row sees are written too (as -inf)
     const int keep = own ? a.keep : kKeepNone;
@@ -295,15 +339,16 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         const int last = k_hi - 1;  // rows past it repeat it: nothing behind a sequence is read
         typename E::K kr;
         typename E::V vr;
-        E::load_k(kr, K, k0, last, lane);
-        E::load_v(vr, V, k0, last, lane);
+        const typename E::Off off = E::offsets(lane);
+        E::load_k(kr, K, k0, last, off, lane);
+        E::load_v(vr, V, k0, last, off, lane);
         for (; k0 < k_hi; k0 += KG * kWaves) {
             f32x4 p[RT][NT];
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 E::logits(p[rt], kr, q[rt]);
             });
-            E::load_k(kr, K, k0 + KG * kWaves, last, lane);
+            E::load_k(kr, K, k0 + KG * kWaves, last, off, lane);
             const bool edge = k0 + KG > min(least, k_hi);
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
@@ -340,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                 });
             });
             E::template values<NR>(o, vr, p);
-            E::load_v(vr, V, k0 + KG * kWaves, last, lane);
+            E::load_v(vr, V, k0 + KG * kWaves, last, off, lane);
         }
     };
     if constexpr (RT == 2) {
@@ -566,7 +611,7 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(Args a, int nchunk) {
     if (k0 >= len) return;
     const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
     typename E::K kr;
-    E::load_k(kr, K, k0, len - 1, lane);
+    E::load_k(kr, K, k0, len - 1, E::offsets(lane), lane);
     float sum[NT * 4] = {};
     // the first query that sees key k0
     const int t0 = sg.causal ? max(0, k0 - (len - a.T)) : 0;
