@@ -55,7 +55,7 @@ struct Plan {
     int own_nrb, pre_nrb;
     int own_ns, own_chunk, pre_ns, pre_chunk;
     bool keep;                // the logits are kept for the mass
-    int parts;                // else: workgroups that share a block of keys (bf16)
+    int parts;                // else: workgroups that share a block of keys
     size_t part_o, part_ml, row_lse2, logits, parts_at, end;
 };
 Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap);
@@ -114,6 +114,61 @@ inline JoinGrid join_grid(const Args& a) {
     return g;
 }
 
+// Length of a unit's keys: lens may hold anything, the keys read stay in [0, n).
+__device__ __forceinline__ int unit_len(const Segment& sg, int unit, int Hkv) {
+    return sg.lens ? min(max(sg.lens[unit / Hkv], 0), sg.n) : sg.n;
+}
+
+// ---- rows of the weights' sums -------------------------------------------------------
+// The kernels that sum the weights of many rows take a unit's rows as they lie
+// (g T + t), `parts` workgroups to a block of kMassKeys keys, each a range of
+// rows.  Key j of a causal cache is seen by the queries t >= j - lead.
+constexpr int kMassKeys = 128;
+inline long long mass_blocks(const Args& a, int parts) {
+    return (long long)a.seg[1].units * parts * ((a.seg[1].n + kMassKeys - 1) / kMassKeys);
+}
+
+struct MassRows {
+    int T, causal, lead, t0, full, end;  // t0: the first query that sees any key; full: from here on, all of them
+    int first, first_t;
+    __device__ __forceinline__ MassRows(const Args& a, int causal_, int len, int key0, int keys, int part, int parts) {
+        T = a.T;
+        causal = causal_;
+        lead = len - a.T;
+        t0 = causal ? max(0, key0 - lead) : 0;
+        full = causal ? key0 + keys - 1 - lead : 0;
+        end = (int)((long long)a.R * (part + 1) / parts);
+        first = (int)((long long)a.R * part / parts);
+        first_t = first % T;
+        if (t0 >= T)
+            first = end;  // no query sees these keys
+        else
+            skip(first, first_t);
+    }
+    // To the head's first query that sees anything.
+    __device__ __forceinline__ void skip(int& r, int& t) const {
+        if (t < t0) {
+            r += t0 - t;
+            t = t0;
+        }
+    }
+    __device__ __forceinline__ void advance(int& r, int& t, int rows) const {
+        r += rows;
+        t += rows;
+        if (t >= T) {
+            t %= T;
+            skip(r, t);
+        }
+    }
+    // Whether some of the rows [r, r + rows), the first one query t, may not see
+    // some key, or belong to a later head.
+    __device__ __forceinline__ bool edge(int r, int t, int rows) const {
+        return t < full || (causal && t + rows > T && r + T - t < end);
+    }
+    // Keys that row r sees.
+    __device__ __forceinline__ int seen(int r) const { return lead + 1 + r % T; }
+};
+
 // Lowest running maximum: finite, so that exp2(-inf - m) is 0 and not NaN in
 // a row that has seen nothing yet.
 constexpr float kLowest = -3.402823466e38f;
@@ -126,9 +181,10 @@ hipError_t launch_attend_stream(const attend::Args& a, int dtype, bool wide, hip
 hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, hipStream_t s);
 // Joins the partials and, where the logits were kept, adds the weights to the mass.
 hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s);
-// Adds the weights to the mass from the queries and keys: fp32 caches, and bf16 ones (part: parts * units * n floats
-// where parts > 1).
-hipError_t launch_attend_mass(const attend::Args& a, hipStream_t s);
+// The weights' sums from the queries and keys, of fp32 and of bf16 caches: added to the mass, or, where parts > 1, to
+// part [parts][units][n], whose sums the third adds.
+hipError_t launch_attend_mass(const attend::Args& a, float* part, int parts, hipStream_t s);
 hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s);
+hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s);
 
 }  // namespace bkv

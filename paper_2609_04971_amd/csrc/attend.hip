@@ -222,11 +222,6 @@ struct F32 {
     __device__ static void store(elem* p, float x) { *p = x; }
 };
 
-// Length of a unit's keys: lens may hold anything, the keys read stay in [0, n).
-__device__ __forceinline__ int unit_len(const Segment& sg, int unit, int Hkv) {
-    return sg.lens ? min(max(sg.lens[unit / Hkv], 0), sg.n) : sg.n;
-}
-
 // Keys that query t sees: the T queries are the newest tokens of the cache.
 __device__ __forceinline__ int seen_by(const Args& a, const Segment& sg, int len, int t) {
     return sg.causal ? max(0, len - a.T + 1 + t) : len;
@@ -597,46 +592,89 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Args a, int njoin, int n
 }
 
 // The same from the queries and keys, for more rows than the logits are kept
-// of: a workgroup holds 4 x 16 NT keys, streams the unit's rows past them, and
-// every lane sums its keys' weights over its rows (lane % 16) in order.
-template <class E, int D>
-__global__ __launch_bounds__(kThreads) void mass_kernel(Args a, int nchunk) {
-    constexpr int NT = E::kTiles, KG = E::kKeys;
+// of (fp32): a wave holds 32 keys, two key tiles and so two independent chains
+// of products, and streams a part of the unit's rows past them, 16 at a time as
+// they lie in memory (head by head), the next ones under way.  A lane sums its
+// eight keys' weights over its rows (lane % 16) in order.
+template <int D>
+__global__ __launch_bounds__(kThreads) void mass_kernel(Args a, float* part, int parts) {
+    using E = F32<D>;
+    constexpr int kTiles = 2, kRows = 16;
     const Segment& sg = a.seg[1];
-    const int unit = blockIdx.x / nchunk, ch = blockIdx.x % nchunk;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int item = blockIdx.x;
+    const int unit = item % sg.units;
+    item /= sg.units;
+    const int pt = item % parts, k0 = item / parts * kMassKeys;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int len = unit_len(sg, unit, a.Hkv);
-    const int k0 = (ch * kWaves + wave) * KG;
-    if (k0 >= len) return;
-    const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
-    typename E::K kr;
-    E::load_k(kr, K, k0, len - 1, E::offsets(lane), lane);
-    float sum[NT * 4] = {};
-    // the first query that sees key k0
-    const int t0 = sg.causal ? max(0, k0 - (len - a.T)) : 0;
-    for (int r0 = min(t0, a.T) * a.G / 16 * 16; r0 < a.R; r0 += 16) {
-        const int rr = r0 + col;
-        const bool valid = rr < a.R;
-        const Row x = decode_row(a, unit, 1, valid ? rr : 0);
-        const typename E::Q q = load_q<E, D>(a, x, valid, g);
-        const float norm = valid ? a.row_lse2[x.lse] : INFINITY;
-        const int lim = valid ? seen_by(a, sg, len, x.t) : 0;
-        f32x4 s[NT];
-        E::logits(s, kr, q);
-        dev::static_for<NT * 4>([&](auto ic) {
+    const int key0 = k0 + 16 * kTiles * wave;
+    if (key0 >= len) return;
+    const float* K = static_cast<const float*>(sg.K) + (long long)unit * sg.cap * D;
+    typename E::K kr[kTiles];
+    dev::static_for<kTiles>([&](auto ac) {
+        constexpr int t = decltype(ac)::value;
+        E::load_k(kr[t], K, key0 + 16 * t, len - 1, E::offsets(lane), lane);
+    });
+    f32x4 sum[kTiles] = {};
+    const MassRows rows(a, sg.causal, len, key0, 16 * kTiles, pt, parts);
+    int r = rows.first, t = rows.first_t;
+    const float* q = static_cast<const float*>(a.q) + (long long)unit * a.R * D;
+    const float* norms = a.row_lse2 + (long long)unit * a.R;
+    auto load = [&](typename E::Q& y, float& norm) __attribute__((always_inline)) {
+        const bool valid = r + col < rows.end;
+        const float* p = q + (long long)(r + col) * D + 4 * g;
+        dev::static_for<E::kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            y.v[kk] = valid ? *reinterpret_cast<const f32x4*>(p + 16 * kk) : f32x4{0.f, 0.f, 0.f, 0.f};
+        });
+        norm = valid ? norms[r + col] : INFINITY;
+    };
+    typename E::Q y;
+    float norm;
+    load(y, norm);
+    while (r < rows.end) {
+        const int row = r, query = t;
+        f32x4 s[kTiles];
+        dev::static_for<kTiles>([&](auto ac) {
+            f32x4 one[1];
+            E::logits(one, kr[decltype(ac)::value], y);
+            s[decltype(ac)::value] = one[0];
+        });
+        const float n = norm;
+        rows.advance(r, t, kRows);
+        load(y, norm);
+        const bool edge = rows.edge(row, query, kRows);
+        const int lim = edge ? rows.seen(row + col) - key0 - 4 * g : 0;  // from the lane's first key
+        dev::static_for<kTiles * 4>([&](auto ic) {
             constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-            const float e = exp2_hw(s[ti][i] * a.scale2 - norm);
-            sum[decltype(ic)::value] += k0 + 16 * ti + 4 * g + i < lim ? e : 0.f;
+            const float w = exp2_hw(s[ti][i] * a.scale2 - n);
+            sum[ti][i] += !edge || 16 * ti + i < lim ? w : 0.f;
         });
     }
-    float* mass = a.mass + (long long)unit * a.N_cap;
-    dev::static_for<NT * 4>([&](auto ic) {
+    dev::static_for<kTiles * 4>([&](auto ic) {
         constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-        const float v = dev::row16_sum(sum[decltype(ic)::value]);
-        const int j = k0 + 16 * ti + 4 * g + i;
-        if (col == 0 && j < len) mass[j] += v;
+        const float v = dev::row16_sum(sum[ti][i]);
+        const int j = key0 + 16 * ti + 4 * g + i;
+        if (col != 0 || j >= len) return;
+        if (parts > 1)
+            part[((long long)pt * sg.units + unit) * sg.n + j] = v;
+        else
+            a.mass[(long long)unit * a.N_cap + j] += v;
     });
+}
+
+// The parts' sums, in order.
+__global__ __launch_bounds__(kThreads) void add_parts_kernel(Args a, const float* part, int parts) {
+    const Segment& sg = a.seg[1];
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x, n = (long long)sg.units * sg.n;
+    if (i >= n) return;
+    const int unit = (int)(i / sg.n), j = (int)(i - (long long)unit * sg.n);
+    if (j >= unit_len(sg, unit, a.Hkv)) return;
+    float v = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) v += part[p * n + i];
+    a.mass[(long long)unit * a.N_cap + j] += v;
 }
 
 template <class E, int D>
@@ -662,15 +700,6 @@ hipError_t join(const Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <class E, int D>
-hipError_t masses(const Args& a, hipStream_t s) {
-    const Segment& sg = a.seg[1];
-    if (sg.n == 0 || sg.units == 0) return hipSuccess;
-    const int nchunk = (sg.n + kWaves * E::kKeys - 1) / (kWaves * E::kKeys);
-    hipLaunchKernelGGL((mass_kernel<E, D>), dim3((unsigned)(sg.units * nchunk)), dim3(kThreads), 0, s, a, nchunk);
-    return hipGetLastError();
-}
-
 }  // namespace
 }  // namespace attend
 
@@ -684,9 +713,21 @@ hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s) {
     if (dtype == BKV_BF16) return a.D == 128 ? join<Bf16<128>, 128>(a, s) : join<Bf16<64>, 64>(a, s);
     return a.D == 128 ? join<F32<128>, 128>(a, s) : join<F32<64>, 64>(a, s);
 }
-hipError_t launch_attend_mass(const attend::Args& a, hipStream_t s) {
+hipError_t launch_attend_mass(const attend::Args& a, float* part, int parts, hipStream_t s) {
     using namespace attend;
-    return a.D == 128 ? masses<F32<128>, 128>(a, s) : masses<F32<64>, 64>(a, s);
+    const dim3 grid((unsigned)mass_blocks(a, parts)), block(kThreads);
+    if (a.D == 128)
+        hipLaunchKernelGGL(mass_kernel<128>, grid, block, 0, s, a, part, parts);
+    else
+        hipLaunchKernelGGL(mass_kernel<64>, grid, block, 0, s, a, part, parts);
+    return hipGetLastError();
+}
+hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s) {
+    using namespace attend;
+    const long long n = (long long)a.seg[1].units * a.seg[1].n;
+    hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a, part,
+                       parts);
+    return hipGetLastError();
 }
 
 }  // namespace bkv

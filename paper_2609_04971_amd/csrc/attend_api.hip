@@ -22,8 +22,7 @@ constexpr long long kWhole = 128 << 10;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
 constexpr int kMassItems = 2048;    // workgroups that sum the weights of many rows, at least
-constexpr int kMassRows = 1024;     // rows that make such a workgroup worth its own sums
-constexpr int kMassBlock = 128;     // keys of one
+constexpr int kMassRows = 256;      // rows that make such a workgroup worth its own sums
 
 // Splits of n keys at most, of `base` items each: what a workspace has room for.
 int most_splits(long long base, int n) {
@@ -123,17 +122,17 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
     p.logits = off;
     if (p.keep) off = up(off + sizeof(float) * (size_t)rows * up((size_t)d.N_cap, 32), kAlign);
-    // the heads of a group share a block of keys where there are few blocks and
-    // each head has many rows; parts > 1 means fewer blocks than kMassItems, so
-    // their sums never pass kMassItems blocks and as many again
+    // a unit's rows are dealt out where there are few blocks of keys; parts > 1
+    // means fewer blocks than kMassItems, so their sums never pass kMassItems
+    // blocks and as many again
     p.parts = 1;
     p.parts_at = off;
-    const long long most = G < R / kMassRows ? G : R / kMassRows;
-    if (mass && p.own_tile && most > 1) {
-        const long long blocks = (long long)d.B * d.Hkv * ((d.N + kMassBlock - 1) / kMassBlock);
+    const long long most = R / kMassRows;
+    if (mass && !p.keep && most > 1) {
+        const long long blocks = (long long)d.B * d.Hkv * ((d.N + kMassKeys - 1) / kMassKeys);
         const long long want = blocks > 0 ? (kMassItems + blocks - 1) / blocks : 1;
         p.parts = (int)(want < most ? want : most);
-        off = up(off + sizeof(float) * 2 * kMassItems * kMassBlock, kAlign);
+        off = up(off + sizeof(float) * 2 * kMassItems * kMassKeys, kAlign);
     }
     p.end = off;
     return p;
@@ -226,9 +225,7 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     }
     const long long items0 = (long long)pre.units * pre.nrb * pre.ns;
     const long long items1 = (long long)own.units * own.nrb * own.ns;
-    // every launch's grid; the weights' sums take at most one block per 64 tokens
-    if (items0 + items1 > kMaxBlocks || (mass && !p.keep && own.units * ((d->N + 63LL) / 64) > kMaxBlocks))
-        return BKV_ERR_SHAPE;
+    if (items0 + items1 > kMaxBlocks || (mass && !p.keep && mass_blocks(a, p.parts) > kMaxBlocks)) return BKV_ERR_SHAPE;
     a.ns = p.own_ns + p.pre_ns;
     a.part_o = reinterpret_cast<float*>(w + p.part_o);
     a.part_ml = reinterpret_cast<float*>(w + p.part_ml);
@@ -248,11 +245,11 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
         if (launch_attend_stream(a, d->dtype, p.wide, stream) != hipSuccess) return BKV_ERR_HIP;
     }
     if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
-    if (mass && !p.keep) {
-        const hipError_t e = p.own_tile
-                                 ? launch_attend_tile_mass(a, reinterpret_cast<float*>(w + p.parts_at), p.parts, stream)
-                                 : launch_attend_mass(a, stream);
-        if (e != hipSuccess) return BKV_ERR_HIP;
+    if (mass && !p.keep && d->N > 0) {
+        float* part = reinterpret_cast<float*>(w + p.parts_at);
+        if ((p.own_tile ? launch_attend_tile_mass : launch_attend_mass)(a, part, p.parts, stream) != hipSuccess)
+            return BKV_ERR_HIP;
+        if (p.parts > 1 && launch_attend_add_parts(a, part, p.parts, stream) != hipSuccess) return BKV_ERR_HIP;
     }
     return BKV_OK;
 }

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
         rb = item % sg.nrb;
         split = item / sg.nrb;
     }
-    const int len = sg.lens ? min(max(sg.lens[unit / a.Hkv], 0), sg.n) : sg.n;
+    const int len = unit_len(sg, unit, a.Hkv);
     const int r0 = rb * kWaves * kWaveRows;
     const int rr = r0 + wave * kWaveRows + (lane & 31);
     const bool valid = rr < sg.rows;
@@ -339,11 +339,6 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
 // holds 128 keys in operand registers and walks the unit's rows in tiles of 64
 // through LDS: waves 0, 1 take a tile's first 32 rows and 2, 3 the others,
 // each for 64 of the keys.  A lane sums its 32 keys over its rows in order.
-// Rows are taken as they lie, head by head (g T + t).  With few units the
-// heads of the group go to `parts` workgroups, whose sums are added by
-// add_parts_kernel.
-constexpr int kMassKeys = 128;
-
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* part, int parts) {
     using T = Tile<D>;
@@ -357,7 +352,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* p
     const int unit = item % sg.units;
     item /= sg.units;
     const int pt = item % parts, k0 = item / parts * kMassKeys;
-    const int len = sg.lens ? min(max(sg.lens[unit / a.Hkv], 0), sg.n) : sg.n;
+    const int len = unit_len(sg, unit, a.Hkv);
     if (k0 >= len) return;
     const int key0 = k0 + 64 * kw;
     const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
@@ -371,27 +366,15 @@ __global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* p
         });
     });
     f32x16 sum[2] = {};
-    // heads [g0, g1) of the group, rows [r, r1) of them; key j is seen by the
-    // queries t >= j - lead
-    const int g0 = pt * a.G / parts, g1 = (pt + 1) * a.G / parts, r1 = g1 * a.T;
-    const int lead = len - a.T;
-    const int t0 = sg.causal ? max(0, k0 - lead) : 0;
-    const int full = sg.causal ? k0 + kMassKeys - 1 - lead : 0;  // queries from here on see all the keys
-    int r = g0 * a.T, t = 0;  // the tile's first row and its query
-    auto skip = [&]() {       // to the head's first query that sees anything
-        if (t < t0) {
-            r += t0 - t;
-            t = t0;
-        }
-    };
-    if (t0 >= a.T) r = r1;
-    skip();
+    const MassRows rows(a, sg.causal, len, k0, kMassKeys, pt, parts);
+    int r = rows.first, t = rows.first_t;  // the tile's first row and its query
     auto load = [&](int row, uint16_t* stage) {
-        if (row < r1)
-            load_tile<D>(static_cast<const uint16_t*>(a.q) + ((long long)unit * a.R + row) * D, r1 - row, stage, wave, lane);
+        if (row < rows.end)
+            load_tile<D>(static_cast<const uint16_t*>(a.q) + ((long long)unit * a.R + row) * D, rows.end - row, stage, wave,
+                         lane);
     };
     const float* norms = a.row_lse2 + (long long)unit * a.R + 32 * rw + (lane & 31);
-    auto norm_at = [&](int row) { return row + 32 * rw + (lane & 31) < r1 ? norms[row] : INFINITY; };
+    auto norm_at = [&](int row) { return row + 32 * rw + (lane & 31) < rows.end ? norms[row] : INFINITY; };
     int at[T::KK];
     row_offsets<D>(at, lane);
     auto step = [&](int row, int query, const uint16_t* stage, float norm) {
@@ -402,10 +385,8 @@ __global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* p
             s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[0][kk], q, s[0], 0, 0, 0);
             s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[1][kk], q, s[1], 0, 0, 0);
         });
-        if (query < full || (sg.causal && query + kKeys > a.T && row + a.T - query < r1)) {
-            // some row may not see some key, or a later head's first queries are in the tile
-            const int qt = (row + 32 * rw + (lane & 31)) % a.T;
-            const int lim = lead + 1 + qt - key0 - 4 * h;  // keys that the row sees, from the lane's first
+        if (rows.edge(row, query, kKeys)) {
+            const int lim = rows.seen(row + 32 * rw + (lane & 31)) - key0 - 4 * h;  // from the lane's first key
             dev::static_for<32>([&](auto ic) {
                 constexpr int kt = decltype(ic)::value / 16, e = decltype(ic)::value % 16;
                 const float w = exp2_hw(__builtin_fmaf(s[kt][e], a.scale2, -norm));
@@ -418,27 +399,18 @@ __global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* p
             });
         }
     };
-    // the tile after (r, t)
-    auto advance = [&]() {
-        r += kKeys;
-        t += kKeys;
-        if (t >= a.T) {
-            t %= a.T;
-            skip();
-        }
-    };
     load(r, q_a);
     float norm = norm_at(r);
-    while (r < r1) {
+    while (r < rows.end) {
         const int ra = r, ta = t;
-        advance();
+        rows.advance(r, t, kKeys);
         turn();
         load(r, q_b);
         const float next = norm_at(r);
         step(ra, ta, q_a, norm);
-        if (r >= r1) break;
+        if (r >= rows.end) break;
         const int rb = r, tb = t;
-        advance();
+        rows.advance(r, t, kKeys);
         turn();
         load(r, q_a);
         norm = norm_at(r);
@@ -466,18 +438,6 @@ __global__ __launch_bounds__(kThreads, 2) void tile_mass_kernel(Args a, float* p
         });
 }
 
-__global__ __launch_bounds__(kThreads) void add_parts_kernel(Args a, const float* part, int parts) {
-    const Segment& sg = a.seg[1];
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x, n = (long long)sg.units * sg.n;
-    if (i >= n) return;
-    const int unit = (int)(i / sg.n), j = (int)(i - (long long)unit * sg.n);
-    const int len = sg.lens ? min(max(sg.lens[unit / a.Hkv], 0), sg.n) : sg.n;
-    if (j >= len) return;
-    float v = 0.f;
-    for (int p = 0; p < parts; ++p) v += part[p * n + i];
-    a.mass[(long long)unit * a.N_cap + j] += v;
-}
-
 }  // namespace
 }  // namespace attend
 
@@ -494,17 +454,11 @@ hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, 
 
 hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s) {
     using namespace attend;
-    const Segment& sg = a.seg[1];
-    if (sg.n == 0 || sg.units == 0) return hipSuccess;
-    const dim3 grid((unsigned)((long long)sg.units * parts * ((sg.n + kMassKeys - 1) / kMassKeys))), block(kThreads);
+    const dim3 grid((unsigned)mass_blocks(a, parts)), block(kThreads);
     if (a.D == 128)
         hipLaunchKernelGGL(tile_mass_kernel<128>, grid, block, 0, s, a, part, parts);
     else
         hipLaunchKernelGGL(tile_mass_kernel<64>, grid, block, 0, s, a, part, parts);
-    if (parts > 1) {
-        const long long n = (long long)sg.units * sg.n;
-        hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), block, 0, s, a, part, parts);
-    }
     return hipGetLastError();
 }
 
