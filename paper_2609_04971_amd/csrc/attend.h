@@ -119,6 +119,18 @@ __device__ __forceinline__ int unit_len(const Segment& sg, int unit, int Hkv) {
     return sg.lens ? min(max(sg.lens[unit / Hkv], 0), sg.n) : sg.n;
 }
 
+// What a row's sums come to.  z is 0 for a row that saw nothing and at least 1
+// otherwise (or NaN, where it saw one, and then so are its results).
+struct RowEnd {
+    float inv;   // 1 / z, or 0
+    float lse;   // natural log of the normaliser, -inf for nothing
+    float lse2;  // its log2 for the weights, +inf for nothing: they come out 0
+};
+__device__ __forceinline__ RowEnd row_end(float m, float z) {
+    const float l2 = m + log2f(z);
+    return z == 0.f ? RowEnd{0.f, -INFINITY, INFINITY} : RowEnd{1.f / z, l2 * 0.6931471805599453f, l2};
+}
+
 // ---- rows of the weights' sums -------------------------------------------------------
 // The kernels that sum the weights of many rows take a unit's rows as they lie
 // (g T + t), `parts` workgroups to a block of kMassKeys keys, each a range of

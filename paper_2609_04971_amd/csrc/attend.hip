@@ -435,14 +435,13 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     a.part_ml[2 * at + 1] = Z;
                 }
             } else {
-                const float inv = Z > 0.f ? 1.f / Z : 0.f;
+                const RowEnd end = row_end(M, Z);
                 typename E::elem* out = static_cast<typename E::elem*>(a.out) + x.q + 4 * v;
-                dev::static_for<4>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * inv); });
+                dev::static_for<4>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * end.inv); });
                 if (v == 0) {
-                    const float l2 = M + log2f(Z);
-                    if (a.lse) a.lse[x.lse] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-                    if (a.mass) a.row_lse2[x.lse] = Z > 0.f ? l2 : INFINITY;
-                    if (keep) s_norm[16 * rt + r] = Z > 0.f ? l2 : INFINITY;
+                    if (a.lse) a.lse[x.lse] = end.lse;
+                    if (a.mass) a.row_lse2[x.lse] = end.lse2;
+                    if (keep) s_norm[16 * rt + r] = end.lse2;
                 }
             }
         }
@@ -486,13 +485,13 @@ __device__ __forceinline__ void join_rows(const Args& a) {
     const float* po = a.part_o + gr * a.ns * D + PER * lane;
     float M = kLowest;
     for (int s = lane; s < a.ns; s += 64)
-        if (ml[2 * s + 1] > 0.f) M = fmaxf(M, ml[2 * s]);
+        if (ml[2 * s + 1] != 0.f) M = fmaxf(M, ml[2 * s]);
     for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, dev::shfl_xor_f(M, x));
     float Z = 0.f, sum[PER] = {};
     for (int s0 = 0; s0 < a.ns; s0 += 64) {
         const int s = s0 + lane;
         float f = 0.f;
-        if (s < a.ns && ml[2 * s + 1] > 0.f) {
+        if (s < a.ns && ml[2 * s + 1] != 0.f) {
             f = exp2_hw(ml[2 * s] - M);
             Z += f * ml[2 * s + 1];
         }
@@ -510,7 +509,7 @@ __device__ __forceinline__ void join_rows(const Args& a) {
                 const float w = i < n ? __shfl(f, i, 64) : 0.f;
                 dev::static_for<PER>([&](auto c) {
                     constexpr int e = decltype(c)::value;
-                    sum[e] += w > 0.f ? w * v[k][e] : 0.f;
+                    sum[e] += w != 0.f ? w * v[k][e] : 0.f;
                 });
             });
         }
@@ -528,13 +527,12 @@ __device__ __forceinline__ void join_rows(const Args& a) {
     const long long bh = gr / a.R;
     const int t = r / a.G, g = r - t * a.G;
     const long long at = (bh * a.G + g) * a.T + t;  // (b Hkv + h) G + g is the query head
-    const float inv = Z > 0.f ? 1.f / Z : 0.f;
+    const RowEnd end = row_end(M, Z);
     typename E::elem* out = static_cast<typename E::elem*>(a.out) + at * D + PER * lane;
-    dev::static_for<PER>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * inv); });
+    dev::static_for<PER>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * end.inv); });
     if (lane == 0) {
-        const float l2 = M + log2f(Z);
-        if (a.lse) a.lse[at] = Z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-        if (a.mass && !a.logits) a.row_lse2[at] = Z > 0.f ? l2 : INFINITY;
+        if (a.lse) a.lse[at] = end.lse;
+        if (a.mass && !a.logits) a.row_lse2[at] = end.lse2;
     }
 }
 
@@ -551,7 +549,7 @@ __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
         if (r < a.R) {
             const float* ml = a.part_ml + 2 * (row0 + r) * a.ns;
             for (int s = threadIdx.x / kKeptRows; s < a.ns; s += kThreads / kKeptRows) {
-                if (!(ml[2 * s + 1] > 0.f)) continue;
+                if (ml[2 * s + 1] == 0.f) continue;
                 const float mn = fmaxf(m, ml[2 * s]);
                 z = z * exp2_hw(m - mn) + ml[2 * s + 1] * exp2_hw(ml[2 * s] - mn);
                 m = mn;
@@ -565,7 +563,7 @@ __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
             z = 0.f;
             for (int w = 0; w < kThreads / kKeptRows; ++w)
                 z += s_z[threadIdx.x + w * kKeptRows] * exp2_hw(s_m[threadIdx.x + w * kKeptRows] - m);
-            s_norm[threadIdx.x] = z > 0.f ? m + log2f(z) : INFINITY;
+            s_norm[threadIdx.x] = row_end(m, z).lse2;
         }
     } else if ((int)threadIdx.x < a.R) {
         const int t = threadIdx.x / a.G, g = threadIdx.x - t * a.G;

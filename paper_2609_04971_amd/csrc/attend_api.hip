@@ -45,7 +45,7 @@ int most_splits(long long base, int n) {
 // only in part: 2 or 3 of them at once take 1.7 or 2.4 times as long as one.
 // us, splits as taken (*) and others, streaming: 8 heads x 65536 tokens 32* 49,
 // 64 50, 96 53, 256 57; 192 x 4000 1 78, 3 78, 4* 67, 6 76; 160 x 6000 (ragged)
-// 2 105, 3 79, 7 74, 8* 74; 296 x 2000 fp32 1 143, 2 127, 4 119; tile: 112
+// 2 105, 3* 79, 7 74; 296 x 2000 fp32 1 143, 2 127, 3* 123, 4 119; tile: 112
 // blocks of 500 x 7 queries against 24000 3 146, 4 119, 5 135, 9* 113, 19 138.
 int best_splits(bool tile, long long base, int n, long long rows, int D) {
     constexpr float kRound[4] = {0.f, 1.f, 1.7f, 2.4f};
@@ -211,7 +211,7 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     own.ns = p.own_ns;
     own.chunk = p.own_chunk;
     own.split0 = p.pre_ns;
-    own.causal = flags & BKV_ATTEND_CAUSAL;
+    own.causal = (flags & BKV_ATTEND_CAUSAL) && T > 1;  // one query sees all of its cache either way
     Segment& pre = a.seg[0];
     pre.nrb = pre.ns = pre.seqs = 1;
     if (groups > 0 && P > 0) {

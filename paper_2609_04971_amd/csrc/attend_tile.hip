@@ -317,19 +317,18 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
             a.part_ml[2 * at + 1] = z;
         }
     } else {
-        const float inv = z > 0.f ? 1.f / z : 0.f;
+        const RowEnd end = row_end(st.m, z);
         uint16_t* out = static_cast<uint16_t*>(a.out) + x.q;
         dev::static_for<T::DT * 4>([&](auto ic) {
             constexpr int dt = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
             typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
             *reinterpret_cast<bf16x4_t*>(out + 32 * dt + 8 * i + 4 * h) =
-                bf16x4_t{(__bf16)(st.o[dt][4 * i] * inv), (__bf16)(st.o[dt][4 * i + 1] * inv),
-                         (__bf16)(st.o[dt][4 * i + 2] * inv), (__bf16)(st.o[dt][4 * i + 3] * inv)};
+                bf16x4_t{(__bf16)(st.o[dt][4 * i] * end.inv), (__bf16)(st.o[dt][4 * i + 1] * end.inv),
+                         (__bf16)(st.o[dt][4 * i + 2] * end.inv), (__bf16)(st.o[dt][4 * i + 3] * end.inv)};
         });
         if (h == 0) {
-            const float l2 = st.m + log2f(z);
-            if (a.lse) a.lse[x.lse] = z > 0.f ? l2 * 0.6931471805599453f : -INFINITY;
-            if (a.mass) a.row_lse2[x.lse] = z > 0.f ? l2 : INFINITY;
+            if (a.lse) a.lse[x.lse] = end.lse;
+            if (a.mass) a.row_lse2[x.lse] = end.lse2;
         }
     }
 }

@@ -94,6 +94,30 @@ def test_ragged_lengths_and_rows_that_see_nothing(dtype, T):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_kept_logits_that_do_not_fit_lds(dtype):
+    run_case(2, 2, 8, 128, 4, 20000, 20000, dtype, causal=True)   # several splits
+    run_case(64, 4, 8, 128, 2, 1500, 1503, dtype)                 # one
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,N", [(1, 300), (1, 3000), (40, 300), (40, 3000)])
+def test_a_nan_stays_in_its_head(dtype, T, N):
+    d = bkv.dims(B=2, Hq=8, Hkv=2, D=128, N=N, W=0, C=0, budget=1, dtype=dtype)
+    x = make(2, 2, 4, 128, T, N, N, dtype, seed=3)
+    want = call(d, x, T)
+    for k in "KV":
+        y = dict(x, **{k: x[k].clone()})
+        y[k][1, 0, N // 2, 5] = float("nan")
+        out, lse, mass = call(d, y, T)
+        for got, ref, axis in ((out, want[0], 4), (lse, want[1], 4), (mass, want[2], 1)):
+            assert torch.equal(got[0], ref[0]) and torch.equal(got[1, axis:], ref[1, axis:])  # the other heads
+        if k == "K":
+            assert out[1, :4].isnan().all() and lse[1, :4].isnan().all() and mass[1, 0].isnan().all()
+        else:
+            assert out[1, :4, :, 5].isnan().all() and torch.equal(lse, want[1]) and torch.equal(mass, want[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_no_tokens_at_all(dtype):
     run_case(2, 2, 2, 128, 3, 0, 8, dtype)
     d = bkv.dims(B=2, Hq=4, Hkv=2, D=128, N=0, N_cap=8, W=0, C=0, budget=1, dtype=dtype)
