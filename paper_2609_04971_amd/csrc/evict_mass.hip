@@ -272,7 +272,7 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
             const int count = s_count;
             take -= s_above;
             lo += (unsigned)s_bin << shift;
-            hi = min(hi, lo + ((1u << shift) - 1u));
+            hi = lo + min(hi - lo, (1u << shift) - 1u);  // the last bin's end may lie past 2^32
             if (take == count) {  // the whole bin
                 theta = lo;
                 last = 0x7fffffff;

@@ -119,6 +119,34 @@ def test_nan_masses_keep_an_exact_count(fill):
 
 
 @pytest.mark.parametrize("fill", [False, True])
+@pytest.mark.parametrize("kind", ["any bits", "top NaNs", "bottom NaNs"])
+@pytest.mark.parametrize("Hkv,N", [(2, 800), (2, 9000), (300, 800)])
+def test_masses_of_any_bits(kind, Hkv, N, fill):
+    """NaNs rank by their bits: the keys' range reaches both ends of 32 bits."""
+    g = torch.Generator().manual_seed(N)
+    b = torch.randint(-2 ** 31, 2 ** 31, (1, Hkv, N), generator=g, dtype=torch.int64)
+    if kind != "any bits":
+        b = 1 + torch.randint(0, 2 ** 30, (1, Hkv, N), generator=g)   # positive, none of them 0
+        b[..., ::3] = 0x7fffffff - torch.randint(0, 2 ** 18, b[..., ::3].shape, generator=g)
+        b[..., 1], b[..., 6] = 1, 0x7fffffff
+        if kind == "bottom NaNs":
+            b -= 2 ** 31
+    u = b & 0xffffffff
+    key = torch.where(u >= 2 ** 31, 0xffffffff - u, u + 2 ** 31)
+    key[u == 2 ** 31] = 2 ** 31                                      # -0
+    budget = {"any bits": N // 3, "top NaNs": N // 6, "bottom NaNs": N - N // 6}[kind]
+    d = bkv.dims(B=1, Hq=Hkv, Hkv=Hkv, D=64, N=N, W=8, C=0, budget=budget, n_prefix=2)
+    key[..., :2] = key[..., N - 8:] = 2 ** 40
+    want = key[0].sort(dim=-1, descending=True, stable=True).indices[:, :budget].sort(dim=-1).values
+    K = torch.arange(N).float().view(1, 1, N, 1).expand(1, Hkv, N, 64).bfloat16().cuda()
+    kept = torch.full((1, Hkv, budget), -1, dtype=torch.int32, device="cuda")
+    ws = bkv.mass_workspace(d)
+    bkv.evict_mass(d, K, K.clone(), b.to(torch.int32).view(torch.float32).cuda(), ws, kept=kept, fill=fill)
+    assert bkv.device_status(ws) == bkv.OK
+    assert torch.equal(host(kept)[0].long().sort(dim=-1).values, want)
+
+
+@pytest.mark.parametrize("fill", [False, True])
 @pytest.mark.parametrize("Hkv", [2, 300])
 def test_a_workspace_stamped_for_other_dims_moves_nothing(fill, Hkv):
     d = bkv.dims(B=1, Hq=Hkv, Hkv=Hkv, D=64, N=700, W=8, C=0, budget=300, n_prefix=2)
