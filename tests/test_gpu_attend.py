@@ -180,6 +180,45 @@ def test_one_workspace_serves_every_length_and_calls_repeat():
         assert torch.equal(again[0], out) and torch.equal(again[1], lse) and torch.equal(again[2], mass)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kw", [
+    dict(B=3, Hkv=1, G=71, D=64, T=1, N=1234, cap=1234, lens=[1234, 0, 777]),    # one kv-head for all
+    dict(B=2, Hkv=1, G=128, D=128, T=1, N=2500, cap=2501),
+    dict(B=1, Hkv=1, G=33, D=128, T=1, N=4000, cap=4000),
+    dict(B=3, Hkv=2, G=6, D=64, T=33, N=2100, cap=2100, causal=True, lens=[2100, 40, 1999]),
+    dict(B=2, Hkv=3, G=1, D=128, T=200, N=3100, cap=3100, causal=True, lens=[199, 3100]),
+    dict(B=9, Hkv=5, G=3, D=64, T=11, N=333, cap=340, causal=True, lens=[333, 1, 0, 64, 65, 128, 5, 11, 12]),
+    dict(B=16, Hkv=8, G=8, D=128, T=4, N=900, cap=901, causal=True),
+    dict(B=300, Hkv=2, G=2, D=64, T=1, N=65, cap=66),
+    dict(B=4, Hkv=2, G=5, D=64, T=3, N=700, cap=700, causal=True, lens=[700, 2, 350, 0], groups=2, P=5000, P_cap=5003, p_lens=[4999, 64]),
+    dict(B=8, Hkv=1, G=8, D=64, T=9, N=300, cap=300, causal=True, lens=[300, 9, 8, 299, 0, 1, 64, 65], groups=1, P=3001, P_cap=3001),
+])
+def test_head_layouts_and_ragged_batches(dtype, kw):
+    run_case(dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 60])
+def test_two_streams_at_once(dtype, T):
+    """Calls in flight together, each with a workspace of its own."""
+    N = 6000
+    d = bkv.dims(B=1, Hq=8, Hkv=2, D=128, N=N, W=0, C=0, budget=1, dtype=dtype)
+    x = [make(1, 2, 4, 128, T, N, N, dtype, seed=s) for s in (1, 2)]
+    want = [call(d, y, T, causal=True) for y in x]
+    ws = [bkv.attend_workspace(d, T, True) for _ in x]
+    outs = [[(torch.empty_like(y["q"]), torch.empty_like(want[0][1]), y["mass"].clone()) for _ in range(10)] for y in x]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in x]
+    for i in range(10):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                out, lse, mass = outs[k][i]
+                bkv.attend(d, x[k]["q"], x[k]["K"], x[k]["V"], out, ws[k], lse=lse, mass=mass, causal=True)
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(a, b) for got in outs[k] for a, b in zip(got, want[k]))
+
+
 @pytest.mark.parametrize("T,groups", [(1, 0), (40, 0), (1, 2)])
 def test_side_stream_and_captured_graph(T, groups):
     B, Hkv, G, D, N = 4, 2, 4, 128, 600

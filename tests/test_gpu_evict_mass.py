@@ -190,6 +190,25 @@ def test_captured_graph(fill):
             assert torch.equal(a, b), f"replay {i}"
 
 
+@pytest.mark.parametrize("fill", [False, True])
+def test_two_streams_at_once(fill):
+    d = bkv.dims(B=1, Hq=2, Hkv=2, D=128, N=5000, W=8, C=0, budget=3000, n_prefix=2)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = [[torch.randn(1, 2, 5000, 128, generator=g, device="cuda").bfloat16() for _ in "KV"]
+         + [torch.rand(1, 2, 5000, generator=g, device="cuda"), torch.empty(1, 2, 3000, dtype=torch.int32, device="cuda")]
+         for _ in range(16)]
+    want = [[t.clone() for t in y] for y in x]
+    for K, V, m, kept in want:
+        bkv.evict_mass(d, K, V, m, bkv.mass_workspace(d), kept=kept, fill=fill)
+    ws, streams = [bkv.mass_workspace(d) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i, (K, V, m, kept) in enumerate(x):
+        with torch.cuda.stream(streams[i % 2]):
+            bkv.evict_mass(d, K, V, m, ws[i % 2], kept=kept, fill=fill)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for got, ref in zip(x, want) for a, b in zip(got, ref))
+
+
 @pytest.mark.parametrize("compaction", ["order", "fill"])
 def test_attention_and_eviction_together(compaction):
     """Two layers of two sequences decode past their budget twice: the weights
