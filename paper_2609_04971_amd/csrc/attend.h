@@ -55,7 +55,8 @@ struct Plan {
     int own_nrb, pre_nrb;
     int own_ns, own_chunk, pre_ns, pre_chunk;
     bool keep;                // the logits are kept for the mass
-    int parts;                // else: workgroups that share a block of keys
+    int mass_ns, mass_chunk;  // else, of rows that fit registers (mass_ns > 0): splits of the keys
+    int parts;                // or: workgroups that share a block of keys
     size_t part_o, part_ml, row_lse2, logits, parts_at, end;
 };
 Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap);
@@ -136,6 +137,7 @@ __device__ __forceinline__ RowEnd row_end(float m, float z) {
 // (g T + t), `parts` workgroups to a block of kMassKeys keys, each a range of
 // rows.  Key j of a causal cache is seen by the queries t >= j - lead.
 constexpr int kMassKeys = 128;
+constexpr int kRegRows = 96;  // rows of a bf16 cache that workgroups hold in registers instead (128 of D 128 do not fit)
 inline long long mass_blocks(const Args& a, int parts) {
     return (long long)a.seg[1].units * parts * ((a.seg[1].n + kMassKeys - 1) / kMassKeys);
 }
@@ -193,7 +195,9 @@ hipError_t launch_attend_stream(const attend::Args& a, int dtype, bool wide, hip
 hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, hipStream_t s);
 // Joins the partials and, where the logits were kept, adds the weights to the mass.
 hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s);
-// The weights' sums from the queries and keys, of fp32 and of bf16 caches: added to the mass, or, where parts > 1, to
+// The weights' sums from the queries and keys, added to the mass: of at most kRegRows rows of a bf16 cache.
+hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipStream_t s);
+// And of more, of fp32 and of bf16 caches: added to the mass, or, where parts > 1, to
 // part [parts][units][n], whose sums the third adds.
 hipError_t launch_attend_mass(const attend::Args& a, float* part, int parts, hipStream_t s);
 hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s);

@@ -662,6 +662,110 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(Args a, float* part, int
     });
 }
 
+// The same of a bf16 cache, for rows that fit registers: the unit's rows stay
+// there and the keys are streamed past them, groups of 32 a wave in turn and
+// the next group under way, so that the keys are read once at the rate of
+// memory.  S = Q K^T, the transpose of the above: a lane's logits are of one
+// key (lane % 16 of a tile) and rows 4 (lane / 16) + i, and a key's sum is the
+// lane's own but for one add over the four lane groups.  Bound by the keys'
+// reads and the chain of a wave: 54 heads of 48110 tokens and 56 rows 134 us
+// (5.0 TB/s; blocks of keys in registers and the rows past them 593), 1504
+// heads of 560 and 40 rows 50 (4.3 TB/s; 210).
+template <int D, int RT>
+__global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk) {
+    using E = Bf16<D>;
+    __shared__ __attribute__((aligned(16))) float s_norm[16 * RT];
+    __shared__ __attribute__((aligned(16))) int s_lim[16 * RT];  // keys that the row sees
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const Segment& sg = a.seg[1];
+    const int unit = blockIdx.x % sg.units, split = blockIdx.x / sg.units;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    const int len = unit_len(sg, unit, a.Hkv);
+    const int k_lo = split * chunk, k_hi = min(k_lo + chunk, len);
+    if (k_lo >= k_hi) return;
+    const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
+    float* mass = a.mass + (long long)unit * a.N_cap;
+    const typename E::Off off = E::offsets(lane);
+    struct Group {
+        typename E::K k;
+        float old;  // the masses of the group's keys, in the first 32 lanes
+    };
+    auto load = [&](Group& x, int k0) __attribute__((always_inline)) {
+        if (k0 < k_hi) {
+            E::load_k(x.k, K, k0, len - 1, off, lane);
+            x.old = mass[min(k0 + (lane & 31), k_hi - 1)];
+        }
+    };
+    Group one, two;
+    load(one, k_lo + E::kKeys * wave);
+    const long long row0 = (long long)unit * a.R;
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + row0 * D + 8 * g;
+    typename E::Q y[RT];
+    dev::static_for<RT>([&](auto rc) {
+        constexpr int rt = decltype(rc)::value;
+        const int r = 16 * rt + col;
+        dev::static_for<E::kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            y[rt].v[kk] = r < a.R ? *reinterpret_cast<const dev::u32x4*>(q + (long long)r * D + 32 * kk) : dev::u32x4{};
+        });
+    });
+    if ((int)threadIdx.x < 16 * RT) {
+        const int r = threadIdx.x;
+        s_norm[r] = r < a.R ? a.row_lse2[row0 + r] : INFINITY;
+        s_lim[r] = sg.causal ? len - a.T + 1 + r % a.T : len;
+    }
+    __syncthreads();
+    const int all = sg.causal ? len - a.T + 1 : len;  // keys that every row sees
+    auto step = [&](const Group& x, int k0) __attribute__((always_inline)) {
+        f32x4 sum[E::kTiles] = {};
+        const bool edge = k0 + E::kKeys > all;
+        asm volatile("" ::: "memory");  // or every row's normaliser would be kept in a register
+        dev::static_for<RT>([&](auto rc) {
+            constexpr int rt = decltype(rc)::value;
+            const f32x4 n = *reinterpret_cast<const f32x4*>(s_norm + 16 * rt + 4 * g);
+            f32x4 s[E::kTiles] = {};
+            dev::static_for<E::kKK * E::kTiles>([&](auto c) {
+                constexpr int kk = decltype(c)::value / E::kTiles, t = decltype(c)::value % E::kTiles;
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, y[rt].v[kk]),
+                                                               __builtin_bit_cast(bf16x8_t, x.k.v[t][kk]), s[t], 0, 0, 0);
+            });
+            dev::static_for<E::kTiles>([&](auto tc) {
+                constexpr int t = decltype(tc)::value;
+                dev::static_for<4>([&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    s[t][i] = exp2_hw(__builtin_fmaf(s[t][i], a.scale2, -n[i]));
+                });
+            });
+            if (edge) {
+                const i32x4 lim = *reinterpret_cast<const i32x4*>(s_lim + 16 * rt + 4 * g);
+                dev::static_for<E::kTiles * 4>([&](auto ic) {
+                    constexpr int t = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                    if (k0 + 16 * t + col >= lim[i]) s[t][i] = 0.f;
+                });
+            }
+            dev::static_for<E::kTiles>([&](auto tc) { sum[decltype(tc)::value] += s[decltype(tc)::value]; });
+            if (rt % 2) __builtin_amdgcn_sched_barrier(0);
+        });
+        float v[E::kTiles];
+        dev::static_for<E::kTiles>([&](auto tc) {
+            constexpr int t = decltype(tc)::value;
+            v[t] = (sum[t][0] + sum[t][1]) + (sum[t][2] + sum[t][3]);
+            v[t] += dev::shfl_xor_f(v[t], 16);
+            v[t] += dev::shfl_xor_f(v[t], 32);
+        });
+        if (lane < E::kKeys && k0 + lane < k_hi) mass[k0 + lane] = x.old + (g == 0 ? v[0] : v[1]);
+    };
+    constexpr int kStep = E::kKeys * kWaves;
+    for (int k0 = k_lo + E::kKeys * wave; k0 < k_hi; k0 += 2 * kStep) {
+        load(two, k0 + kStep);
+        step(one, k0);
+        if (k0 + kStep >= k_hi) break;
+        load(one, k0 + 2 * kStep);
+        step(two, k0 + kStep);
+    }
+}
+
 // The parts' sums, in order.
 __global__ __launch_bounds__(kThreads) void add_parts_kernel(Args a, const float* part, int parts) {
     const Segment& sg = a.seg[1];
@@ -718,6 +822,22 @@ hipError_t launch_attend_mass(const attend::Args& a, float* part, int parts, hip
         hipLaunchKernelGGL(mass_kernel<128>, grid, block, 0, s, a, part, parts);
     else
         hipLaunchKernelGGL(mass_kernel<64>, grid, block, 0, s, a, part, parts);
+    return hipGetLastError();
+}
+hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipStream_t s) {
+    using namespace attend;
+    const dim3 grid((unsigned)(a.seg[1].units * ns)), block(kThreads);
+    if (a.R <= 64) {
+        if (a.D == 128)
+            hipLaunchKernelGGL((row_mass_kernel<128, 4>), grid, block, 0, s, a, chunk);
+        else
+            hipLaunchKernelGGL((row_mass_kernel<64, 4>), grid, block, 0, s, a, chunk);
+    } else {
+        if (a.D == 128)
+            hipLaunchKernelGGL((row_mass_kernel<128, 6>), grid, block, 0, s, a, chunk);
+        else
+            hipLaunchKernelGGL((row_mass_kernel<64, 6>), grid, block, 0, s, a, chunk);
+    }
     return hipGetLastError();
 }
 hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s) {

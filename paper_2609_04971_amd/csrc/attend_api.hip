@@ -118,6 +118,8 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     cut(d.N, own_ns, &p.own_ns, &p.own_chunk);
     if (groups > 0 && P > 0) cut(P, pre_ns, &p.pre_ns, &p.pre_chunk);
     p.keep = mass && R <= kFewRows;
+    if (mass && !p.keep && tiles && R <= kRegRows)
+        cut(d.N, best_splits(false, (long long)d.B * d.Hkv, d.N, 0, d.D), &p.mass_ns, &p.mass_chunk);
     size_t off = 0;
     p.part_o = off;
     if (ns_cap > 1) off = up(off + sizeof(float) * (size_t)rows * ns_cap * d.D, kAlign);
@@ -249,7 +251,9 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
         if (launch_attend_stream(a, d->dtype, p.wide, stream) != hipSuccess) return BKV_ERR_HIP;
     }
     if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
-    if (mass && !p.keep && d->N > 0) {
+    if (p.mass_ns > 0 && d->N > 0) {
+        if (launch_attend_row_mass(a, p.mass_ns, p.mass_chunk, stream) != hipSuccess) return BKV_ERR_HIP;
+    } else if (mass && !p.keep && d->N > 0) {
         float* part = reinterpret_cast<float*>(w + p.parts_at);
         if ((p.own_tile ? launch_attend_tile_mass : launch_attend_mass)(a, part, p.parts, stream) != hipSuccess)
             return BKV_ERR_HIP;

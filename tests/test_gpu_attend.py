@@ -197,6 +197,13 @@ def test_head_layouts_and_ragged_batches(dtype, kw):
     run_case(dtype=dtype, **kw)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,T", [(1, 33), (8, 5), (8, 8), (5, 13), (1, 65), (12, 8), (1, 96), (1, 97)])
+def test_weights_of_rows_about_the_registers(G, T, D):
+    run_case(3, 2, G, D, T, 1100, 1103, "bf16", causal=True, lens=[1100, T - 2, 1025])
+    run_case(2, 1, G, D, T, 130, 130, "bf16", lens=[33, 130])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("T", [1, 60])
 def test_two_streams_at_once(dtype, T):
