@@ -96,18 +96,18 @@ inline size_t stream_lds(const Args& a) {
 // 32 bits.
 constexpr long long kMaxBlocks = 0xffffffffLL / 256;
 
-// Blocks of the launches below.
+// Blocks of the join's launch.
+constexpr int kFewSplits = 11;  // a row to some lanes, else to a workgroup
 struct JoinGrid {
-    int wpr;  // waves per row
+    bool few;
     int njoin, nchunk;
     long long blocks;
 };
 inline JoinGrid join_grid(const Args& a) {
-    // a wave per row, or four where there are so many splits that one would walk them for long
-    constexpr int kManySplits = 12, kWaves = 4, kTokens = 1024;
+    constexpr int kThreads = 256, kTokens = 1024;
     JoinGrid g;
-    g.wpr = a.ns >= kManySplits ? kWaves : 1;
-    const int rpb = kWaves / g.wpr;
+    g.few = a.ns <= kFewSplits;
+    const int rpb = g.few ? kThreads / (a.D / 4) : 1;
     g.njoin = a.ns > 1 ? (int)(((long long)a.rows + rpb - 1) / rpb) : 0;
     // (one split with its logits in LDS has added its weights itself)
     g.nchunk = a.keep && (a.ns > 1 || a.keep == kKeepStore) ? (a.seg[1].n + kTokens - 1) / kTokens : 0;

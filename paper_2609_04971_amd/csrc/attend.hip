@@ -149,7 +149,10 @@ struct Bf16 {
             });
         });
     }
-    __device__ static void store(elem* p, float x) { *p = dev::f32_to_bf16_rne(x); }
+    __device__ static void store4(elem* p, f32x4 x) {
+        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4_t*>(p) = bf16x4_t{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+    }
 };
 
 template <int D>
@@ -219,7 +222,7 @@ struct F32 {
             });
         });
     }
-    __device__ static void store(elem* p, float x) { *p = x; }
+    __device__ static void store4(elem* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 };
 
 // Keys that query t sees: the T queries are the newest tokens of the cache.
@@ -436,8 +439,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                 }
             } else {
                 const RowEnd end = row_end(M, Z);
-                typename E::elem* out = static_cast<typename E::elem*>(a.out) + x.q + 4 * v;
-                dev::static_for<4>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * end.inv); });
+                E::store4(static_cast<typename E::elem*>(a.out) + x.q + 4 * v, sum * end.inv);
                 if (v == 0) {
                     if (a.lse) a.lse[x.lse] = end.lse;
                     if (a.mass) a.row_lse2[x.lse] = end.lse2;
@@ -464,25 +466,78 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
 }
 
 // ---- joining the partials, and the weights of kept logits --------------------------
-// One launch.  The first blocks join: WPR waves per row take the row's splits
-// in turn, the weights exp2(m_s - M) in their lanes, eight splits' sums
-// requested at a time.  A split that saw nothing has z = 0 and weight 0; its
-// sums are never used.
+// One launch.  The first blocks join: the weights exp2(m_s - M) of a row's
+// splits in lanes, their sums requested several splits at a time.  A split
+// that saw nothing has z = 0 and weight 0; its sums are never used.  Bound by
+// the partials' way through memory where there are many rows, which a row to
+// D / 4 lanes takes at 3.8 TB/s (44520 rows of D 64 in two splits: 7.6 us, a
+// wave a row 21.8).  Many splits come with few rows: four waves a row take
+// them in turn.
 // The other blocks add the kept logits' weights to the masses, four tokens a
 // thread, rows in order, so that no sum depends on the launch:
 //   mass_j += sum over the unit's rows of exp2(l2_rj - lse2_r).
 // They take the rows' normalisers from the partials themselves.
-template <class E, int D, int WPR>
-__device__ __forceinline__ void join_rows(const Args& a) {
-    constexpr int PER = D / 64, RPB = kWaves / WPR;
-    __shared__ float s_sum[WPR > 1 ? kWaves : 1][D];
+
+// A row's results, coordinates [c, c + 4) of them; row gr of the partials.
+template <class E, int D>
+__device__ __forceinline__ void finish_row(const Args& a, long long gr, int c, f32x4 sum, float M, float Z) {
+    const int r = (int)(gr % a.R);
+    const long long bh = gr / a.R;
+    const int t = r / a.G, g = r - t * a.G;
+    const long long at = (bh * a.G + g) * a.T + t;  // (b Hkv + h) G + g is the query head
+    const RowEnd end = row_end(M, Z);
+    E::store4(static_cast<typename E::elem*>(a.out) + at * D + c, sum * end.inv);
+    if (c == 0) {
+        if (a.lse) a.lse[at] = end.lse;
+        if (a.mass && !a.logits) a.row_lse2[at] = end.lse2;
+    }
+}
+
+// Up to kFewSplits splits: a row to D / 4 lanes.
+template <class E, int D>
+__device__ __forceinline__ void join_few(const Args& a) {
+    constexpr int LPR = D / 4, AHEAD = 4;
+    static_assert(kFewSplits <= LPR, "a lane for every split");
+    const int sub = threadIdx.x % LPR, ns = a.ns;
+    const long long row = (long long)blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+    if (row >= a.rows) return;  // all lanes of a row at once
+    const float* po = a.part_o + row * ns * D + 4 * sub;
+    f32x4 v[AHEAD];
+    auto load = [&](int s0) {
+        dev::static_for<AHEAD>([&](auto kc) {
+            constexpr int k = decltype(kc)::value;
+            v[k] = *reinterpret_cast<const f32x4*>(po + (long long)min(s0 + k, ns - 1) * D);
+        });
+    };
+    const float* ml = a.part_ml + 2 * (row * ns + min(sub, ns - 1));
+    const float m = ml[0], z = sub < ns ? ml[1] : 0.f;
+    load(0);
+    float M = z != 0.f ? m : kLowest;
+    for (int x = 1; x < LPR; x <<= 1) M = fmaxf(M, dev::shfl_xor_f(M, x));
+    const float f = z != 0.f ? exp2_hw(m - M) : 0.f;
+    float Z = f * z;
+    for (int x = 1; x < LPR; x <<= 1) Z += dev::shfl_xor_f(Z, x);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < ns; s0 += AHEAD) {
+        dev::static_for<AHEAD>([&](auto kc) {
+            constexpr int k = decltype(kc)::value;
+            const float w = s0 + k < ns ? __shfl(f, s0 + k, LPR) : 0.f;
+            dev::static_for<4>([&](auto c) { sum[decltype(c)::value] += w != 0.f ? w * v[k][decltype(c)::value] : 0.f; });
+        });
+        if (s0 + AHEAD < ns) load(s0 + AHEAD);
+    }
+    finish_row<E, D>(a, row, 4 * sub, sum, M, Z);
+}
+
+// More: a row to a workgroup.
+template <class E, int D>
+__device__ __forceinline__ void join_many(const Args& a) {
+    constexpr int PER = D / 64;
+    __shared__ float s_sum[kWaves][D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int sub = wave % WPR;
-    const long long row = (long long)blockIdx.x * RPB + wave / WPR;
-    const bool valid = row < a.rows;
-    const long long gr = valid ? row : 0;
-    const float* ml = a.part_ml + 2 * gr * a.ns;
-    const float* po = a.part_o + gr * a.ns * D + PER * lane;
+    const long long row = blockIdx.x;
+    const float* ml = a.part_ml + 2 * row * a.ns;
+    const float* po = a.part_o + row * a.ns * D + PER * lane;
     float M = kLowest;
     for (int s = lane; s < a.ns; s += 64)
         if (ml[2 * s + 1] != 0.f) M = fmaxf(M, ml[2 * s]);
@@ -496,16 +551,16 @@ __device__ __forceinline__ void join_rows(const Args& a) {
             Z += f * ml[2 * s + 1];
         }
         const int n = min(64, a.ns - s0);
-        for (int i0 = sub; i0 < n; i0 += 8 * WPR) {
+        for (int i0 = wave; i0 < n; i0 += 8 * kWaves) {
             float v[8][PER];
             dev::static_for<8>([&](auto kc) {
                 constexpr int k = decltype(kc)::value;
-                const int i = s0 + min(i0 + k * WPR, n - 1);
+                const int i = s0 + min(i0 + k * kWaves, n - 1);
                 dev::static_for<PER>([&](auto c) { v[k][decltype(c)::value] = po[(long long)i * D + decltype(c)::value]; });
             });
             dev::static_for<8>([&](auto kc) {
                 constexpr int k = decltype(kc)::value;
-                const int i = i0 + k * WPR;
+                const int i = i0 + k * kWaves;
                 const float w = i < n ? __shfl(f, i, 64) : 0.f;
                 dev::static_for<PER>([&](auto c) {
                     constexpr int e = decltype(c)::value;
@@ -515,25 +570,14 @@ __device__ __forceinline__ void join_rows(const Args& a) {
         }
     }
     for (int x = 1; x < 64; x <<= 1) Z += dev::shfl_xor_f(Z, x);
-    if constexpr (WPR > 1) {
-        dev::static_for<PER>([&](auto c) { s_sum[wave][PER * lane + decltype(c)::value] = sum[decltype(c)::value]; });
-        __syncthreads();
-        if (sub != 0) return;
-        for (int w = 1; w < WPR; ++w)
-            dev::static_for<PER>([&](auto c) { sum[decltype(c)::value] += s_sum[wave + w][PER * lane + decltype(c)::value]; });
-    }
-    if (!valid) return;
-    const int r = (int)(gr % a.R);
-    const long long bh = gr / a.R;
-    const int t = r / a.G, g = r - t * a.G;
-    const long long at = (bh * a.G + g) * a.T + t;  // (b Hkv + h) G + g is the query head
-    const RowEnd end = row_end(M, Z);
-    typename E::elem* out = static_cast<typename E::elem*>(a.out) + at * D + PER * lane;
-    dev::static_for<PER>([&](auto c) { E::store(out + decltype(c)::value, sum[decltype(c)::value] * end.inv); });
-    if (lane == 0) {
-        if (a.lse) a.lse[at] = end.lse;
-        if (a.mass && !a.logits) a.row_lse2[at] = end.lse2;
-    }
+    dev::static_for<PER>([&](auto c) { s_sum[wave][PER * lane + decltype(c)::value] = sum[decltype(c)::value]; });
+    __syncthreads();
+    const int c = 4 * threadIdx.x;
+    if (c >= D) return;
+    f32x4 all = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < kWaves; ++w)
+        dev::static_for<4>([&](auto ic) { all[decltype(ic)::value] += s_sum[w][c + decltype(ic)::value]; });
+    finish_row<E, D>(a, row, c, all, M, Z);
 }
 
 __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
@@ -581,12 +625,14 @@ __device__ __forceinline__ void kept_mass(const Args& a, int item, int nchunk) {
     add_mass(a.mass + (long long)unit * a.N_cap + j, sum, len - j);
 }
 
-template <class E, int D, int WPR>
+template <class E, int D, bool FEW>
 __global__ __launch_bounds__(kThreads) void join_kernel(Args a, int njoin, int nchunk) {
-    if ((int)blockIdx.x < njoin)
-        join_rows<E, D, WPR>(a);
-    else
+    if ((int)blockIdx.x >= njoin)
         kept_mass(a, blockIdx.x - njoin, nchunk);
+    else if (FEW)
+        join_few<E, D>(a);
+    else
+        join_many<E, D>(a);
 }
 
 // The same from the queries and keys, for more rows than the logits are kept
@@ -795,10 +841,10 @@ hipError_t join(const Args& a, hipStream_t s) {
     const JoinGrid g = join_grid(a);
     if (g.blocks == 0) return hipSuccess;
     const dim3 grid((unsigned)g.blocks), block(kThreads);
-    if (g.wpr > 1)
-        hipLaunchKernelGGL((join_kernel<E, D, kWaves>), grid, block, 0, s, a, g.njoin, g.nchunk);
+    if (g.few)
+        hipLaunchKernelGGL((join_kernel<E, D, true>), grid, block, 0, s, a, g.njoin, g.nchunk);
     else
-        hipLaunchKernelGGL((join_kernel<E, D, 1>), grid, block, 0, s, a, g.njoin, g.nchunk);
+        hipLaunchKernelGGL((join_kernel<E, D, false>), grid, block, 0, s, a, g.njoin, g.nchunk);
     return hipGetLastError();
 }
 
