@@ -21,12 +21,12 @@ constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a 
 constexpr long long kWhole = 128 << 10;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
-// Workgroups that sum the weights of many rows: two to a compute unit, and
-// where the blocks of keys alone are as many, two to a block, since a causal
-// block's rows are fewer the later it is (us, a prompt of 8 x 4096 tokens of one
-// kv-head: 256 of them 128, 512 114, 1024 126, 2048 143; 2 x 4096 of eight, 512
-// blocks: one each 471, two 429).
-constexpr int kMassItems = 512;
+// Workgroups that sum the weights of many rows: where the blocks of keys alone
+// are fewer, a block's rows are dealt out, since three fit a compute unit and a
+// causal block's rows are fewer the later it is (us, a call of 4509 queries of
+// 7 heads, 2 kv-heads, 72 blocks, for 512 workgroups 159, 768 151, 1024 147,
+// 1536 152; 9 x 1510 of 4 heads, 108 blocks: 63, 61, 62, 68).
+constexpr int kMassItems = 1024;
 constexpr int kMassRows = 256;      // rows that make such a workgroup worth its own sums
 
 // Splits of n keys at most, of `base` items each: what a workspace has room for.
@@ -129,16 +129,15 @@ Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap
     if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
     p.logits = off;
     if (p.keep) off = up(off + sizeof(float) * (size_t)rows * up((size_t)d.N_cap, 32), kAlign);
-    // a unit's rows are dealt out where there are few blocks of keys: the sums
-    // of parts > 1 never pass 4 kMassItems blocks
+    // the sums of parts > 1 never pass 2 kMassItems blocks
     p.parts = 1;
     p.parts_at = off;
     const long long most = R / kMassRows;
     if (mass && !p.keep && most > 1) {
         const long long blocks = (long long)d.B * d.Hkv * ((d.N + kMassKeys - 1) / kMassKeys);
-        const long long want = blocks < 1 ? 1 : blocks < kMassItems ? (kMassItems + blocks - 1) / blocks : blocks < 2 * kMassItems ? 2 : 1;
+        const long long want = blocks < 1 ? 1 : (kMassItems + blocks - 1) / blocks;
         p.parts = (int)(want < most ? want : most);
-        off = up(off + sizeof(float) * 4 * kMassItems * kMassKeys, kAlign);
+        off = up(off + sizeof(float) * 2 * kMassItems * kMassKeys, kAlign);
     }
     p.end = off;
     return p;
