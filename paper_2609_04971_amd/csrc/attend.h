@@ -12,8 +12,8 @@ namespace attend {
 // prefix of a group of sequences.  A unit is one (sequence or group, kv-head)
 // pair.  Its rows are those of seqs consecutive sequences, R = G*T each, in
 // the order sequence, query, head of the kv-head's group; a unit's rows are
-// cut into nrb row blocks and its keys into ns splits of `chunk` keys, and
-// every (unit, row block, split) is one work item.
+// cut into nrb row blocks and its keys into ns splits, and every (unit, row
+// block, split) is one work item.
 struct Segment {
     const void* K;
     const void* V;
@@ -59,7 +59,7 @@ struct Plan {
     int parts;                // or: workgroups that share a block of keys
     size_t part_o, part_ml, row_lse2, logits, parts_at, end;
 };
-Plan make_plan(const bkv_dims& d, int T, bool mass, int groups, int P, int P_cap);
+Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int P, int P_cap);
 
 // A row of a segment's unit: which query it is.
 struct Row {
@@ -118,6 +118,19 @@ inline JoinGrid join_grid(const Args& a) {
 // Length of a unit's keys: lens may hold anything, the keys read stay in [0, n).
 __device__ __forceinline__ int unit_len(const Segment& sg, int unit, int Hkv) {
     return sg.lens ? min(max(sg.lens[unit / Hkv], 0), sg.n) : sg.n;
+}
+
+// The unit of an item of a launch whose units go round fastest.  Workgroups go
+// round the eight XCDs, so that each works on few units at a time and keeps
+// them in its L2; units of other lengths are dealt out anew every kTurns
+// rounds, or an XCD would have the long ones all along (us, every 1, 2, 4, 8
+// rounds and never: ragged prompts of 8 x 2048 queries of one kv-head 109 103
+// 99 98 124, 2 x 4096 of eight 170 169 193 202 224; 8 x 200 against 8000 of
+// four 257 284 286 286 292).
+constexpr int kTurns = 2;
+__device__ __forceinline__ int turning_unit(const Segment& sg, int item, int Hkv) {
+    const int unit = item % sg.units;
+    return sg.lens && sg.units > Hkv ? (unit + item / sg.units / kTurns) % sg.units : unit;
 }
 
 // What a row's sums come to.  z is 0 for a row that saw nothing and at least 1

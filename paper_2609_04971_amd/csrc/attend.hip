@@ -288,9 +288,20 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     const bool own = (int)blockIdx.x >= a.items0;
     const Segment sg = own ? a.seg[1] : a.seg[0];
     int item = blockIdx.x - (own ? a.items0 : 0);
-    const int rb = item % sg.nrb;
-    item /= sg.nrb;
-    const int split = item % sg.ns, unit = item / sg.ns;
+    // one row block: a unit's splits one after another.  Several (fp32 caches):
+    // units fastest, so that an XCD's L2 keeps to few of them, and causal row
+    // blocks longest first
+    int unit, split, rb = 0;
+    if (sg.nrb == 1) {
+        split = item % sg.ns;
+        unit = item / sg.ns;
+    } else {
+        unit = turning_unit(sg, item, a.Hkv);
+        item /= sg.units;
+        split = item % sg.ns;
+        rb = item / sg.ns;
+        if (sg.causal) rb = sg.nrb - 1 - rb;
+    }
     const int len = unit_len(sg, unit, a.Hkv);
     const int r0 = rb * 16 * RT;
 
@@ -646,7 +657,7 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(Args a, float* part, int
     constexpr int kTiles = 2, kRows = 16;
     const Segment& sg = a.seg[1];
     int item = blockIdx.x;
-    const int unit = item % sg.units;
+    const int unit = turning_unit(sg, item, a.Hkv);
     item /= sg.units;
     const int pt = item % parts, k0 = item / parts * kMassKeys;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -724,7 +735,7 @@ __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk
     __shared__ __attribute__((aligned(16))) int s_lim[16 * RT];  // keys that the row sees
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     const Segment& sg = a.seg[1];
-    const int unit = blockIdx.x % sg.units, split = blockIdx.x / sg.units;
+    const int unit = turning_unit(sg, blockIdx.x, a.Hkv), split = blockIdx.x / sg.units;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int len = unit_len(sg, unit, a.Hkv);

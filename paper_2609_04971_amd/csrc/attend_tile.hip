@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     // units fastest, so that an XCD's L2 keeps to few of them; causal row
     // blocks longest first
     int item = blockIdx.x;
-    const int unit = item % sg.units;
+    const int unit = turning_unit(sg, item, a.Hkv);
     item /= sg.units;
     int rb, split;
     if (sg.causal) {
@@ -278,7 +278,15 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
         const int last_row = min(r0 + kWaves * kWaveRows, sg.rows) - 1;  // the largest t of the row block (seqs is 1)
         all = max(0, len - a.T + 1 + last_row / a.G);
     }
-    const int k_lo = split * sg.chunk, k_hi = min(k_lo + sg.chunk, all);
+    // a prompt's row blocks cut their own keys and ragged sequences theirs, so that
+    // their splits are alike and none is empty; others share their tiles in L2
+    int chunk = sg.chunk;
+    const bool prompt = sg.causal && a.T > sg.n / 5;
+    if (prompt || sg.lens) {
+        const int each = ((prompt ? all : len) + sg.ns - 1) / sg.ns;
+        chunk = __builtin_amdgcn_readfirstlane(max(2 * kKeys, (each + kKeys - 1) / kKeys * kKeys));
+    }
+    const int k_lo = split * chunk, k_hi = min(k_lo + chunk, all);
     const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
     const uint16_t* V = static_cast<const uint16_t*>(sg.V) + (long long)unit * sg.cap * D;
     auto load = [&](int k0, uint16_t* ks, uint16_t* vs) {
@@ -357,7 +365,7 @@ __global__ __launch_bounds__(kThreads, 3) void tile_mass_kernel(Args a, float* p
     const int h = lane >> 5, kw = wave & 1, rw = wave >> 1;
     // chunks of keys slowest: the first ones are seen by the most rows
     int item = blockIdx.x;
-    const int unit = item % sg.units;
+    const int unit = turning_unit(sg, item, a.Hkv);
     item /= sg.units;
     const int pt = item % parts, k0 = item / parts * kMassKeys;
     const int len = unit_len(sg, unit, a.Hkv);
