@@ -501,6 +501,10 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
                                       : select<kShortThreads, kPerMax>(a, P, mode, stream);
     else if (a.N <= 8 * kLongThreads)
         e = select<kLongThreads, 8>(a, P, mode, stream);
+    else if (a.N <= 16 * kLongThreads)  // every pass takes all of its registers: 2 heads of 12932 37 us, with 32 46
+        e = select<kLongThreads, 16>(a, P, mode, stream);
+    else if (a.N <= 24 * kLongThreads)
+        e = select<kLongThreads, 24>(a, P, mode, stream);
     else if (a.N <= kPerMax * kLongThreads)
         e = select<kLongThreads, kPerMax>(a, P, mode, stream);
     else
