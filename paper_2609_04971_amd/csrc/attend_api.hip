@@ -21,6 +21,14 @@ constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a 
 constexpr long long kWhole = 128 << 10;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
+// Items of 32 rows and kMinChunk keys up to which a prefix of more rows is
+// streamed all the same, in one launch with the sequences' own caches: its keys
+// are read by every row block, but from L2, and the tiles' launch is spared (us
+// captured, tiles and so, items: 12 23.0 18.7, 96 23.7 21.5, 120 35.1 27.3, 440
+// 21.5 23.4, 496 35.2 27.8, 592 28.6 24.3, 928 32.3 29.0, 1088 52.7 68.6, 1344
+// 155 148, 3360 38 49, 4914 74 101).
+constexpr long long kFewItems = 4 * kCus;
+
 // Workgroups that sum the weights of many rows: where the blocks of keys alone
 // are fewer, a block's rows are dealt out, since three fit a compute unit and a
 // causal block's rows are fewer the later it is (us, a call of 4509 queries of
@@ -120,14 +128,16 @@ Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int
     const long long pre_rows = groups > 0 ? d.B / groups * R : 0;
     const bool tiles = d.dtype == BKV_BF16;
     p.own_tile = tiles && R > kFewRows;
-    p.pre_tile = tiles && pre_rows > kFewRows;
+    const long long pre_units = (long long)groups * d.Hkv, few_rb = (pre_rows + 31) / 32;
+    const long long few_items = pre_units * few_rb * ((P + kMinChunk - 1) / kMinChunk);
+    p.pre_tile = tiles && pre_rows > kFewRows && (p.own_tile || few_items > kFewItems);
     p.wide = (!p.own_tile && R > 16) || (!p.pre_tile && pre_rows > 16);
     const int own_rb = p.own_tile ? 128 : p.wide ? 32 : 16, pre_rb = p.pre_tile ? 128 : p.wide ? 32 : 16;
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
     const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
     int ns_cap = most_splits(own, d.N_cap), own_ns, pre_ns = 1;
-    if (groups > 0) ns_cap += most_splits(pre, P_cap);
+    if (groups > 0) ns_cap += most_splits(pre_units * ((pre_rows + 127) / 128), P_cap);  // as many as either kernel takes
     if (groups > 0 && P > 0 && !p.own_tile && !p.pre_tile) {  // one launch takes both
         const long long all = own * d.N + pre * P;
         own_ns = shared_splits(own, d.N, all);

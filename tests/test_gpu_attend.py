@@ -146,6 +146,9 @@ def test_large_logits_and_scale(dtype, T):
     dict(B=4, Hkv=2, G=4, D=128, T=2, N=0, cap=4, groups=4, P=0, P_cap=5),
     dict(B=3, Hkv=1, G=1, D=128, T=1, N=1, cap=1, groups=3, P=1, P_cap=1),
     dict(B=33, Hkv=1, G=8, D=64, T=3, N=9, cap=9, groups=1, P=260, P_cap=300, causal=True),
+    dict(B=64, Hkv=4, G=4, D=128, T=1, N=9, cap=9, groups=2, P=2000, P_cap=2048, p_lens=[2000, 129]),  # rows in blocks, streamed
+    dict(B=64, Hkv=4, G=4, D=128, T=1, N=9, cap=9, groups=2, P=4200, P_cap=4200, p_lens=[4200, 129]),  # and in tiles
+    dict(B=20, Hkv=2, G=5, D=64, T=4, N=300, cap=300, groups=4, P=100, P_cap=5000, causal=True, lens=[i * 16 for i in range(20)]),
 ])
 def test_shared(dtype, kw):
     run_case(dtype=dtype, **kw)
