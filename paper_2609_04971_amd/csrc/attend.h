@@ -210,10 +210,8 @@ hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, 
 hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s);
 // The weights' sums from the queries and keys, added to the mass: of at most kRegRows rows of a bf16 cache.
 hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipStream_t s);
-// And of more, of fp32 and of bf16 caches: added to the mass, or, where parts > 1, to
-// part [parts][units][n], whose sums the third adds.
-hipError_t launch_attend_mass(const attend::Args& a, float* part, int parts, hipStream_t s);
-hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s);
+// And of more rows, added to the mass, or, where parts > 1, to part [parts][units][n], whose sums the third adds.
+hipError_t launch_attend_tile_mass(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s);
 hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s);
 
 }  // namespace bkv

@@ -274,6 +274,11 @@ typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 // no key passes through LDS, a wave's next keys are requested before this
 // group's weights are computed and its next values after they are used, and
 // rows that share a kv-head share every load.
+// Measured, bf16 of D 128: 4608 units of 3584 tokens 1.31 ms (6.6 TB/s, where a
+// probe with these loads alone reaches 7.0), 8 units of 65536 in 32 splits 44 us
+// (6.1), 128 of 4224 in two 47 (6.0).  More rows (fp32 caches, prefixes of few
+// items) come in row blocks and are bound by the products: fp32, 2048 causal
+// queries of 32 heads 350 us (98 TFLOP/s of what is seen, products alone 154).
 template <class E, int D, int RT>
 __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     constexpr int KG = E::kKeys, NT = E::kTiles, DV = E::kDV;
@@ -646,83 +651,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Args a, int njoin, int n
         join_many<E, D>(a);
 }
 
-// The same from the queries and keys, for more rows than the logits are kept
-// of (fp32): a wave holds 32 keys, two key tiles and so two independent chains
-// of products, and streams a part of the unit's rows past them, 16 at a time as
-// they lie in memory (head by head), the next ones under way.  A lane sums its
-// eight keys' weights over its rows (lane % 16) in order.
-template <int D>
-__global__ __launch_bounds__(kThreads) void mass_kernel(Args a, float* part, int parts) {
-    using E = F32<D>;
-    constexpr int kTiles = 2, kRows = 16;
-    const Segment& sg = a.seg[1];
-    int item = blockIdx.x;
-    const int unit = turning_unit(sg, item, a.Hkv);
-    item /= sg.units;
-    const int pt = item % parts, k0 = item / parts * kMassKeys;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, g = lane >> 4;
-    const int len = unit_len(sg, unit, a.Hkv);
-    const int key0 = k0 + 16 * kTiles * wave;
-    if (key0 >= len) return;
-    const float* K = static_cast<const float*>(sg.K) + (long long)unit * sg.cap * D;
-    typename E::K kr[kTiles];
-    dev::static_for<kTiles>([&](auto ac) {
-        constexpr int t = decltype(ac)::value;
-        E::load_k(kr[t], K, key0 + 16 * t, len - 1, E::offsets(lane), lane);
-    });
-    f32x4 sum[kTiles] = {};
-    const MassRows rows(a, sg.causal, len, key0, 16 * kTiles, pt, parts);
-    int r = rows.first, t = rows.first_t;
-    const float* q = static_cast<const float*>(a.q) + (long long)unit * a.R * D;
-    const float* norms = a.row_lse2 + (long long)unit * a.R;
-    auto load = [&](typename E::Q& y, float& norm) __attribute__((always_inline)) {
-        const bool valid = r + col < rows.end;
-        const float* p = q + (long long)(r + col) * D + 4 * g;
-        dev::static_for<E::kKK>([&](auto c) {
-            constexpr int kk = decltype(c)::value;
-            y.v[kk] = valid ? *reinterpret_cast<const f32x4*>(p + 16 * kk) : f32x4{0.f, 0.f, 0.f, 0.f};
-        });
-        norm = valid ? norms[r + col] : INFINITY;
-    };
-    typename E::Q y;
-    float norm;
-    load(y, norm);
-    while (r < rows.end) {
-        const int row = r, query = t;
-        f32x4 s[kTiles];
-        dev::static_for<kTiles>([&](auto ac) {
-            f32x4 one[1];
-            E::logits(one, kr[decltype(ac)::value], y);
-            s[decltype(ac)::value] = one[0];
-        });
-        const float n = norm;
-        rows.advance(r, t, kRows);
-        load(y, norm);
-        const bool edge = rows.edge(row, query, kRows);
-        const int lim = edge ? rows.seen(row + col) - key0 - 4 * g : 0;  // from the lane's first key
-        dev::static_for<kTiles * 4>([&](auto ic) {
-            constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-            const float w = exp2_hw(s[ti][i] * a.scale2 - n);
-            sum[ti][i] += !edge || 16 * ti + i < lim ? w : 0.f;
-        });
-    }
-    dev::static_for<kTiles * 4>([&](auto ic) {
-        constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-        const float v = dev::row16_sum(sum[ti][i]);
-        const int j = key0 + 16 * ti + 4 * g + i;
-        if (col != 0 || j >= len) return;
-        if (parts > 1)
-            part[((long long)pt * sg.units + unit) * sg.n + j] = v;
-        else
-            a.mass[(long long)unit * a.N_cap + j] += v;
-    });
-}
-
-// The same of a bf16 cache, for rows that fit registers: the unit's rows stay
-// there and the keys are streamed past them, groups of 32 a wave in turn and
+// The same from the queries and keys, for more rows of a bf16 cache than the
+// logits are kept of, as long as they fit registers: the unit's rows stay there
+// and the keys are streamed past them, groups of 32 a wave in turn and
 // the next group under way, so that the keys are read once at the rate of
-// memory.  S = Q K^T, the transpose of the above: a lane's logits are of one
+// memory.  S = Q K^T, the transpose of the streaming kernel's: a lane's logits are of one
 // key (lane % 16 of a tile) and rows 4 (lane / 16) + i, and a key's sum is the
 // lane's own but for one add over the four lane groups.  Bound by the keys'
 // reads and the chain of a wave: 54 heads of 48110 tokens and 56 rows 134 us
@@ -871,15 +804,6 @@ hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s) {
     using namespace attend;
     if (dtype == BKV_BF16) return a.D == 128 ? join<Bf16<128>, 128>(a, s) : join<Bf16<64>, 64>(a, s);
     return a.D == 128 ? join<F32<128>, 128>(a, s) : join<F32<64>, 64>(a, s);
-}
-hipError_t launch_attend_mass(const attend::Args& a, float* part, int parts, hipStream_t s) {
-    using namespace attend;
-    const dim3 grid((unsigned)mass_blocks(a, parts)), block(kThreads);
-    if (a.D == 128)
-        hipLaunchKernelGGL(mass_kernel<128>, grid, block, 0, s, a, part, parts);
-    else
-        hipLaunchKernelGGL(mass_kernel<64>, grid, block, 0, s, a, part, parts);
-    return hipGetLastError();
 }
 hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipStream_t s) {
     using namespace attend;

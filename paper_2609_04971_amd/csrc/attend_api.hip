@@ -292,8 +292,7 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
         if (launch_attend_row_mass(a, p.mass_ns, p.mass_chunk, stream) != hipSuccess) return BKV_ERR_HIP;
     } else if (mass && !p.keep && d->N > 0) {
         float* part = reinterpret_cast<float*>(w + p.parts_at);
-        if ((p.own_tile ? launch_attend_tile_mass : launch_attend_mass)(a, part, p.parts, stream) != hipSuccess)
-            return BKV_ERR_HIP;
+        if (launch_attend_tile_mass(a, d->dtype, part, p.parts, stream) != hipSuccess) return BKV_ERR_HIP;
         if (p.parts > 1 && launch_attend_add_parts(a, part, p.parts, stream) != hipSuccess) return BKV_ERR_HIP;
     }
     return BKV_OK;

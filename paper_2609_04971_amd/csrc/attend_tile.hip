@@ -1,5 +1,6 @@
 // Attention of many query rows of a bf16 cache for gfx950 (prompts, chunks,
-// the samples of a shared prefix), and the sums of their weights.
+// the samples of a shared prefix), and the sums of their weights (of fp32
+// caches too).
 //
 // More rows than a few make the products the bound, so keys and values go
 // through LDS once for 128 rows: a workgroup's four waves own 32 rows each and
@@ -19,7 +20,7 @@
 // of four rows, V).  f takes the low bits of r to the chunk's high bits, so
 // that four rows put their four chunks into four different blocks of 64
 // bytes, and is a permutation over 16 rows (over the 8 pairs of rows that
-// share 256 bytes, D = 64).
+// share 256 bytes, bf16 of D = 64).
 #include "attend.h"
 
 namespace bkv {
@@ -34,8 +35,10 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
-constexpr int kKeys = 64;        // keys per tile
 constexpr int kWaveRows = 32;
+
+// Kinds of instructions for the scheduler.
+constexpr int kSchedMfma = 0x8, kSchedLds = 0x100;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -48,85 +51,154 @@ __device__ __forceinline__ void turn() {
 }
 
 // Position of chunk c of row r is c ^ swz(r).
-template <int D>
+template <class E>
 __device__ __forceinline__ int swz(int r) {
-    if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    if constexpr (E::CPR >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
     return ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
-template <int D>
-struct Tile {
-    static constexpr int CPR = D / 8;        // 16-byte chunks per row
-    static constexpr int RPI = 64 / CPR;     // rows per load instruction
-    static constexpr int NI = kKeys / RPI / kWaves;  // load instructions per wave and tile
-    static constexpr int KK = D / 16;        // contraction steps of the logits
-    static constexpr int DT = D / 32;        // 32-coordinate tiles of the outputs
-    static constexpr int ELEMS = kKeys * D;
-};
-
-// One tile of rows [0, rows) at base into LDS; rows past them become zero.
-template <int D>
-__device__ __forceinline__ void load_tile(const uint16_t* base, int rows, uint16_t* stage, int wave, int lane) {
+// ROWS rows of [0, rows) at base into LDS; rows past them become zero.
+template <class E, int ROWS>
+__device__ __forceinline__ void load_tile(const typename E::elem* base, int rows, typename E::elem* stage, int wave,
+                                          int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using T = Tile<D>;
+    constexpr int RB = E::CPR * 16, RPI = 64 / E::CPR;  // bytes of a row, rows of a load instruction
     const __amdgpu_buffer_rsrc_t rsrc =
-        __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, max(0, min(rows, kKeys)) * D * 2, 0x00020000);
-    dev::static_for<T::NI>([&](auto jc) {
-        constexpr int jj = decltype(jc)::value;
-        const int j = jj * kWaves + wave;
-        const int r = j * T::RPI + lane / T::CPR;
-        const int off = r * D * 2 + (((lane % T::CPR) ^ swz<D>(r)) * 16);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(stage + j * 512), 16,
-                                                 off, 0, 0, 0);
+        __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, max(0, min(rows, ROWS)) * RB, 0x00020000);
+    dev::static_for<ROWS / RPI / kWaves>([&](auto jc) {
+        const int j = decltype(jc)::value * kWaves + wave;
+        const int r = j * RPI + lane / E::CPR;
+        const int off = r * RB + (((lane % E::CPR) ^ swz<E>(r)) * 16);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rsrc, (__attribute__((address_space(3))) void*)(reinterpret_cast<char*>(stage) + j * 1024), 16, off, 0, 0, 0);
     });
 #endif
 }
 
-// Where a lane finds its operands in a tile: the swizzle depends on r % 16
-// alone, so that every read is one of these offsets and a constant.
-template <int D>
-struct Offsets {
-    int k[D / 16];     // A operand of S^T: key lane % 32, chunk 2 kk + h
-    int v[D / 32][2];  // A operand of out^T: coordinates 32 dt + lane % 32, keys 4 h + L / 4 and 8 more
+// Where a lane finds the operands that run over a row's coordinates: of row
+// lane % 32, chunk 2 kk + h.  The swizzle depends on r % 16 alone, so that every
+// read is one of these offsets and a constant.  Those of fp32's many chunks are
+// one offset that 2 kk turns bits of.
+template <class E>
+struct RowAt {
+    int k[E::kRowAts];
+    __device__ __forceinline__ explicit RowAt(int lane) {
+        const int r = lane & 31, h = lane >> 5;
+        dev::static_for<E::kRowAts>([&](auto kc) {
+            constexpr int kk = decltype(kc)::value;
+            k[kk] = r * E::D + ((2 * kk + h) ^ swz<E>(r)) * E::EPC;
+        });
+    }
+    __device__ __forceinline__ RowAt opaque() const {
+        RowAt x = *this;  // or the turned offsets would be kept in registers
+        if constexpr (E::kRowAts == 1) asm volatile("" : "+v"(x.k[0]));
+        return x;
+    }
+    template <int KK>
+    __device__ __forceinline__ typename E::frag frag(const typename E::elem* stage, std::integral_constant<int, KK>) const {
+        const int off = E::kRowAts == 1 ? k[0] ^ (2 * KK * E::EPC) : k[KK % E::kRowAts];
+        return *reinterpret_cast<const typename E::frag*>(stage + off);
+    }
 };
 
-template <int D>
-__device__ __forceinline__ void row_offsets(int (&k)[D / 16], int lane) {
-    const int r = lane & 31, h = lane >> 5;
-    dev::static_for<D / 16>([&](auto kc) {
-        constexpr int kk = decltype(kc)::value;
-        k[kk] = r * D + ((2 * kk + h) ^ swz<D>(r)) * 8;
-    });
-}
-template <int D>
-__device__ __forceinline__ Offsets<D> offsets(int lane) {
-    Offsets<D> o;
-    row_offsets<D>(o.k, lane);
-    // lanes 4 i .. 4 i + 3 of a group of 16 read 16 coordinates of key i, and
-    // lane i of the group ends up with coordinate i of the four keys
-    const int L = lane & 15, gg = lane >> 4;
-    dev::static_for<D / 16>([&](auto dc) {
-        constexpr int dt = decltype(dc)::value / 2, jh = decltype(dc)::value % 2;
-        const int r = 8 * jh + 4 * (gg >> 1) + (L >> 2);
-        o.v[dt][jh] = r * D + ((4 * dt + 2 * (gg & 1) + ((L & 3) >> 1)) ^ swz<D>(r)) * 8 + (L & 1) * 4;
-    });
-    return o;
-}
+// ---- the two types -----------------------------------------------------------------
+template <int D_>
+struct Bf16 {
+    static constexpr int D = D_;
+    typedef uint16_t elem;
+    typedef bf16x8_t frag;                  // a chunk's coordinates
+    static constexpr int EPC = 8;           // of them
+    static constexpr int CPR = D / 8;       // chunks of a row
+    static constexpr int KK = D / 16;       // contraction steps of a row, a chunk each half
+    static constexpr int kRowAts = KK;
+    static constexpr int kKeys = 64;        // keys per tile
+    static constexpr int kTiles = kKeys / 32;
+    static constexpr int kMassResident = 3;  // workgroups that sum weights to a compute unit
 
-__device__ __forceinline__ bf16x8_t row_frag(const uint16_t* stage, int off) {
-    return *reinterpret_cast<const bf16x8_t*>(stage + off);
-}
+    __device__ __forceinline__ static f32x16 dot(frag a, frag b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    struct Values { int v[D / 32][2]; };    // coordinates 32 dt + lane % 32, keys 4 h + L / 4 and 8 more
+    __device__ __forceinline__ static Values values(int lane) {
+        // lanes 4 i .. 4 i + 3 of a group of 16 read 16 coordinates of key i, and
+        // lane i of the group ends up with coordinate i of the four keys
+        Values o;
+        const int L = lane & 15, gg = lane >> 4;
+        dev::static_for<D / 16>([&](auto dc) {
+            constexpr int dt = decltype(dc)::value / 2, jh = decltype(dc)::value % 2;
+            const int r = 8 * jh + 4 * (gg >> 1) + (L >> 2);
+            o.v[dt][jh] = r * D + ((4 * dt + 2 * (gg & 1) + ((L & 3) >> 1)) ^ swz<Bf16>(r)) * 8 + (L & 1) * 4;
+        });
+        return o;
+    }
+    // Keys 16 c + 8 (j / 4) + 4 h + j % 4 of a coordinate, j = 0..7.
+    __device__ __forceinline__ static frag value_frag(const elem* stage, const int (&off)[2], int c) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(const_cast<uint16_t*>(stage + off[0] + 16 * c * D)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(const_cast<uint16_t*>(stage + off[1] + 16 * c * D)));
+        return __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    struct Weights { frag p[4]; };
+    template <int I>  // weight I % 16 of key tile I / 16
+    __device__ __forceinline__ static void put(Weights& w, std::integral_constant<int, I>, float e) {
+        w.p[I / 8][I % 8] = (__bf16)e;
+    }
+    __device__ __forceinline__ static void add_values(f32x16 (&o)[D / 32], const Weights& w, const Values& at,
+                                                      const elem* vs) {
+        constexpr int DT = D / 32;
+        dev::static_for<4>([&](auto cc) {
+            constexpr int c = decltype(cc)::value;
+            dev::static_for<DT>([&](auto dc) {
+                constexpr int dt = decltype(dc)::value;
+                o[dt] = dot(value_frag(vs, at.v[dt], c), w.p[c], o[dt]);
+            });
+        });
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, 8, 1);
+        dev::static_for<4 * DT - 4>([&](auto) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 1);
+        });
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 1);
+    }
+    // six key operands ahead of the products: without it the compiler reads
+    // each one right before its product and waits for LDS every time
+    __device__ __forceinline__ static void order_logits() {
+        constexpr int N = kTiles * KK, AHEAD = 6;
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, AHEAD, 0);
+        dev::static_for<N - AHEAD>([&](auto) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+        });
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, AHEAD, 0);
+    }
+    __device__ __forceinline__ static void store4(elem* p, f32x4 x) {
+        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4_t*>(p) = bf16x4_t{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+    }
+};
 
-// Keys 16 c + 8 (j / 4) + 4 h + j % 4 of a coordinate, j = 0..7.
-template <int D>
-__device__ __forceinline__ bf16x8_t value_frag(const uint16_t* stage, const int (&off)[2], int c) {
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (lds_s16x4*)(const_cast<uint16_t*>(stage + off[0] + 16 * c * D)));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (lds_s16x4*)(const_cast<uint16_t*>(stage + off[1] + 16 * c * D)));
-    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
+// fp32, for the weights' sums, on 32x32x2 products: a chunk is four steps.
+template <int D_>
+struct F32 {
+    static constexpr int D = D_;
+    typedef float elem;
+    typedef f32x4 frag;
+    static constexpr int EPC = 4;
+    static constexpr int CPR = D / 4;
+    static constexpr int KK = D / 8;
+    static constexpr int kRowAts = 1;
+    static constexpr int kMassResident = 2;
+
+    __device__ __forceinline__ static f32x16 dot(frag a, frag b, f32x16 c) {
+        dev::static_for<4>([&](auto ec) {
+            constexpr int e = decltype(ec)::value;
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        });
+        return c;
+    }
+};
 
 // The larger of the lane's value and that of lane ^ 32.
 __device__ __forceinline__ float max_halves(float x) {
@@ -134,53 +206,38 @@ __device__ __forceinline__ float max_halves(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int D>
+template <class E>
 struct State {
-    f32x16 o[D / 32];
-    bf16x8_t q[D / 16];
+    f32x16 o[E::D / 32];
+    typename E::frag q[E::KK];
     float m, z;
 };
 
 // New weights of a lane that call for another maximum.
 constexpr float kMost = 16777216.f;
 
-// Kinds of instructions for the scheduler.
-constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100;
-
-template <int D>
-__device__ __forceinline__ void tile_logits(f32x16 (&s)[2], const State<D>& st, const Offsets<D>& at,
-                                            const uint16_t* ks) {
-    dev::static_for<2>([&](auto tc) {
+// One tile of keys [k0, k0 + kKeys) against the wave's rows.  edge: some row
+// does not see some key (lim: keys that the lane's row sees).
+template <class E>
+__device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, const typename E::Values& at_v,
+                                          const typename E::elem* ks, const typename E::elem* vs, int k0, int lim,
+                                          bool edge, float scale2, int lane) {
+    constexpr int N = 16 * E::kTiles;
+    f32x16 s[E::kTiles];
+    const RowAt<E> at_k = at.opaque();
+    dev::static_for<E::kTiles>([&](auto tc) {
         constexpr int kt = decltype(tc)::value;
         f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        dev::static_for<D / 16>([&](auto kc) {
+        dev::static_for<E::KK>([&](auto kc) {
             constexpr int kk = decltype(kc)::value;
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_frag(ks, at.k[kk] + 32 * kt * D), st.q[kk], acc, 0, 0, 0);
+            acc = E::dot(at_k.frag(ks + 32 * kt * E::D, kc), st.q[kk], acc);
         });
         s[kt] = acc;
     });
-    // six key operands ahead of the products: without it the compiler reads
-    // each one right before its product and waits for LDS every time
-    constexpr int N = 2 * (D / 16), AHEAD = 6;
-    __builtin_amdgcn_sched_group_barrier(kSchedLds, AHEAD, 0);
-    dev::static_for<N - AHEAD>([&](auto) {
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
-    });
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, AHEAD, 0);
-}
-
-// One tile of keys [k0, k0 + 64) against the wave's rows.  edge: some row
-// does not see some key (lim: keys that the lane's row sees).
-template <int D>
-__device__ __forceinline__ void tile_step(State<D>& st, const Offsets<D>& at, const uint16_t* ks, const uint16_t* vs,
-                                          int k0, int lim, bool edge, float scale2, int lane) {
-    constexpr int DT = D / 32;
-    f32x16 s[2];
-    tile_logits<D>(s, st, at, ks);
+    E::order_logits();
     if (edge) {
         const int h4 = 4 * (lane >> 5);
-        dev::static_for<32>([&](auto ic) {
+        dev::static_for<N>([&](auto ic) {
             constexpr int kt = decltype(ic)::value / 16, i = decltype(ic)::value % 16;
             if (k0 + 32 * kt + 8 * (i / 4) + h4 + i % 4 >= lim) s[kt][i] = -INFINITY;
         });
@@ -190,21 +247,21 @@ __device__ __forceinline__ void tile_step(State<D>& st, const Offsets<D>& at, co
     // new weights pass kMost (the first tile's, whose m is the lowest float,
     // always do) is the maximum looked for and everything brought down to it.
     // That spares the common tile the search and its wait for every logit.
-    bf16x8_t p[4];
+    typename E::Weights p;
     float z;
     auto weights = [&]() __attribute__((always_inline)) {
         z = 0.f;
-        dev::static_for<32>([&](auto ic) {
+        dev::static_for<N>([&](auto ic) {
             constexpr int kt = decltype(ic)::value / 16, i = decltype(ic)::value % 16;
             const float e = exp2_hw(__builtin_fmaf(s[kt][i], scale2, -st.m));
             z += e;
-            p[2 * kt + i / 8][i % 8] = (__bf16)e;
+            E::put(p, ic, e);
         });
     };
     weights();
     if (__any(!(z <= kMost))) {
         float top = s[0][0];
-        dev::static_for<31>([&](auto ic) {
+        dev::static_for<N - 1>([&](auto ic) {
             constexpr int e = decltype(ic)::value + 1;
             top = fmaxf(top, s[e / 16][e % 16]);
         });
@@ -212,29 +269,23 @@ __device__ __forceinline__ void tile_step(State<D>& st, const Offsets<D>& at, co
         const float mn = fmaxf(st.m, top), f = exp2_hw(st.m - mn);
         st.m = mn;
         st.z *= f;
-        dev::static_for<DT>([&](auto dc) { st.o[decltype(dc)::value] *= f; });
+        dev::static_for<E::D / 32>([&](auto dc) { st.o[decltype(dc)::value] *= f; });
         weights();
     }
     st.z += z;
-    dev::static_for<4>([&](auto cc) {
-        constexpr int c = decltype(cc)::value;
-        dev::static_for<DT>([&](auto dc) {
-            constexpr int dt = decltype(dc)::value;
-            st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_frag<D>(vs, at.v[dt], c), p[c], st.o[dt], 0, 0, 0);
-        });
-    });
-    __builtin_amdgcn_sched_group_barrier(kSchedLds, 8, 1);
-    dev::static_for<4 * DT - 4>([&](auto) {
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 1);
-    });
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 1);
+    E::add_values(st.o, p, at_v, vs);
 }
 
-template <int D>
+// Bound by the chip's power where both products and exponentials run: 2 x 4096
+// causal queries of 32 heads 265 us (1.03 PFLOP/s of what is seen; the library's
+// product of 8192^3 1.21), and by the exponentials at D 64: 500 queries of 28
+// heads against 24001 keys 93 us (910 TFLOP/s).  With 35 to 56 rows it reads
+// keys and values at 5.3 to 6.0 TB/s.
+template <class E>
 __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
-    using T = Tile<D>;
-    __shared__ __attribute__((aligned(16))) uint16_t k_a[T::ELEMS], v_a[T::ELEMS], k_b[T::ELEMS], v_b[T::ELEMS];
+    using elem = typename E::elem;
+    constexpr int D = E::D, DT = D / 32, kKeys = E::kKeys;
+    __shared__ __attribute__((aligned(16))) elem k_a[kKeys * D], v_a[kKeys * D], k_b[kKeys * D], v_b[kKeys * D];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5;
     // units fastest, so that an XCD's L2 keeps to few of them; causal row
@@ -255,13 +306,13 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     const int rr = r0 + wave * kWaveRows + (lane & 31);
     const bool valid = rr < sg.rows;
     const Row x = decode_row(a, unit, sg.seqs, valid ? rr : 0);
-    State<D> st;
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + x.q + 8 * h;
-    dev::static_for<T::KK>([&](auto kc) {
+    State<E> st;
+    const elem* qp = static_cast<const elem*>(a.q) + x.q + E::EPC * h;
+    dev::static_for<E::KK>([&](auto kc) {
         constexpr int kk = decltype(kc)::value;
-        st.q[kk] = valid ? *reinterpret_cast<const bf16x8_t*>(qp + 16 * kk) : bf16x8_t{};
+        st.q[kk] = valid ? *reinterpret_cast<const typename E::frag*>(qp + 2 * E::EPC * kk) : typename E::frag{};
     });
-    dev::static_for<T::DT>([&](auto dc) { st.o[decltype(dc)::value] = f32x16{}; });
+    dev::static_for<DT>([&](auto dc) { st.o[decltype(dc)::value] = f32x16{}; });
     st.m = kLowest;
     st.z = 0.f;
     // keys that the lane's row sees, and the fewest and most of the wave's rows and the workgroup's
@@ -284,21 +335,22 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     const bool prompt = sg.causal && a.T > sg.n / 5;
     if (prompt || sg.lens) {
         const int each = ((prompt ? all : len) + sg.ns - 1) / sg.ns;
-        chunk = __builtin_amdgcn_readfirstlane(max(2 * kKeys, (each + kKeys - 1) / kKeys * kKeys));
+        chunk = __builtin_amdgcn_readfirstlane(max(128, (each + 63) / 64 * 64));
     }
     const int k_lo = split * chunk, k_hi = min(k_lo + chunk, all);
-    const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
-    const uint16_t* V = static_cast<const uint16_t*>(sg.V) + (long long)unit * sg.cap * D;
-    auto load = [&](int k0, uint16_t* ks, uint16_t* vs) {
+    const elem* K = static_cast<const elem*>(sg.K) + (long long)unit * sg.cap * D;
+    const elem* V = static_cast<const elem*>(sg.V) + (long long)unit * sg.cap * D;
+    auto load = [&](int k0, elem* ks, elem* vs) {
         if (k0 < k_hi) {
-            load_tile<D>(K + (long long)k0 * D, k_hi - k0, ks, wave, lane);
-            load_tile<D>(V + (long long)k0 * D, k_hi - k0, vs, wave, lane);
+            load_tile<E, kKeys>(K + (long long)k0 * D, k_hi - k0, ks, wave, lane);
+            load_tile<E, kKeys>(V + (long long)k0 * D, k_hi - k0, vs, wave, lane);
         }
     };
-    const Offsets<D> at = offsets<D>(lane);
-    auto step = [&](int k0, const uint16_t* ks, const uint16_t* vs) {
+    const RowAt<E> at_k(lane);
+    const typename E::Values at_v = E::values(lane);
+    auto step = [&](int k0, const elem* ks, const elem* vs) {
         if (k0 < most)
-            tile_step<D>(st, at, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
+            tile_step<E>(st, at_k, at_v, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
     };
     load(k_lo, k_a, v_a);
     for (int k0 = k_lo; k0 < k_hi; k0 += 2 * kKeys) {
@@ -315,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     const float z = __uint_as_float(zr[0]) + __uint_as_float(zr[1]);
     if (a.ns > 1) {
         const long long at = x.gr * a.ns + sg.split0 + split;
-        dev::static_for<T::DT * 4>([&](auto ic) {
+        dev::static_for<DT * 4>([&](auto ic) {
             constexpr int dt = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
             *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * dt + 8 * i + 4 * h) =
                 f32x4{st.o[dt][4 * i], st.o[dt][4 * i + 1], st.o[dt][4 * i + 2], st.o[dt][4 * i + 3]};
@@ -326,13 +378,11 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
         }
     } else {
         const RowEnd end = row_end(st.m, z);
-        uint16_t* out = static_cast<uint16_t*>(a.out) + x.q;
-        dev::static_for<T::DT * 4>([&](auto ic) {
+        elem* out = static_cast<elem*>(a.out) + x.q;
+        dev::static_for<DT * 4>([&](auto ic) {
             constexpr int dt = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<bf16x4_t*>(out + 32 * dt + 8 * i + 4 * h) =
-                bf16x4_t{(__bf16)(st.o[dt][4 * i] * end.inv), (__bf16)(st.o[dt][4 * i + 1] * end.inv),
-                         (__bf16)(st.o[dt][4 * i + 2] * end.inv), (__bf16)(st.o[dt][4 * i + 3] * end.inv)};
+            E::store4(out + 32 * dt + 8 * i + 4 * h,
+                      f32x4{st.o[dt][4 * i], st.o[dt][4 * i + 1], st.o[dt][4 * i + 2], st.o[dt][4 * i + 3]} * end.inv);
         });
         if (h == 0) {
             if (a.lse) a.lse[x.lse] = end.lse;
@@ -351,14 +401,17 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
 // unit, and no sum over lanes at the end).  Bound by the exponentials and the
 // products, which overlap in part: 2 x 4096 causal queries of 32 heads 161 us
 // (850 TFLOP/s of what is seen), 340 queries of 32 heads against 21124 keys 85
-// (690; with the rows in the lanes 112).
-template <int D>
-__global__ __launch_bounds__(kThreads, 3) void tile_mass_kernel(Args a, float* part, int parts) {
-    using T = Tile<D>;
+// (690; with the rows in the lanes 112).  fp32: 300 queries of 28 heads
+// against 16000 285 us (120 of the 154 TFLOP/s that its products reach; 409 with
+// every wave loading rows of its own).
+template <class E>
+__global__ __launch_bounds__(kThreads, E::kMassResident) void tile_mass_kernel(Args a, float* part, int parts) {
+    using elem = typename E::elem;
+    constexpr int D = E::D, kRows = 64;  // rows per tile
     typedef int i32x4 __attribute__((ext_vector_type(4)));
-    __shared__ __attribute__((aligned(16))) uint16_t q_a[T::ELEMS], q_b[T::ELEMS];
-    __shared__ __attribute__((aligned(16))) float s_norm[2][kKeys];  // of the tiles' rows
-    __shared__ __attribute__((aligned(16))) int s_lim[2][kKeys];     // keys that they see
+    __shared__ __attribute__((aligned(16))) elem q_a[kRows * D], q_b[kRows * D];
+    __shared__ __attribute__((aligned(16))) float s_norm[2][kRows];  // of the tiles' rows
+    __shared__ __attribute__((aligned(16))) int s_lim[2][kRows];     // keys that they see
     __shared__ float s_sum[kMassKeys];
     const Segment& sg = a.seg[1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -371,23 +424,23 @@ __global__ __launch_bounds__(kThreads, 3) void tile_mass_kernel(Args a, float* p
     const int len = unit_len(sg, unit, a.Hkv);
     if (k0 >= len) return;
     const int key0 = k0 + 64 * kw;
-    const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
-    bf16x8_t kr[2][T::KK];
+    const elem* K = static_cast<const elem*>(sg.K) + (long long)unit * sg.cap * D;
+    typename E::frag kr[2][E::KK];
     dev::static_for<2>([&](auto tc) {
         constexpr int kt = decltype(tc)::value;
-        const uint16_t* kp = K + (long long)min(key0 + 32 * kt + (lane & 31), len - 1) * D + 8 * h;
-        dev::static_for<T::KK>([&](auto kc) {
+        const elem* kp = K + (long long)min(key0 + 32 * kt + (lane & 31), len - 1) * D + E::EPC * h;
+        dev::static_for<E::KK>([&](auto kc) {
             constexpr int kk = decltype(kc)::value;
-            kr[kt][kk] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * kk);
+            kr[kt][kk] = *reinterpret_cast<const typename E::frag*>(kp + 2 * E::EPC * kk);
         });
     });
     f32x4 sum[2] = {};
     const MassRows rows(a, sg.causal, len, k0, kMassKeys, pt, parts);
     int r = rows.first, t = rows.first_t;  // the tile's first row and its query
-    auto load = [&](int row, uint16_t* stage) {
+    auto load = [&](int row, elem* stage) {
         if (row < rows.end)
-            load_tile<D>(static_cast<const uint16_t*>(a.q) + ((long long)unit * a.R + row) * D, rows.end - row, stage, wave,
-                         lane);
+            load_tile<E, kRows>(static_cast<const elem*>(a.q) + ((long long)unit * a.R + row) * D, rows.end - row, stage,
+                                wave, lane);
     };
     // wave 0 sees to the rows' normalisers: requested with a tile, put into LDS after the one before it
     const float* norms = a.row_lse2 + (long long)unit * a.R + lane;
@@ -398,17 +451,17 @@ __global__ __launch_bounds__(kThreads, 3) void tile_mass_kernel(Args a, float* p
             s_lim[buf][lane] = sg.causal ? rows.seen(row + lane) : len;
         }
     };
-    int at[T::KK];
-    row_offsets<D>(at, lane);
-    auto step = [&](int row, int query, const uint16_t* stage, int buf) {
+    const RowAt<E> at(lane);
+    auto step = [&](int row, int query, const elem* stage, int buf) {
         f32x16 s[2] = {};
-        dev::static_for<T::KK>([&](auto kc) {
+        const RowAt<E> rows_at = at.opaque();
+        dev::static_for<E::KK>([&](auto kc) {
             constexpr int kk = decltype(kc)::value;
-            const bf16x8_t q = row_frag(stage, at[kk] + 32 * rw * D);
-            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, kr[0][kk], s[0], 0, 0, 0);
-            s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, kr[1][kk], s[1], 0, 0, 0);
+            const typename E::frag q = rows_at.frag(stage + 32 * rw * D, kc);
+            s[0] = E::dot(q, kr[0][kk], s[0]);
+            s[1] = E::dot(q, kr[1][kk], s[1]);
         });
-        const bool edge = rows.edge(row, query, kKeys);
+        const bool edge = rows.edge(row, query, kRows);
         dev::static_for<4>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
             const f32x4 n = *reinterpret_cast<const f32x4*>(&s_norm[buf][32 * rw + 8 * j + 4 * h]);
@@ -433,7 +486,7 @@ __global__ __launch_bounds__(kThreads, 3) void tile_mass_kernel(Args a, float* p
     put(0, r, norm_at(r));
     while (r < rows.end) {
         const int ra = r, ta = t;
-        rows.advance(r, t, kKeys);
+        rows.advance(r, t, kRows);
         turn();
         load(r, q_b);
         const float nb = norm_at(r);
@@ -441,7 +494,7 @@ __global__ __launch_bounds__(kThreads, 3) void tile_mass_kernel(Args a, float* p
         if (r >= rows.end) break;
         put(1, r, nb);
         const int rb = r, tb = t;
-        rows.advance(r, t, kKeys);
+        rows.advance(r, t, kRows);
         turn();
         load(r, q_a);
         const float na = norm_at(r);
@@ -474,19 +527,23 @@ hipError_t launch_attend_tile(const attend::Args& a, const attend::Segment& sg, 
     const long long items = (long long)sg.units * sg.nrb * sg.ns;
     if (items == 0) return hipSuccess;
     if (a.D == 128)
-        hipLaunchKernelGGL(tile_kernel<128>, dim3((unsigned)items), dim3(kThreads), 0, s, a, sg);
+        hipLaunchKernelGGL(tile_kernel<Bf16<128>>, dim3((unsigned)items), dim3(kThreads), 0, s, a, sg);
     else
-        hipLaunchKernelGGL(tile_kernel<64>, dim3((unsigned)items), dim3(kThreads), 0, s, a, sg);
+        hipLaunchKernelGGL(tile_kernel<Bf16<64>>, dim3((unsigned)items), dim3(kThreads), 0, s, a, sg);
     return hipGetLastError();
 }
 
-hipError_t launch_attend_tile_mass(const attend::Args& a, float* part, int parts, hipStream_t s) {
+hipError_t launch_attend_tile_mass(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s) {
     using namespace attend;
     const dim3 grid((unsigned)mass_blocks(a, parts)), block(kThreads);
-    if (a.D == 128)
-        hipLaunchKernelGGL(tile_mass_kernel<128>, grid, block, 0, s, a, part, parts);
+    if (dtype == BKV_BF16 && a.D == 128)
+        hipLaunchKernelGGL(tile_mass_kernel<Bf16<128>>, grid, block, 0, s, a, part, parts);
+    else if (dtype == BKV_BF16)
+        hipLaunchKernelGGL(tile_mass_kernel<Bf16<64>>, grid, block, 0, s, a, part, parts);
+    else if (a.D == 128)
+        hipLaunchKernelGGL(tile_mass_kernel<F32<128>>, grid, block, 0, s, a, part, parts);
     else
-        hipLaunchKernelGGL(tile_mass_kernel<64>, grid, block, 0, s, a, part, parts);
+        hipLaunchKernelGGL(tile_mass_kernel<F32<64>>, grid, block, 0, s, a, part, parts);
     return hipGetLastError();
 }
 

@@ -131,6 +131,9 @@ __device__ __forceinline__ void move_rows(char* K, char* V, const int* src, cons
 
 // NT threads, PER tokens each in registers; PER 0: masses, ballots and counts
 // stay in memory.
+// Bound by its passes over the registers (search, ballots, moves), a compute
+// unit's instructions: 64 heads of 32768 37 us, 2 of 22101 30; in the form that
+// moves rows too, by those (4608 heads of 4096 -> 3584, 2.4 GB, 293 us).
 template <int NT, int PER, int MODE>
 __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
     constexpr int NW = NT / 64, BPT = kBins / NT;
