@@ -314,12 +314,10 @@ def evict_noalloc(d: Dims, K, V, q_win, beacons, counts, kept=None, scores=None,
 
 
 # ---- attention over the cache, eviction by accumulated weight ----------------------
-def _arg(t, shape, dtype, name, dev, optional=False):
+def _arg(t, shape, dtype, name, dev):
     """Address of a contiguous tensor of this shape and type on GPU `dev`, the
     current device: its stream is where the work goes.  One test decides the
     usual case; what is wrong is found out only where it fails."""
-    if t is None and optional:
-        return None
     if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev
             and t.is_contiguous()):
         return t.data_ptr()
@@ -330,7 +328,7 @@ def _arg(t, shape, dtype, name, dev, optional=False):
 def _device_of(t, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
-    return torch.cuda.current_device()
+    return torch._C._cuda_getDevice()
 
 
 def _arg_ws(ws, dev):
@@ -355,9 +353,9 @@ def _attend_args(d, q, K, V, out, lens, lse, mass, dev):
     if (B, Hq, D) != (d.B, d.Hq, d.D):
         raise ValueError(f"q must have shape {(d.B, d.Hq, T, d.D)}, got {tuple(q.shape)}")
     return T, dt, (_arg(q, rows, dt, "q", dev), _arg(K, cache, dt, "K", dev), _arg(V, cache, dt, "V", dev),
-                   _arg(lens, (B,), torch.int32, "lens", dev, True), _arg(out, rows, dt, "out", dev),
-                   _arg(lse, (B, Hq, T), torch.float32, "lse", dev, True),
-                   _arg(mass, cache[:3], torch.float32, "mass", dev, True))
+                   None if lens is None else _arg(lens, (B,), torch.int32, "lens", dev), _arg(out, rows, dt, "out", dev),
+                   None if lse is None else _arg(lse, (B, Hq, T), torch.float32, "lse", dev),
+                   None if mass is None else _arg(mass, cache[:3], torch.float32, "mass", dev))
 
 
 def attend(d: Dims, q, K, V, out, ws, lens=None, lse=None, mass=None, scale: float = 0.0, causal: bool = False):
@@ -385,7 +383,7 @@ def attend_shared(d: Dims, q, PK, PV, K, V, out, ws, P: int | None = None, p_len
     T, dt, (qp, kp, vp, lp, op, ep, mp) = _attend_args(d, q, K, V, out, lens, lse, mass, dev)
     shape = (groups, d.Hkv, P_cap, d.D)
     pk, pv = _arg(PK, shape, dt, "PK", dev), _arg(PV, shape, dt, "PV", dev)
-    pl = _arg(p_lens, (groups,), torch.int32, "p_lens", dev, True)
+    pl = None if p_lens is None else _arg(p_lens, (groups,), torch.int32, "p_lens", dev)
     wp, wn = _arg_ws(ws, dev)
     st = lib().bkv_attend_shared(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, groups, pk, pv,
                                  P_cap if P is None else int(P), P_cap, pl, kp, vp, lp, scale, op, ep, mp, wp, wn,
@@ -410,7 +408,7 @@ def evict_mass(d: Dims, K, V, mass, ws, kept=None, fill: bool = False):
     dt, cache = _tdtype(d), (d.B, d.Hkv, d.N_cap, d.D)
     kp, vp = _arg(K, cache, dt, "K", dev), _arg(V, cache, dt, "V", dev)
     mp = _arg(mass, cache[:3], torch.float32, "mass", dev)
-    op = _arg(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", dev, True)
+    op = None if kept is None else _arg(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", dev)
     wp, wn = _arg_ws(ws, dev)
     st = lib().bkv_evict_mass(ctypes.byref(d), EVICT_FILL if fill else 0, kp, vp, mp, op, wp, wn,
                               torch._C._cuda_getCurrentRawStream(dev))
