@@ -150,7 +150,10 @@ __device__ __forceinline__ RowEnd row_end(float m, float z) {
 // (g T + t), `parts` workgroups to a block of kMassKeys keys, each a range of
 // rows.  Key j of a causal cache is seen by the queries t >= j - lead.
 constexpr int kMassKeys = 128;
-constexpr int kRegRows = 96;  // rows of a bf16 cache that workgroups hold in registers instead (128 of D 128 do not fit)
+// Rows of a bf16 cache that workgroups hold in registers instead: 128 of D 128
+// do not fit (us, a call of 96 rows, registers and tiles: 128 heads of 4000 tokens
+// 85 103, 16 of 16000 54 61, 512 of 600 57 64, 8 of 8000 29 29).
+constexpr int kRegRows = 96;
 inline long long mass_blocks(const Args& a, int parts) {
     return (long long)a.seg[1].units * parts * ((a.seg[1].n + kMassKeys - 1) / kMassKeys);
 }
