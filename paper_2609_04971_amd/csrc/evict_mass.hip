@@ -21,7 +21,7 @@
 // The rest is moving rows.  Order preserved, compact.hip does it.  Filling
 // holes, the moves are a list, which the selecting workgroup works off itself
 // where there are many heads (one's selection then overlaps another's copies)
-// and a second launch otherwise.
+// or few moves, and a second launch otherwise.
 #include "device_common.h"
 #include "internal.h"
 
@@ -36,6 +36,11 @@ constexpr int kShortThreads = 256;
 // and the other form, 4096 -> 3584 filling holes: 128 heads 31 26, 256 40 40, 512
 // 65 75, 2048 217 268; 8192 -> 7168: 256 73 67, 384 99 100, 768 167 183).
 constexpr int kManyHeads = 256, kManyLongHeads = 384;
+// Bytes that move in a head at most, K and V, where that form is taken whatever
+// the heads' number, as it spares a launch (us captured, the other form and that:
+// 28 heads, 13 KB 14.6 13.2, 13 heads, 54 KB 17.3 14.9, 40 heads, 104 KB 16.7 18.2,
+// 16 heads, 140 KB 16.7 19.3).
+constexpr long long kLittle = 96 << 10;
 constexpr int kOwnMoves = kBins / 2;  // moves that the selecting workgroup's lists hold
 constexpr int kCopyThreads = 256;
 constexpr int kCopyMoves = 64;  // rows per copy item
@@ -494,8 +499,9 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     const bool fill = flags & BKV_EVICT_FILL;
     const int most = n < a.N - n ? n : a.N - n;  // moves of a head at most
     const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
-    const bool many = P >= (a.N <= 16 * kShortThreads ? kManyHeads : kManyLongHeads) &&
-                      a.N <= kPerMax * kShortThreads && (!fill || most <= kOwnMoves);
+    const bool few_moves = fill && a.N <= 16 * kShortThreads && 2LL * most * rb <= kLittle;
+    const bool many = few_moves || (P >= (a.N <= 16 * kShortThreads ? kManyHeads : kManyLongHeads) &&
+                                    a.N <= kPerMax * kShortThreads && (!fill || most <= kOwnMoves));
     if (fill && !many && (long long)P * nchunk > 0xffffffffLL / kCopyThreads) return BKV_ERR_SHAPE;
     const int mode = !fill ? kOrder : many ? kFillCopy : kFill;
     hipError_t e;

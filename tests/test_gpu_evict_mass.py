@@ -190,6 +190,13 @@ def test_captured_graph(fill):
             assert torch.equal(a, b), f"replay {i}"
 
 
+@pytest.mark.parametrize("N,budget", [(700, 652), (700, 650), (4096, 3904), (4096, 3903), (4097, 4000), (4096, 100)])
+def test_few_moves_of_few_heads(N, budget):
+    """Both sides of the bytes that the selecting workgroup moves itself."""
+    for dtype, D in (("bf16", 128), ("fp32", 128), ("bf16", 64)):
+        run_case(1, 3, D, N, N + 3, budget, 16, 4, dtype, "sinks", True)
+
+
 @pytest.mark.parametrize("fill", [False, True])
 def test_two_streams_at_once(fill):
     d = bkv.dims(B=1, Hq=2, Hkv=2, D=128, N=5000, W=8, C=0, budget=3000, n_prefix=2)
