@@ -314,9 +314,10 @@ bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes,
 /* ---- Attention over the cache --------------------------------------------------
  * What the cache is kept for: the newest T tokens of every sequence attend to
  * it, and, optionally, every cached token collects the weight it was given,
- * which bkv_evict_mass ranks by.  With l_tj = scale * <q_t, k_j> (fp32; scale is
- * finite and not negative, 0 selects fp32(1/sqrt(D))), query head hq = h * G + g
- * reading kv-head h:
+ * which bkv_evict_mass ranks by.  With l_tj = scale * <q_t, k_j> (fp32, worked
+ * with as l_tj log2(e), which has to be in fp32's range; scale is not negative,
+ * scale * log2(e) is finite, 0 selects fp32(1/sqrt(D))), query head
+ * hq = h * G + g reading kv-head h:
  *   lse_t = log sum_j exp(l_tj),   out_t = sum_j exp(l_tj - lse_t) v_j,
  *   mass_j += sum over g and t of exp(l_tj - lse_t),
  * over the keys that query t sees: j < len, and with BKV_ATTEND_CAUSAL (the T

@@ -214,7 +214,8 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     if (!q || !out || !aligned(q) || !aligned(out)) return BKV_ERR_INVALID;
     if (d->N > 0 && (!K || !V || !aligned(K) || !aligned(V))) return BKV_ERR_INVALID;
     if (groups > 0 && P > 0 && (!PK || !PV || !aligned(PK) || !aligned(PV))) return BKV_ERR_INVALID;
-    if (!(scale >= 0.0f) || isinf(scale)) return BKV_ERR_INVALID;
+    const float scale2 = (scale == 0.0f ? 1.0f / sqrtf((float)d->D) : scale) * 1.4426950408889634f;
+    if (!(scale >= 0.0f) || isinf(scale2)) return BKV_ERR_INVALID;  // 0 times infinity would be a NaN
     const size_t q_bytes = (size_t)d->B * d->Hq * T * d->D * (d->dtype == BKV_BF16 ? 2 : 4);
     const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
     if (q0 < o0 + q_bytes && o0 < q0 + q_bytes) return BKV_ERR_INVALID;  // queries are read after outputs are written
@@ -236,7 +237,7 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     a.out = out;
     a.lse = lse;
     a.mass = mass;
-    a.scale2 = (scale == 0.0f ? 1.0f / sqrtf((float)d->D) : scale) * 1.4426950408889634f;
+    a.scale2 = scale2;
     Segment& own = a.seg[1];
     own.K = K;
     own.V = V;
