@@ -333,8 +333,10 @@ bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes,
  *           j < len only (NULL to skip).
  * The rows of K, V at or past len are not read, whatever they hold; those
  * below it must be finite (what a query does not see of them has weight 0, and
- * 0 times an infinity or a NaN is a NaN).  Sums,
- * maxima and normalisers are fp32 and no sum depends on the launch; weights
+ * 0 times an infinity or a NaN is a NaN).  Results are finite where no
+ * |v| (keys + 128) passes 2^122, keys being all that a query sees, a prefix's
+ * among them: sums of weighted values are divided last.  Sums, maxima and
+ * normalisers are fp32 and no sum depends on the launch; weights
  * enter the matrix cores as bf16 for bf16 caches.  Of the dims, B, Hq, Hkv, D,
  * N, N_cap and dtype are used; the others need only pass bkv_validate.  N may
  * be 0 (then every query sees nothing).  B * Hq * T < 2^31; T == 0 or B == 0

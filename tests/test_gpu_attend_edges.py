@@ -1,0 +1,42 @@
+"""Edges of the attention over the cache that the sweep of sizes and layouts
+does not reach: values near fp32's range, ragged prompts, and bounds tight
+enough that a single misplaced or missing row of V shows."""
+import pytest
+import torch
+
+import attend_ref
+import paper_2609_04971_amd as bkv
+from gpu_util import say
+from test_gpu_attend import call, make, ref_of
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def _rising(B, Hkv, G, D, T, N, dtype, rise, v_max, seed):
+    """One key in 64 has a logit `rise` above all others', from the second tile
+    on; values of size v_max."""
+    x = make(B, Hkv, G, D, T, N, N, dtype, seed)
+    x["q"].zero_()
+    x["q"][..., 0] = 8.0
+    x["K"].zero_()
+    x["K"][:, :, 70::64, 0] = rise / 8.0  # scale 1
+    g = torch.Generator().manual_seed(seed)
+    x["V"] = (v_max * (0.5 + 0.5 * torch.rand(B, Hkv, N, D, generator=g))).to(DT[dtype]).cuda()
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("rise", [0.0, 4.0, 6.9, 16.5])
+@pytest.mark.parametrize("N", [64, 1000, 9000])
+def test_values_near_the_range_of_fp32(N, rise, T, dtype):
+    """bkv.h: |v| (keys + 128) up to 2^122 gives finite results.  The output is
+    a weighted mean of values, so it is bounded as any other's."""
+    v_max = 2.0 ** 122 / (N + 128)
+    say(f"N{N} T{T} rise {rise} {dtype} values {v_max:.3g}")
+    x = _rising(2, 2, 4, 128, T, N, dtype, rise, v_max, seed=N)
+    d = bkv.dims(B=2, Hq=8, Hkv=2, D=128, N=N, W=0, C=0, budget=1, dtype=dtype)
+    out, lse, mass = call(d, x, T, scale=1.0)
+    assert out.isfinite().all()
+    attend_ref.check(ref_of(x, N, scale=1.0), out, lse, mass, x["mass"], N)
