@@ -324,13 +324,15 @@ bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes,
  * queries are the cache's newest tokens, oldest first) j <= len - T + t.  A
  * query that sees no key has out 0 and lse -inf and gives no weight.
  *   q, out  [B, Hq, T, D] post-RoPE queries and their outputs, dtype of the
- *           dims; out must not overlap any input (q: BKV_ERR_INVALID).
+ *           dims.
  *   K, V    [B, Hkv, N_cap, D] (may be NULL when N is 0); 0 <= N <= N_cap.
  *   lens    optional device [B] int32: sequence b holds lens[b] tokens, taken
  *           as 0 below 0 and as N above N; NULL: N each.
  *   lse     optional [B, Hq, T] fp32 (NULL to skip).
  *   mass    optional [B, Hkv, N_cap] fp32, read and written for the tokens
  *           j < len only (NULL to skip).
+ * out, lse, mass and the workspace must not overlap one another or any input
+ * (BKV_ERR_INVALID).
  * The rows of K, V at or past len are not read, whatever they hold; those
  * below it must be finite (what a query does not see of them has weight 0, and
  * 0 times an infinity or a NaN is a NaN).  Results are finite where no

@@ -216,11 +216,18 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     if (groups > 0 && P > 0 && (!PK || !PV || !aligned(PK) || !aligned(PV))) return BKV_ERR_INVALID;
     const float scale2 = (scale == 0.0f ? 1.0f / sqrtf((float)d->D) : scale) * 1.4426950408889634f;
     if (!(scale >= 0.0f) || isinf(scale2)) return BKV_ERR_INVALID;  // 0 times infinity would be a NaN
-    const size_t q_bytes = (size_t)d->B * d->Hq * T * d->D * (d->dtype == BKV_BF16 ? 2 : 4);
-    const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
-    if (q0 < o0 + q_bytes && o0 < q0 + q_bytes) return BKV_ERR_INVALID;  // queries are read after outputs are written
     const Plan p = make_plan(*d, T, flags & BKV_ATTEND_CAUSAL, mass != nullptr, groups, P, P_cap);
     if (p.end > 0 && (!ws || ws_bytes < p.end || !aligned(ws))) return BKV_ERR_WORKSPACE;
+    // what is written, then what is only read; of the last head the tokens that are there
+    const size_t row = (size_t)d->D * (d->dtype == BKV_BF16 ? 2 : 4), queries = (size_t)d->B * d->Hq * T;
+    auto tokens = [](size_t units, size_t n, size_t cap) { return n > 0 ? (units - 1) * cap + n : 0; };
+    const size_t own_tokens = tokens((size_t)d->B * d->Hkv, d->N, d->N_cap);
+    const size_t pre_tokens = groups > 0 ? tokens((size_t)groups * d->Hkv, P, P_cap) : 0;
+    const Span spans[] = {{out, queries * row},        {lse, queries * sizeof(float)}, {mass, own_tokens * sizeof(float)},
+                          {ws, p.end},                 {q, queries * row},             {K, own_tokens * row},
+                          {V, own_tokens * row},       {PK, pre_tokens * row},         {PV, pre_tokens * row},
+                          {lens, d->B * sizeof(int32_t)}, {p_lens, groups * sizeof(int32_t)}};
+    if (!apart(spans, 11, 4)) return BKV_ERR_INVALID;
     char* w = static_cast<char*>(ws);
     Args a;
     memset(&a, 0, sizeof a);

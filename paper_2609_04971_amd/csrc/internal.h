@@ -164,6 +164,23 @@ constexpr int kFastRowGroups = 8;
 // size is the same for all of them.
 WsLayout ws_layout(const bkv_dims& d, int flags = 0);
 
+// ---- arguments that must not share memory ----------------------------------------
+struct Span {
+    const void* p;  // null: not given
+    size_t bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+// Whether none of the first `written` spans meets any other of the n.
+inline bool apart(const Span* spans, int n, int written) {
+    for (int i = 0; i < written; ++i)
+        for (int j = i + 1; j < n; ++j)
+            if (overlap(spans[i], spans[j])) return false;
+    return true;
+}
+
 // ---- the whole eviction (bkv_evict_ex), split so that a caller can check the
 // arguments before it enqueues anything of its own -----------------------------
 bkv_status evict_check(const bkv_dims* d, int32_t flags, const void* K, const void* V, const void* q_win,

@@ -16,3 +16,38 @@ def test_a_scale_that_leaves_fp32_in_log2_units(call):
         assert ctypes.c_float(scale).value != float("inf")
         assert call(scale=scale, n=16) == bkv.ERR_INVALID
     assert call(scale=2.35e38, n=16) == bkv.ERR_WORKSPACE  # the next check
+
+
+# what is written must not meet anything else: B 4, Hq 8, Hkv 2, D 128, 1000 of 1100 tokens, a prefix of 50 of 60
+ROW = 256
+SIZES = {"out": 4 * 8 * ROW, "lse": 4 * 8 * 4, "mass": (7 * 1100 + 1000) * 4, "ws": None, "q": 4 * 8 * ROW,
+         "K": (7 * 1100 + 1000) * ROW, "V": (7 * 1100 + 1000) * ROW, "PK": (3 * 60 + 50) * ROW, "PV": (3 * 60 + 50) * ROW,
+         "lens": 16, "p_lens": 8}
+WRITTEN = ["out", "lse", "mass", "ws"]
+
+
+def spread(groups, **moved):
+    at = {k: (i + 1) << 36 for i, k in enumerate(SIZES)}
+    at.update(moved)
+    a = {k: ctypes.c_void_p(v) for k, v in at.items()}
+    d = bkv.dims(B=4, Hq=8, Hkv=2, D=128, N=1000, N_cap=1100, W=8, C=0, budget=256, n_prefix=2)
+    need = bkv.lib().bkv_attend_workspace_bytes(ctypes.byref(d), 1, 1, groups, 60 if groups else 0)
+    if groups:
+        return at, need, lambda: bkv.lib().bkv_attend_shared(
+            ctypes.byref(d), 0, a["q"], 1, groups, a["PK"], a["PV"], 50, 60, a["p_lens"], a["K"], a["V"], a["lens"], 0.0, a["out"],
+            a["lse"], a["mass"], a["ws"], need, None)
+    return at, need, lambda: bkv.lib().bkv_attend(ctypes.byref(d), 0, a["q"], 1, a["K"], a["V"], a["lens"], 0.0, a["out"], a["lse"],
+                                                  a["mass"], a["ws"], need, None)
+
+
+@pytest.mark.parametrize("groups", [0, 2])
+@pytest.mark.parametrize("written", WRITTEN)
+@pytest.mark.parametrize("other", list(SIZES))
+def test_outputs_over_anything_else(written, other, groups):
+    if written == other or (not groups and other in ("PK", "PV", "p_lens")):
+        return
+    at, need, _ = spread(groups)
+    size = {**SIZES, "ws": 1024}
+    # at its start, across its end (16 bytes of it), and around all of it
+    for to in (at[other], at[other] + (size[other] - 16 & ~15), at[other] - 16 if size[written] > 16 else at[other]):
+        assert spread(groups, **{written: to})[2]() == bkv.ERR_INVALID

@@ -40,3 +40,28 @@ def test_values_near_the_range_of_fp32(N, rise, T, dtype):
     out, lse, mass = call(d, x, T, scale=1.0)
     assert out.isfinite().all()
     attend_ref.check(ref_of(x, N, scale=1.0), out, lse, mass, x["mass"], N)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 40])
+def test_arrays_that_touch(T, dtype):
+    """Everything in one allocation, each array at the last one's end."""
+    B, Hkv, G, D, N = 2, 2, 4, 64, 300
+    d = bkv.dims(B=B, Hq=Hkv * G, Hkv=Hkv, D=D, N=N, W=0, C=0, budget=1, dtype=dtype)
+    x = make(B, Hkv, G, D, T, N, N, dtype, seed=4, lens=[300, 77])
+    want = call(d, x, T)
+    parts = [x["q"], x["K"], x["V"], x["mass"], want[0], want[1], x["lens"].repeat(32), bkv.attend_workspace(d, T, True)]  # whole vectors
+    store = torch.zeros(sum(p.nbytes for p in parts), dtype=torch.uint8, device="cuda")
+    cut = []
+    for p, raw in zip(parts, store.split([p.nbytes for p in parts])):
+        cut.append(raw.view(p.dtype).view(p.shape))
+        cut[-1].copy_(p)
+    q, K, V, mass, out, lse, lens, ws = cut
+    out.zero_(), lse.zero_()
+    bkv.attend(d, q, K, V, out, ws, lens=lens[:B], lse=lse, mass=mass)
+    assert all(torch.equal(a, b) for a, b in zip((out, lse, mass), want))
+    for bad in (dict(out=q), dict(lse=mass.view(-1)[1:1 + lse.numel()].view(lse.shape)), dict(ws=K.view(-1).view(torch.uint8))):
+        kw = dict(out=out, lse=lse, ws=ws) | bad
+        with pytest.raises(bkv.BkvError) as e:
+            bkv.attend(d, q, K, V, kw["out"], kw["ws"], lens=lens[:B], lse=kw["lse"], mass=mass)
+        assert e.value.status in (bkv.ERR_INVALID, bkv.ERR_WORKSPACE)
