@@ -381,6 +381,9 @@ bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, in
  * Rows of K and V from n on are left as they were; mass[n..N) becomes 0, so
  * that tokens appended there start from nothing.  N <= budget changes nothing.
  *   kept    optional [B, Hkv, n] int32 (NULL to skip).
+ * K, V, mass, kept and the workspace must not overlap (BKV_ERR_INVALID), but
+ * K and V may be one and the same array.  N is the number of tokens of every
+ * sequence, as in the other evictions.
  * Workspace: bkv_mass_workspace_bytes(d), which covers every N <= N_cap,
  * initialised by bkv_workspace_init and usable with bkv_device_status. */
 #define BKV_EVICT_FILL 1

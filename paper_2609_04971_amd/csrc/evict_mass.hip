@@ -465,8 +465,17 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     char* w = static_cast<char*>(ws);
     const int P = d->B * d->Hkv;
     const int n = d->N < d->budget ? d->N : d->budget;
+    if (d->N <= d->budget && !kept) return BKV_OK;
+    const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
+    const size_t tokens = (size_t)(P - 1) * d->N_cap + d->N;  // of the last head those that are there
+    // K and V may be one array, whose rows then move once more to the same places
+    const Span spans[] = {{K, tokens * rb},
+                          {V == K ? nullptr : V, tokens * rb},
+                          {mass, tokens * sizeof(float)},
+                          {kept, (size_t)P * n * sizeof(int32_t)},
+                          {ws, m.end}};
+    if (!apart(spans, 5, 5)) return BKV_ERR_INVALID;
     if (d->N <= d->budget) {
-        if (!kept) return BKV_OK;
         const long long total = (long long)P * n;  // at most 2^31
         hipLaunchKernelGGL(mass_identity_kernel, dim3((unsigned)((total + kCopyThreads - 1) / kCopyThreads)),
                            dim3(kCopyThreads), 0, stream, kept, n, total);
@@ -491,7 +500,6 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     a.hdr = reinterpret_cast<int*>(w);
     a.P = P;
     a.budget = d->budget;
-    const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
     a.K = static_cast<char*>(K);
     a.V = static_cast<char*>(V);
     a.head_stride = (size_t)d->N_cap * rb;

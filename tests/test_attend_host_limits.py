@@ -51,3 +51,26 @@ def test_outputs_over_anything_else(written, other, groups):
     # at its start, across its end (16 bytes of it), and around all of it
     for to in (at[other], at[other] + (size[other] - 16 & ~15), at[other] - 16 if size[written] > 16 else at[other]):
         assert spread(groups, **{written: to})[2]() == bkv.ERR_INVALID
+
+
+def _evict_spread(N, **moved):
+    """evict_mass of 4 x 2 heads of N of 1100 tokens, budget 256, its arrays far apart but for those moved."""
+    at = {k: (i + 1) << 36 for i, k in enumerate(("K", "V", "mass", "kept", "ws"))}
+    at.update(moved)
+    a = {k: ctypes.c_void_p(v) for k, v in at.items()}
+    d = bkv.dims(B=4, Hq=8, Hkv=2, D=128, N=N, N_cap=1100, W=8, C=0, budget=256, n_prefix=2)
+    need = bkv.lib().bkv_mass_workspace_bytes(ctypes.byref(d))
+    size = {"K": (7 * 1100 + N) * ROW, "V": (7 * 1100 + N) * ROW, "mass": (7 * 1100 + N) * 4, "kept": 8 * min(N, 256) * 4, "ws": need}
+    return at, size, lambda: bkv.lib().bkv_evict_mass(ctypes.byref(d), 0, a["K"], a["V"], a["mass"], a["kept"], a["ws"], need, None)
+
+
+@pytest.mark.parametrize("N", [1000, 200])
+@pytest.mark.parametrize("one", ["K", "V", "mass", "kept", "ws"])
+@pytest.mark.parametrize("other", ["K", "V", "mass", "kept", "ws"])
+def test_eviction_over_itself(one, other, N):
+    if one == other:
+        return
+    at, size, _ = _evict_spread(N)
+    for to in (at[other], at[other] + (size[other] - 16 & ~15), at[other] - 16):
+        if {one, other} != {"K", "V"} or to != at[other]:  # K and V may be one array
+            assert _evict_spread(N, **{one: to})[2]() == bkv.ERR_INVALID
