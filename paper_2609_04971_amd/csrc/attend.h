@@ -46,14 +46,15 @@ struct Args {
     float scale2;         // scale * log2(e)
 };
 
-// How a call is cut.  Everything but the splits depends on the capacities
-// only, and the splits are at most those of the capacities, so a workspace
-// serves every N <= N_cap and P <= P_cap.
+// How a call is cut.  N and P choose between kernels, row blocks, splits and
+// parts; the workspace is laid out by what is most over all N <= N_cap and
+// P <= P_cap, from the capacities alone, so that one serves them all.
 struct Plan {
     bool own_tile, pre_tile;  // the tile kernel takes the segment
     bool wide;                // the streaming kernel takes 32 rows an item, else 16
     int own_nrb, pre_nrb;
     int own_ns, own_chunk, pre_ns, pre_chunk;
+    int ns_room;              // partials of a row that the workspace holds
     bool keep;                // the logits are kept for the mass
     int mass_ns, mass_chunk;  // else, of rows that fit registers (mass_ns > 0): splits of the keys
     int parts;                // or: workgroups that share a block of keys

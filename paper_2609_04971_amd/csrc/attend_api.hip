@@ -136,8 +136,12 @@ Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
     const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
-    int ns_cap = most_splits(own, d.N_cap), own_ns, pre_ns = 1;
-    if (groups > 0) ns_cap += most_splits(pre_units * ((pre_rows + 127) / 128), P_cap);  // as many as either kernel takes
+    // room for every N and P within the capacities: P decides between the kernels
+    // and so the size of the row blocks, and the splits are most with the fewest items
+    const int widest = p.own_tile ? 128 : 32;
+    p.ns_room = most_splits((long long)d.B * d.Hkv * ((R + widest - 1) / widest), d.N_cap);
+    if (groups > 0) p.ns_room += most_splits(pre_units * ((pre_rows + 127) / 128), P_cap);
+    int own_ns, pre_ns = 1;
     if (groups > 0 && P > 0 && !p.own_tile && !p.pre_tile) {  // one launch takes both
         const long long all = own * d.N + pre * P;
         own_ns = shared_splits(own, d.N, all);
@@ -160,9 +164,9 @@ Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int
         cut(d.N, best_splits(false, (long long)d.B * d.Hkv, d.N, 0, d.D), &p.mass_ns, &p.mass_chunk);
     size_t off = 0;
     p.part_o = off;
-    if (ns_cap > 1) off = up(off + sizeof(float) * (size_t)rows * ns_cap * d.D, kAlign);
+    if (p.ns_room > 1) off = up(off + sizeof(float) * (size_t)rows * p.ns_room * d.D, kAlign);
     p.part_ml = off;
-    if (ns_cap > 1) off = up(off + sizeof(float) * (size_t)rows * ns_cap * 2, kAlign);
+    if (p.ns_room > 1) off = up(off + sizeof(float) * (size_t)rows * p.ns_room * 2, kAlign);
     p.row_lse2 = off;
     if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
     p.logits = off;
@@ -218,6 +222,7 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     if (!(scale >= 0.0f) || isinf(scale2)) return BKV_ERR_INVALID;  // 0 times infinity would be a NaN
     const Plan p = make_plan(*d, T, flags & BKV_ATTEND_CAUSAL, mass != nullptr, groups, P, P_cap);
     if (p.end > 0 && (!ws || ws_bytes < p.end || !aligned(ws))) return BKV_ERR_WORKSPACE;
+    if (p.own_ns + p.pre_ns > p.ns_room) return BKV_ERR_WORKSPACE;  // (the room covers every N and P)
     // what is written, then what is only read; of the last head the tokens that are there
     const size_t row = (size_t)d->D * (d->dtype == BKV_BF16 ? 2 : 4), queries = (size_t)d->B * d->Hq * T;
     auto tokens = [](size_t units, size_t n, size_t cap) { return n > 0 ? (units - 1) * cap + n : 0; };

@@ -74,3 +74,38 @@ def test_eviction_over_itself(one, other, N):
     for to in (at[other], at[other] + (size[other] - 16 & ~15), at[other] - 16):
         if {one, other} != {"K", "V"} or to != at[other]:  # K and V may be one array
             assert _evict_spread(N, **{one: to})[2]() == bkv.ERR_INVALID
+
+
+# B, Hkv, G, T, N_cap, groups, P_cap: both sides of the items up to which a prefix is streamed (1024 of 32 rows and
+# 128 keys), of 16, 32, 96 and 128 rows, of one split and many
+SHAPES = [(4, 2, 4, 1, 1100, 2, 600), (64, 4, 4, 1, 500, 2, 6000), (48, 2, 7, 1, 900, 1, 40000), (6, 2, 8, 3, 20000, 3, 3000),
+          (8, 8, 2, 8, 300, 8, 9000), (300, 1, 5, 2, 64, 30, 1000), (2, 1, 33, 1, 70000, 1, 70000), (1, 8, 4, 40, 5000, 1, 100),
+          (16, 2, 16, 1, 2000, 4, 33000), (9, 3, 1, 97, 4000, 3, 129), (200, 8, 4, 1, 4096, 0, 0), (1, 2, 4, 1, 66000, 0, 0),
+          (3, 2, 6, 11, 8000, 0, 0), (1, 4, 1, 700, 7000, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", [bkv.BF16, bkv.F32])
+@pytest.mark.parametrize("mass", [0, 1])
+@pytest.mark.parametrize("B,Hkv,G,T,N_cap,groups,P_cap", SHAPES)
+def test_one_workspace_size_covers_every_length_and_prefix(B, Hkv, G, T, N_cap, groups, P_cap, mass, dtype):
+    """The size asked for with N 0 lets every N and P past the workspace's check: the next one, outputs that overlap,
+    refuses the call then.  One byte less does not."""
+    lib, out = bkv.lib(), ctypes.c_void_p(1 << 50)
+    p = [ctypes.c_void_p((i + 1) << 44) for i in range(7)]
+    for D in (64, 128):
+        d = bkv.dims(B=B, Hq=Hkv * G, Hkv=Hkv, D=D, N=0, N_cap=N_cap, W=0, C=0, budget=1).replace(dtype=dtype)
+        need = lib.bkv_attend_workspace_bytes(ctypes.byref(d), T, mass, groups, P_cap)
+        for N in sorted({0, 1, 127, 129, 1000, N_cap // 3, N_cap // 2, N_cap - 1, N_cap} & set(range(N_cap + 1))):
+            dn = d.replace(N=N)
+            for P in sorted({0, 1, 129, 1000, P_cap // 5, P_cap // 2, P_cap - 1, P_cap} & set(range(P_cap + 1))):
+                for flags in (0, bkv.ATTEND_CAUSAL):
+                    for n, code in ((need, bkv.ERR_INVALID), (need - 1, bkv.ERR_WORKSPACE)):
+                        if not need and n < 0:
+                            continue
+                        m = p[5] if mass else None
+                        if groups:
+                            st = lib.bkv_attend_shared(ctypes.byref(dn), flags, p[0], T, groups, p[1], p[2], P, P_cap, None, p[3], p[4],
+                                                       None, 0.0, out, out, m, p[6], n, None)
+                        else:
+                            st = lib.bkv_attend(ctypes.byref(dn), flags, p[0], T, p[3], p[4], None, 0.0, out, out, m, p[6], n, None)
+                        assert st == code, (D, N, P, flags, n)
