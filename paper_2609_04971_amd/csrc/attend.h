@@ -87,10 +87,11 @@ __device__ __forceinline__ Row decode_row(const Args& a, int unit, int seqs, int
 enum Keep { kKeepNone, kKeepLds, kKeepStore };
 constexpr int kPadO = 4, kPadL = 16;  // floats that keep the rows of the LDS arrays apart
 constexpr size_t kLdsRoom = 79 * 1024;  // two workgroups a compute unit
+inline size_t stream_lds(int o_rows, int D, int kept_rows, int chunk) {
+    return ((size_t)4 * o_rows * (D + kPadO) + (size_t)kept_rows * (chunk + kPadL)) * sizeof(float);
+}
 inline size_t stream_lds(const Args& a) {
-    size_t n = (size_t)4 * a.o_rows * (a.D + kPadO);
-    if (a.keep == kKeepLds) n += (size_t)a.R * (a.seg[1].chunk + kPadL);
-    return n * sizeof(float);
+    return stream_lds(a.o_rows, a.D, a.keep == kKeepLds ? a.R : 0, a.seg[1].chunk);
 }
 
 // Workgroups of 256 threads that one launch holds: its threads are counted in

@@ -170,7 +170,11 @@ Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int
     p.row_lse2 = off;
     if (mass) off = up(off + sizeof(float) * (size_t)rows, kAlign);
     p.logits = off;
-    if (p.keep) off = up(off + sizeof(float) * (size_t)rows * up((size_t)d.N_cap, 32), kAlign);
+    // kept logits go to memory where other splits have a say in the normalisers or
+    // LDS does not hold them; a decoding step of many heads needs no room for them
+    const int most_chunk = (int)up((size_t)d.N_cap, kMinChunk);
+    if (p.keep && (p.ns_room > 1 || stream_lds(R < 16 ? (int)R : 16, d.D, (int)R, most_chunk) > kLdsRoom))
+        off = up(off + sizeof(float) * (size_t)rows * up((size_t)d.N_cap, 32), kAlign);
     // the sums of parts > 1 never pass 2 kMassItems blocks
     p.parts = 1;
     p.parts_at = off;

@@ -109,3 +109,13 @@ def test_one_workspace_size_covers_every_length_and_prefix(B, Hkv, G, T, N_cap, 
                         else:
                             st = lib.bkv_attend(ctypes.byref(dn), flags, p[0], T, p[3], p[4], None, 0.0, out, out, m, p[6], n, None)
                         assert st == code, (D, N, P, flags, n)
+
+
+def test_no_room_for_logits_that_stay_on_the_chip():
+    # 36 layers of 16 sequences, 8 kv-heads of 4 query heads, up to 4096 tokens: more heads than are ever split, and a head's
+    # logits fit LDS, so that only the normalisers are left
+    d = bkv.dims(B=576, Hq=32, Hkv=8, D=128, N=0, N_cap=4096, W=0, C=0, budget=1)
+    rows, asked = 576 * 32, lambda **kw: bkv.lib().bkv_attend_workspace_bytes(ctypes.byref(d.replace(**kw)), 1, 1, 0, 0)  # noqa: E731
+    assert asked() < 1 << 20
+    assert asked(N_cap=5000) >= rows * 5000 * 4   # more than LDS holds
+    assert asked(B=64) >= 64 * 32 * 4096 * 4      # split over two workgroups

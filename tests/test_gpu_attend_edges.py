@@ -65,3 +65,18 @@ def test_arrays_that_touch(T, dtype):
         with pytest.raises(bkv.BkvError) as e:
             bkv.attend(d, q, K, V, kw["out"], kw["ws"], lens=lens[:B], lse=kw["lse"], mass=mass)
         assert e.value.status in (bkv.ERR_INVALID, bkv.ERR_WORKSPACE)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,Hkv,G,T,cap", [(350, 3, 4, 1, 700), (520, 2, 8, 2, 900), (520, 2, 5, 1, 4096), (6, 2, 4, 1, 120)])
+def test_nothing_is_written_behind_the_workspace(B, Hkv, G, T, cap, dtype):
+    """Weights of heads that are never split, whose logits stay in LDS, and of some whose do not."""
+    d = bkv.dims(B=B, Hq=Hkv * G, Hkv=Hkv, D=64, N=cap, W=0, C=0, budget=1, dtype=dtype)
+    n = int(bkv.lib().bkv_attend_workspace_bytes(d, T, 1, 0, 0))
+    store = torch.full((n + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+    for N in (cap, cap // 3):
+        say(f"B{B} Hkv{Hkv} G{G} T{T} N{N}/{cap} {dtype}, workspace of {n} bytes")
+        x = make(B, Hkv, G, 64, T, N, cap, dtype, seed=N)
+        got = call(d.replace(N=N), x, T, causal=True, ws=store[:n])
+        attend_ref.check(ref_of(x, N, True), *got, x["mass"], N)
+        assert (store[n:] == 0xAB).all()
