@@ -157,6 +157,8 @@ class PeriodicEviction:
             raise ValueError("the prefix comes before every other token")
         if K.shape != V.shape or K.dim() != 4 or tuple(K.shape[:2]) != (self.layers, self.Hkv) or K.shape[3] != self.D:
             raise ValueError(f"the prefix is [layers, Hkv, P, D], got {tuple(K.shape)} and {tuple(V.shape)}")
+        if any(x.dtype != self.K.dtype or x.device != self.K.device for x in (K, V)):
+            raise ValueError(f"the prefix must be {self.K.dtype} on {self.K.device}, as the cache is")
         self.t = K.shape[2]
         if self.t:
             self.prefix = (K.contiguous(), V.contiguous())
@@ -181,6 +183,11 @@ class PeriodicEviction:
             raise ValueError("the prompt must end before the recent window")
         if self.mode == "mass" and q_rope is None:
             raise ValueError("mode 'mass' needs the prompt's post-RoPE queries")
+        if self.attention and q_rope is not None:
+            want = (self.LB, self.Hq, T, self.D)
+            if tuple(q_rope.shape) != want or q_rope.dtype != self.K.dtype or q_rope.device != self.K.device:
+                raise ValueError(f"q_rope must be {want}, {self.K.dtype} on {self.K.device}: got {tuple(q_rope.shape)}, "
+                                 f"{q_rope.dtype} on {q_rope.device}")
         self.K[:, :, :T] = K
         self.V[:, :, :T] = V
         self.L = T
