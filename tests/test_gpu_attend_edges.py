@@ -4,6 +4,7 @@ enough that a single misplaced or missing row of V shows."""
 import pytest
 import torch
 
+import attend_bounds
 import attend_ref
 import paper_2609_04971_amd as bkv
 from gpu_util import say
@@ -80,3 +81,45 @@ def test_nothing_is_written_behind_the_workspace(B, Hkv, G, T, cap, dtype):
         got = call(d.replace(N=N), x, T, causal=True, ws=store[:n])
         attend_ref.check(ref_of(x, N, True), *got, x["mass"], N)
         assert (store[n:] == 0xAB).all()
+
+
+def spread(B, Hkv, G, D, T, N, cap, dtype, causal=False, lens=None, groups=0, P=0, P_cap=0, p_lens=None, tiled_prefix=False, seed=0):
+    """A call whose outputs show every row of V: attend_bounds."""
+    say(f"B{B} Hkv{Hkv} G{G} D{D} T{T} N{N}/{cap} {dtype} causal={causal} lens={lens} groups={groups} P={P} {p_lens}")
+    d = bkv.dims(B=B, Hq=Hkv * G, Hkv=Hkv, D=D, N=N, N_cap=cap, W=0, C=0, budget=1, dtype=dtype)
+    x = make(B, Hkv, G, D, T, N, cap, dtype, seed=N + T + seed, lens=lens, groups=groups, P=P, P_cap=P_cap, p_lens=p_lens)
+    attend_bounds.spread_rows(x["V"], first=P, seed=seed)
+    for b in range(B):
+        x["V"][b, :, N if lens is None else min(max(lens[b], 0), N):] = float("nan")
+    if groups:
+        attend_bounds.spread_rows(x["PV"], seed=seed + 1)
+        for a in range(groups):
+            x["PV"][a, :, P if p_lens is None else min(max(p_lens[a], 0), P):] = float("nan")
+    ws = bkv.attend_workspace(d, T, True, groups, P_cap)
+    ws.fill_(0xff)
+    out, lse, mass = call(d, x, T, causal, P=P, ws=ws)
+    worst = attend_bounds.check(d, T, ref_of(x, N, causal, P=P), out, lse, mass, x["mass"], N, tiled_prefix)
+    say(f"  worst {worst:.3f} of the bound")
+    return ws
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,G", [(1, 1), (1, 4), (3, 7), (8, 4), (9, 4), (60, 2), (130, 4)])
+@pytest.mark.parametrize("N", [17, 128, 700, 1111, 4097, 5000])
+def test_every_row_of_v_counts(N, T, G, D, dtype):
+    # one split and several, both kernels, whole tiles and pieces of one
+    spread(1, 2, G, D, T, N, N + N % 3, dtype, causal=T <= N)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kw", [
+    dict(B=4, Hkv=2, G=4, D=128, T=1, N=61, cap=64, groups=1, P=700, P_cap=700),
+    dict(B=6, Hkv=2, G=2, D=64, T=2, N=100, cap=128, groups=3, P=333, P_cap=400, causal=True, lens=[0, 1, 2, 99, 100, 50], p_lens=[333, 0, 17]),
+    dict(B=64, Hkv=4, G=4, D=128, T=1, N=9, cap=9, groups=2, P=2000, P_cap=2048, p_lens=[2000, 129], tiled_prefix=False),
+    dict(B=64, Hkv=4, G=4, D=128, T=1, N=9, cap=9, groups=2, P=4200, P_cap=4200, p_lens=[4200, 129], tiled_prefix=True),
+    dict(B=16, Hkv=8, G=4, D=128, T=1, N=300, cap=300, groups=1, P=9000, P_cap=9001, lens=[300 - 20 * i for i in range(16)], tiled_prefix=True),
+    dict(B=8, Hkv=8, G=4, D=64, T=1, N=3000, cap=3100, lens=[3000, 1, 2999, 0, 64, 1500, 128, 129]),
+])
+def test_every_row_of_v_counts_of_prefixes_and_ragged_batches(kw, dtype):
+    spread(dtype=dtype, **kw)
