@@ -123,3 +123,37 @@ def test_every_row_of_v_counts(N, T, G, D, dtype):
 ])
 def test_every_row_of_v_counts_of_prefixes_and_ragged_batches(kw, dtype):
     spread(dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N,T,lens,splits,parts", [
+    (300, 300, [300, 75, 1, 0], False, True),          # prompts padded to the longest
+    (1500, 600, [1500, 599, 130, 400], True, True),    # lengths below the queries': their first rows see nothing
+    (1500, 600, [601, 1499, 2 ** 31 - 1, -5], True, True),
+    (4000, 500, [4000, 2100, 501, 64], True, True),    # chunks, a fifth of the keys and less
+    (700, 130, [700, 129, 131, 333], False, True),
+    (2000, 64, [2000, 64, 63, 1025], True, False),
+])
+def test_ragged_prompts(N, T, lens, splits, parts, D, dtype):
+    ws = spread(4, 2, 4, D, T, N, N + 3, dtype, causal=True, lens=lens)
+    # partials are the workspace's first region, the parts' sums its last: the fill is gone where they were taken (whether
+    # the other prompts are split depends on D)
+    if splits and dtype == "bf16":
+        assert (ws[:4096] != 0xff).any()
+    if parts:
+        assert (ws[-(1 << 20):] != 0xff).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kw", [
+    dict(B=3, Hkv=2, G=3, D=128, T=400, N=400, cap=400, lens=[400, 33, 256]),                  # not causal
+    dict(B=2, Hkv=1, G=7, D=64, T=290, N=1300, cap=1301, causal=True, lens=[1300, 288]),
+    dict(B=3, Hkv=1, G=1, D=128, T=1030, N=1030, cap=1030, causal=True, lens=[1030, 515, 2]),  # one head, many queries
+    dict(B=9, Hkv=2, G=4, D=128, T=256, N=256, cap=256, causal=True, lens=[256, 0, 1, 63, 64, 65, 127, 128, 255]),
+    dict(B=4, Hkv=2, G=4, D=128, T=150, N=900, cap=900, causal=True, lens=[900, 149, 0, 450], groups=2, P=700, P_cap=701,
+         p_lens=[700, 63], tiled_prefix=True),
+    dict(B=4, Hkv=1, G=4, D=64, T=200, N=200, cap=200, causal=True, lens=[200, 199, 1, 0], groups=1, P=2000, P_cap=2000, tiled_prefix=True),
+])
+def test_ragged_prompts_of_other_layouts(kw, dtype):
+    spread(dtype=dtype, **kw)
