@@ -338,11 +338,13 @@ bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes,
  * 0 times an infinity or a NaN is a NaN).  Results are finite where no
  * |v| (keys + 128) passes 2^122, keys being all that a query sees, a prefix's
  * among them: sums of weighted values are divided last.  Sums, maxima and
- * normalisers are fp32 and no sum depends on the launch; weights
- * enter the matrix cores as bf16 for bf16 caches.  Of the dims, B, Hq, Hkv, D,
- * N, N_cap and dtype are used; the others need only pass bkv_validate.  N may
- * be 0 (then every query sees nothing).  B * Hq * T < 2^31; T == 0 or B == 0
- * enqueues nothing.
+ * normalisers are fp32 and no sum depends on the launch.  Weights enter the
+ * matrix cores in fp32 for fp32 caches; for bf16 ones as two bf16 terms (off by
+ * 2^-17 of a weight) where keys are shared by at most 32 rows, G T, or G T B /
+ * groups for a prefix's (for a short prefix by more), else as one (2^-8).
+ * Of the dims, B, Hq, Hkv, D, N, N_cap and dtype are used; the others need
+ * only pass bkv_validate.  N may be 0 (then every query sees nothing).
+ * B * Hq * T < 2^31; T == 0 or B == 0 enqueues nothing.
  * The workspace needs no initialisation and holds nothing between calls; its
  * size covers every N <= N_cap.  mass: whether calls pass a mass; groups and
  * P_cap: those of bkv_attend_shared (0, 0 for bkv_attend).  0 bytes: none is
