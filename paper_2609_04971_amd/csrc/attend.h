@@ -40,7 +40,7 @@ struct Args {
     int keep;             // Keep: whether and where an item keeps its logits
     int o_rows;           // rows of a 16-row tile that any item has
     int Hq, Hkv, G, T, R, D;
-    int N, N_cap;
+    int N_cap;
     int rows;             // B * Hq * T
     int ns;               // partials per row; 1: the outputs are written directly
     float scale2;         // scale * log2(e)

@@ -246,7 +246,6 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     a.T = T;
     a.R = a.G * T;
     a.D = d->D;
-    a.N = d->N;
     a.N_cap = d->N_cap;
     a.rows = d->B * d->Hq * T;
     a.q = q;
