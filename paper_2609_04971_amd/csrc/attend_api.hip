@@ -15,18 +15,26 @@ inline size_t up(size_t x, size_t n) { return (x + n - 1) / n * n; }
 constexpr int kCus = 256;
 constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a streaming item, two tiles
 // Bytes of a unit's keys that one streaming item takes rather than splits and a
-// join: the second launch costs 3.2 us, a round of 32 bf16 or 16 fp32 keys a
-// wave 1.1 (us captured, in one piece and split, 8 heads of 128: bf16 256 tokens
-// 6.3 8.3, 512 8.4 8.4, 768 10.7 8.4; fp32 256 9.1 9.8, 400 12.4 10.0).
+// join.  The second launch costs 2.5 us where calls are captured, but the host's
+// time for it where they are launched one by one, so the two break even at
+// about 96 and 160 KB: the limit lies between, and up to it neither loses more
+// than a quarter (us captured / one by one, in one piece and split, 8 heads:
+// bf16 D 128 256 tokens 6.3 / 7.5 and 7.8 / 9.9, 512 8.5 / 8.4 and 8.0 / 9.9, 640
+// 10.1 / 9.8 and 8.5 / 9.8; D 64 768 7.5 / 7.5 and 7.5 / 10.1, 1024 8.8 / 8.7 and
+// 7.9 / 9.9; fp32 D 64 256 6.5 / 7.4 and 7.6 / 9.8, 512 9.5 / 9.3 and 7.6 / 9.9; D
+// 128 256 9.2 / 9.0 and 9.3 / 9.8, 384 11.6 / 11.5 and 9.5 / 10.3).
 constexpr long long kWhole = 128 << 10;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
 // Items of 32 rows and kMinChunk keys up to which a prefix of more rows is
 // streamed all the same, in one launch with the sequences' own caches: its keys
-// are read by every row block, but from L2, and the tiles' launch is spared (us
-// captured, tiles and so, items: 12 23.0 18.7, 96 23.7 21.5, 120 35.1 27.3, 440
-// 21.5 23.4, 496 35.2 27.8, 592 28.6 24.3, 928 32.3 29.0, 1088 52.7 68.6, 1344
-// 155 148, 3360 38 49, 4914 74 101).
+// are read by every row block, but from L2, and the tiles' launch is spared.  Up
+// to 480 items that is ahead nearly always, from 1088 on it is far behind; in
+// between the number alone does not decide, by up to 14 % either way (us, tiles
+// and items: 24 13.7 11.0, 192 17.4 13.5, 256 18.8 14.4, 288 21.8 16.4, 320 18.5
+// 18.9, 432 27.2 25.8, 480 21.0 17.8, 504 17.2 19.6, 576 21.9 22.8, 640 20.1 20.1,
+// 704 22.9 21.8, 792 20.0 20.4, 1008 21.4 24.2, 1024 23.0 24.7, 1088 52.7 68.6, 3360
+// 38 49).
 constexpr long long kFewItems = 4 * kCus;
 
 // Workgroups that sum the weights of many rows: where the blocks of keys alone

@@ -32,14 +32,15 @@ constexpr int kBins = 4096;
 constexpr int kPerMax = 32;    // tokens per thread in registers
 constexpr int kLongThreads = 1024;  // threads per head, and few where heads are many and short
 constexpr int kShortThreads = 256;
-// Heads from which on a workgroup of kShortThreads selects and moves (us, that
-// and the other form, 4096 -> 3584 filling holes: 128 heads 31 26, 256 40 40, 512
-// 65 75, 2048 217 268; 8192 -> 7168: 256 73 67, 384 99 100, 768 167 183).
+// Heads from which on a workgroup of kShortThreads selects and moves (us on
+// masses that no eviction has seen, that and the other form, 4096 -> 3584 filling
+// holes: 128 heads 34 28, 256 42 41, 384 57 65, 512 68 78, 2048 209 285; 8192 ->
+// 7168: 256 76 70, 384 104 108, 768 176 194; in order both are the same but for 2 %).
 constexpr int kManyHeads = 256, kManyLongHeads = 384;
 // Bytes that move in a head at most, K and V, where that form is taken whatever
-// the heads' number, as it spares a launch (us captured, the other form and that:
-// 28 heads, 13 KB 14.6 13.2, 13 heads, 54 KB 17.3 14.9, 40 heads, 104 KB 16.7 18.2,
-// 16 heads, 140 KB 16.7 19.3).
+// the heads' number, as it spares a launch (us, the other form and that: 28 heads,
+// 12 KB 18.9 17.9, 13 heads, 50 KB 17.3 16.0, 64 heads, 75 KB 19.0 19.4; 40 heads, 104
+// KB 18.0 17.8, 8 heads, 100 KB 18.1 19.4, 16 heads, 140 KB 18.0 18.9).
 constexpr long long kLittle = 96 << 10;
 constexpr int kOwnMoves = kBins / 2;  // moves that the selecting workgroup's lists hold
 constexpr int kCopyThreads = 256;
@@ -137,8 +138,11 @@ __device__ __forceinline__ void move_rows(char* K, char* V, const int* src, cons
 // NT threads, PER tokens each in registers; PER 0: masses, ballots and counts
 // stay in memory.
 // Bound by its passes over the registers (search, ballots, moves), a compute
-// unit's instructions: 64 heads of 32768 37 us, 2 of 22101 30; in the form that
-// moves rows too, by those (4608 heads of 4096 -> 3584, 2.4 GB, 293 us).
+// unit's instructions: 64 heads of 32768 38 us, 2 of 22101 26; in the form that
+// moves rows too, by those (4608 heads of 4096 -> 3584 on masses that no eviction
+// has seen, 451 rows a head, 2.4 GB, 433 us, 5.5 TB/s; fewer rows move where the
+// same tokens have been kept before).  Heads past the registers' length pass
+// over memory in one workgroup each: 2 of 65000 90 us, 8 of them 104.
 template <int NT, int PER, int MODE>
 __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
     constexpr int NW = NT / 64, BPT = kBins / NT;
@@ -411,6 +415,8 @@ struct MassLayout {
 };
 
 // Behind the control block; sized by the capacity, so that it serves every N.
+// The block holds words of the split selection by score, unused here, as
+// bkv_workspace_init clears the whole of it.
 MassLayout mass_layout(const bkv_dims& d) {
     MassLayout m;
     const size_t P = (size_t)d.B * d.Hkv;
