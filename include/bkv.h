@@ -346,8 +346,8 @@ bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes,
  * only pass bkv_validate.  N may be 0 (then every query sees nothing).
  * B * Hq * T < 2^31; T == 0 or B == 0 enqueues nothing.
  * The workspace needs no initialisation and holds nothing between calls; its
- * size covers every N <= N_cap.  mass: whether calls pass a mass; groups and
- * P_cap: those of bkv_attend_shared (0, 0 for bkv_attend).  0 bytes: none is
+ * size covers every N <= N_cap and P <= P_cap.  mass: whether calls pass a mass;
+ * groups and P_cap: those of bkv_attend_shared (0, 0 for bkv_attend).  0 bytes: none is
  * needed, or the arguments are invalid. */
 #define BKV_ATTEND_CAUSAL 1
 size_t bkv_attend_workspace_bytes(const bkv_dims* d, int32_t T, int32_t mass, int32_t groups, int32_t P_cap);
