@@ -171,7 +171,7 @@ struct Span {
 };
 inline bool overlap(const Span& a, const Span& b) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+    return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 // Whether none of the first `written` spans meets any other of the n.
 inline bool apart(const Span* spans, int n, int written) {

@@ -157,3 +157,21 @@ def test_ragged_prompts(N, T, lens, splits, parts, D, dtype):
 ])
 def test_ragged_prompts_of_other_layouts(kw, dtype):
     spread(dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("groups", [0, 2])
+def test_arrays_of_no_tokens_meet_nothing(groups):
+    """With N (and P) 0 nothing of the cache, the prefix or the masses is touched, wherever they lie."""
+    B, H, T, D, cap = 2, 2, 8, 64, 2
+    store = torch.zeros(1 << 16, dtype=torch.bfloat16, device="cuda")
+    out = store[:B * H * T * D].view(B, H, T, D).fill_(1.0)
+    K = store[512:512 + B * H * cap * D].view(B, H, cap, D)  # within out
+    mass = store[256:256 + 2 * B * H * cap].view(torch.float32).view(B, H, cap)
+    q = torch.randn(B, H, T, D, device="cuda").bfloat16()
+    d = bkv.dims(B=B, Hq=H, Hkv=H, D=D, N=0, N_cap=cap, W=0, C=0, budget=1)
+    ws = bkv.attend_workspace(d, T, True, groups, cap if groups else 0)
+    if groups:
+        bkv.attend_shared(d, q, K, K, K, K, out, ws, P=0, mass=mass)
+    else:
+        bkv.attend(d, q, K, K, out, ws, mass=mass)
+    assert not out.float().any()
