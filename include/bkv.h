@@ -347,8 +347,8 @@ bkv_status bkv_append_rows(const bkv_rows* arrays, int32_t n, int32_t row_bytes,
  * B * Hq * T < 2^31; T == 0 or B == 0 enqueues nothing.
  * The workspace needs no initialisation and holds nothing between calls; its
  * size covers every N <= N_cap and P <= P_cap.  mass: whether calls pass a mass;
- * groups and P_cap: those of bkv_attend_shared (0, 0 for bkv_attend).  0 bytes: none is
- * needed, or the arguments are invalid. */
+ * groups and P_cap: those of bkv_attend_shared (0, 0 for bkv_attend).  0 bytes:
+ * none is needed, or the arguments are invalid. */
 #define BKV_ATTEND_CAUSAL 1
 size_t bkv_attend_workspace_bytes(const bkv_dims* d, int32_t T, int32_t mass, int32_t groups, int32_t P_cap);
 bkv_status bkv_attend(const bkv_dims* d, int32_t flags, const void* q, int32_t T, const void* K, const void* V,
@@ -384,8 +384,9 @@ bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, in
  * that tokens appended there start from nothing.  N <= budget changes nothing.
  *   kept    optional [B, Hkv, n] int32 (NULL to skip).
  * K, V, mass, kept and the workspace must not overlap (BKV_ERR_INVALID), but
- * K and V may be one and the same array.  N is the number of tokens of every
- * sequence, as in the other evictions.
+ * K and V may be one and the same array, or each head's tokens of one lie
+ * behind those of the other within its N_cap rows.  N is the number of tokens
+ * of every sequence, as in the other evictions.
  * Workspace: bkv_mass_workspace_bytes(d), which covers every N <= N_cap,
  * initialised by bkv_workspace_init and usable with bkv_device_status. */
 #define BKV_EVICT_FILL 1

@@ -474,13 +474,15 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     if (d->N <= d->budget && !kept) return BKV_OK;
     const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
     const size_t tokens = (size_t)(P - 1) * d->N_cap + d->N;  // of the last head those that are there
-    // K and V may be one array, whose rows then move once more to the same places
-    const Span spans[] = {{K, tokens * rb},
-                          {V == K ? nullptr : V, tokens * rb},
-                          {mass, tokens * sizeof(float)},
-                          {kept, (size_t)P * n * sizeof(int32_t)},
-                          {ws, m.end}};
-    if (!apart(spans, 5, 5)) return BKV_ERR_INVALID;
+    const Span k = {K, tokens * rb}, v = {V, tokens * rb};
+    const Span spans[] = {{mass, tokens * sizeof(float)}, {kept, (size_t)P * n * sizeof(int32_t)}, {ws, m.end}, k, v};
+    if (!apart(spans, 5, 3)) return BKV_ERR_INVALID;
+    // K and V may be one array, whose rows then move once more to the same places,
+    // or take turns, the tokens of one behind the other's in every head's rows
+    const size_t head = (size_t)d->N_cap * rb, used = (size_t)d->N * rb;
+    const uintptr_t k0 = reinterpret_cast<uintptr_t>(K), v0 = reinterpret_cast<uintptr_t>(V);
+    const size_t off = (k0 < v0 ? v0 - k0 : k0 - v0) % head;
+    if (K != V && overlap(k, v) && (off < used || head - off < used)) return BKV_ERR_INVALID;
     if (d->N <= d->budget) {
         const long long total = (long long)P * n;  // at most 2^31
         hipLaunchKernelGGL(mass_identity_kernel, dim3((unsigned)((total + kCopyThreads - 1) / kCopyThreads)),

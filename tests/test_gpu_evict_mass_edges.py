@@ -76,3 +76,23 @@ def test_one_head_past_32_bits_of_bytes():
     # 17 M tokens of one head: rows past 2^32 bytes move into the holes below
     N = (1 << 24) + 5000
     _past_32_bits(1, N, N + 3, N - 3000, True, (0,))
+
+
+@pytest.mark.parametrize("fill", [False, True])
+@pytest.mark.parametrize("Hkv,N,budget", [(2, 700, 600), (3, 5000, 2400), (300, 700, 300)])
+def test_keys_and_values_in_turns(Hkv, N, budget, fill):
+    """One array of 2 N rows a head, its keys first and its values behind them."""
+    say(f"in turns: {Hkv} heads, {N} -> {budget}, fill={fill}")
+    g = torch.Generator().manual_seed(N)
+    KV = torch.randn(Hkv, 2 * N, 64, generator=g).bfloat16()
+    m = masses("sinks", Hkv, 2 * N, g)
+    d = bkv.dims(B=1, Hq=Hkv, Hkv=Hkv, D=64, N=N, N_cap=2 * N, W=8, C=0, budget=budget, n_prefix=2)
+    KVd, md, ws = KV.cuda(), m.cuda(), bkv.mass_workspace(d)
+    kept = torch.empty(1, Hkv, budget, dtype=torch.int32, device="cuda")
+    call = lambda off: bkv.lib().bkv_evict_mass(d, int(fill), KVd.data_ptr(), KVd.data_ptr() + off * 128, md.data_ptr(),  # noqa: E731
+                                                kept.data_ptr(), ws.data_ptr(), ws.nbytes, torch.cuda.current_stream().cuda_stream)
+    for off in (1, N - 1, N + 1):
+        assert call(off) == bkv.ERR_INVALID
+    assert call(N) == bkv.OK and bkv.device_status(ws) == bkv.OK
+    Kr, Vr, mr, kr = attend_ref.evict(KV[:, :N], KV[:, N:], m, N, budget, 8, 2, fill)
+    assert torch.equal(host(kept)[0], kr) and torch.equal(bits(KVd), bits(torch.cat([Kr, Vr], 1))) and torch.equal(bits(md), bits(mr))
