@@ -29,12 +29,12 @@ constexpr int kFewRows = 32;        // rows per unit up to which keys are stream
 // Items of 32 rows and kMinChunk keys up to which a prefix of more rows is
 // streamed all the same, in one launch with the sequences' own caches: its keys
 // are read by every row block, but from L2, and the tiles' launch is spared.  Up
-// to 480 items that is ahead nearly always, from 1088 on it is far behind; in
-// between the number alone does not decide, by up to 14 % either way (us, tiles
+// to 480 items that is ahead nearly always, from 3360 on it is far behind; in
+// between the number alone does not decide, by up to 14 % up to the limit (us, tiles
 // and items: 24 13.7 11.0, 192 17.4 13.5, 256 18.8 14.4, 288 21.8 16.4, 320 18.5
 // 18.9, 432 27.2 25.8, 480 21.0 17.8, 504 17.2 19.6, 576 21.9 22.8, 640 20.1 20.1,
-// 704 22.9 21.8, 792 20.0 20.4, 1008 21.4 24.2, 1024 23.0 24.7, 1088 52.7 68.6, 3360
-// 38 49).
+// 704 22.9 21.8, 792 20.0 20.4, 1008 21.4 24.2, 1024 23.0 24.7, 1088 52.7 68.6, 1344
+// 155 148, 3360 38 49).
 constexpr long long kFewItems = 4 * kCus;
 
 // Workgroups that sum the weights of many rows: where the blocks of keys alone

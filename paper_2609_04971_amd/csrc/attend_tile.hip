@@ -292,7 +292,7 @@ __device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, cons
 // causal queries of 32 heads 265 us (1.03 PFLOP/s of what is seen; the library's
 // product of 8192^3 1.21), and by the exponentials at D 64: 500 queries of 28
 // heads against 24001 keys 100 us (850 TFLOP/s).  With 35 to 56 rows it reads
-// keys and values at 5.3 to 6.0 TB/s.
+// keys and values at 4.8 to 6.0 TB/s.
 template <class E>
 __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     using elem = typename E::elem;
