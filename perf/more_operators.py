@@ -336,7 +336,7 @@ def _own(c, s):
         s["d"] = bkv.dims(B=c["B"], Hq=c.get("Hq", c["Hkv"]), Hkv=c["Hkv"], D=c["D"], N=c["N"], N_cap=c["N"] + c["cap"], W=c.get("W", 0), C=0,
                           budget=c.get("budget", 1), n_prefix=c.get("n_prefix", 0), dtype=c["dtype"])
         if "KC" in s:
-            s["cache"] = bkv.Cache4(s["KC"], s["KS"], s["VC"], s["VS"])
+            s["cache"] = bkv.MxCache(s["KC"], s["KS"], s["VC"], s["VS"])
         if "q" in s:
             s["ws"] = bkv.attend_workspace(s["d"], T=c["T"], mass=bool(c.get("mass")))
         elif c["kind"] == "evict4":
@@ -352,8 +352,8 @@ def run(s):
         at = s["at"] if s["at"] is not None else c["N"] - c["T"]
         if own:
             bkv = _own(c, s)
-            bkv.store4(s["d"], s["K"], s["V"], s["cache"], at)
-            bkv.load4(s["d"], s["cache"], s["k"], s["v"], at)
+            bkv.store_mx(s["d"], s["K"], s["V"], s["cache"], at)
+            bkv.load_mx(s["d"], s["cache"], s["k"], s["v"], at)
         else:
             _plain_store(c, s, s["K"], s["V"], at)
             _plain_load(c, s, at)
@@ -365,8 +365,8 @@ def run(s):
         if own:
             bkv = _own(c, s)
             if n < c["N"]:
-                bkv.store4(s["d"], s["more_K"][t], s["more_V"][t], s["cache"], n)
-            bkv.evict_mass4(s["d"], s["cache"], s["mass"], s["ws"], kept=s["kept"], fill=c["fill"])
+                bkv.store_mx(s["d"], s["more_K"][t], s["more_V"][t], s["cache"], n)
+            bkv.evict_mass_mx(s["d"], s["cache"], s["mass"], s["ws"], kept=s["kept"], fill=c["fill"])
         else:
             if n < c["N"]:
                 _plain_store(c, s, s["more_K"][t], s["more_V"][t], n)
@@ -377,7 +377,7 @@ def run(s):
         (_plain_attend4 if kind == "attend4" else _plain_window)(c, s)
     elif kind == "attend4":
         bkv = _own(c, s)
-        bkv.attend4(s["d"], s["q"], s["cache"], s["out"], s["ws"], lens=s["lens"], lse=s["lse"], mass=s["mass"], causal=c["causal"],
+        bkv.attend_mx(s["d"], s["q"], s["cache"], s["out"], s["ws"], lens=s["lens"], lse=s["lse"], mass=s["mass"], causal=c["causal"],
                     window=c["window"], sinks=c["sinks"])
     else:
         bkv = _own(c, s)
