@@ -2,7 +2,7 @@
 timing and comparing.
 
 The 4-bit form: blocks of 32 coordinates, value = code * 2^e with codes of one sign, two exponent and one mantissa bit
-(0, 0.5, 1, 1.5, 2, 3, 4, 6) and one byte e + 127 a block.  e is the smallest with amax <= 7 * 2^e, in [-125, 125].
+(0, 0.5, 1, 1.5, 2, 3, 4, 6) and one byte e + 127 a block.  e is the smallest with amax <= 7 * 2^e, in [-124, 125].
 
 A case is a dict of plain values; "kind" names the operator:
 
@@ -116,7 +116,7 @@ def _codes(x):
     a = x.float().unflatten(-1, (-1, 32))
     m, k = torch.frexp(a.abs().amax(-1))
     e = torch.where(m <= 0.875, k - 3, k - 2)  # amax = m 2^k with m in [0.5, 1)
-    e = torch.where(m == 0, -125, e).clamp_(-125, 125)
+    e = torch.where(m == 0, -124, e).clamp_(-124, 125)
     y = torch.ldexp(a.abs(), -e.unsqueeze(-1))
     c = (y > 0.25).to(torch.uint8)
     for up, border in ((True, 0.75), (False, 1.25), (True, 1.75), (False, 2.5), (True, 3.5), (False, 5.0)):
@@ -417,8 +417,8 @@ def _nearest(x):
     """Values of x [..., D] in the 4-bit form, in 64 bits: rounded in units of half a code's own binade."""
     a = x.double().unflatten(-1, (-1, 32))
     top = a.abs().amax(-1, keepdim=True)
-    e = torch.ceil(torch.log2(top.clamp_min(1e-300) / 7.0)).clamp(-125, 125)
-    e = torch.where((top <= 7.0 * 2.0 ** (e - 1)) & (e > -125), e - 1, torch.where((top > 7.0 * 2.0 ** e) & (e < 125), e + 1, e))
+    e = torch.ceil(torch.log2(top.clamp_min(1e-300) / 7.0)).clamp(-124, 125)
+    e = torch.where((top <= 7.0 * 2.0 ** (e - 1)) & (e > -124), e - 1, torch.where((top > 7.0 * 2.0 ** e) & (e < 125), e + 1, e))
     y = a / 2.0 ** e
     unit = torch.where(y.abs() < 2, 0.5, torch.where(y.abs() < 4, 1.0, 2.0))
     return ((torch.round(y / unit) * unit).clamp(-6, 6) * 2.0 ** e).flatten(-2)
