@@ -394,6 +394,45 @@ size_t bkv_mass_workspace_bytes(const bkv_dims* d);
 bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, float* mass, int32_t* kept, void* ws,
                           size_t ws_bytes, hipStream_t stream);
 
+/* ---- A cache held in 4 bits ------------------------------------------------------
+ * K and V in a quarter of bf16's bytes and a little: every row of D coordinates
+ * is D/32 blocks of 32, each coordinate a code of 4 bits (bit 3 the sign; 0 to 7
+ * stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6) and each block one byte e + 127; the
+ * coordinate's value is the code's times 2^e.
+ *   K, V    [B, Hkv, N_cap, D/2] codes, coordinate i in byte i / 2, even ones in
+ *           the low four bits.
+ *   KS, VS  [B, Hkv, N_cap, D/32] bytes.
+ * All four 16-byte aligned and apart from one another.  Storing takes for a block
+ * whose largest magnitude is a the smallest e with a <= 7 2^e, at least -124 and
+ * at most 125, and rounds every coordinate over 2^e to the nearest code, ties to
+ * the even one (magnitudes past 6 to 6): a coordinate of 2^e or more is off by at
+ * most a fifth of itself, a smaller one by at most 2^e / 4 (e past -124; e is below
+ * 125 wherever a <= 7 2^125).  Values are exact in bf16.
+ * Rows written otherwise need bytes of 3 to 252; others give unspecified values. */
+typedef struct {
+    uint8_t* K;
+    uint8_t* KS;
+    uint8_t* V;
+    uint8_t* VS;
+} bkv_mx_cache;
+
+/* T rows of every head into the cache: row t of sequence b of k and v [B, Hkv, T,
+ * D] (dtype of the dims) becomes the cache's row first + t, or at[b] + t where
+ * at, optional device [B] int32, is given.  Without it 0 <= first <= N_cap - T
+ * (BKV_ERR_SHAPE); with it first is not used and rows outside of [0, N_cap) are
+ * not stored.  k or v may be NULL: that side is left as it was, and its arrays are
+ * not needed.  Of the dims, B, Hkv, D, N_cap and dtype are used.
+ * B * Hkv * T < 2^31; T == 0 or B == 0 enqueues nothing.  k and v must not overlap
+ * the cache, nor at any of its arrays.  Needs no workspace. */
+bkv_status bkv_store_mx(const bkv_dims* d, const void* k, const void* v, int32_t T, int32_t first, const int32_t* at,
+                        const bkv_mx_cache* cache, hipStream_t stream);
+
+/* The way back: the cache's rows first + t, or at[b] + t, as rows t of k and v
+ * [B, Hkv, T, D], exact.  Rows that the cache has not got are left as they were
+ * in k and v; k or v may be NULL.  Everything else as in bkv_store_mx. */
+bkv_status bkv_load_mx(const bkv_dims* d, const bkv_mx_cache* cache, int32_t T, int32_t first, const int32_t* at, void* k,
+                       void* v, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* bkv_status_string(bkv_status s);
 

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -27,7 +28,7 @@ EXPORTS = ("bkv_validate", "bkv_workspace_bytes", "bkv_workspace_init", "bkv_dev
            "bkv_score_ex", "bkv_evict_ex", "bkv_fps", "bkv_fps_gather", "bkv_status_string",
            "bkv_abi_version", "bkv_compact_fill", "bkv_evict_noalloc", "bkv_append_rows",
            "bkv_attend", "bkv_attend_shared", "bkv_attend_workspace_bytes", "bkv_evict_mass",
-           "bkv_mass_workspace_bytes")
+           "bkv_mass_workspace_bytes", "bkv_store_mx", "bkv_load_mx")
 APPEND_MAX = 4
 SCORE_MEAN, SCORE_CAUSAL = 1, 2
 ATTEND_CAUSAL = 1
@@ -64,6 +65,20 @@ class Rows(ctypes.Structure):
     """One array of append_rows: see bkv_rows."""
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("src_stride", ctypes.c_int64),
                 ("dst_stride", ctypes.c_int64), ("heads", ctypes.c_int64)]
+
+
+class _MxPtrs(ctypes.Structure):
+    """See bkv_mx_cache."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("K", "KS", "V", "VS")]
+
+
+class MxCache(NamedTuple):
+    """A cache held in 4 bits: codes [B,Hkv,N_cap,D/2] and the blocks' bytes
+    [B,Hkv,N_cap,D/32] of K and of V, all uint8."""
+    K: torch.Tensor
+    KS: torch.Tensor
+    V: torch.Tensor
+    VS: torch.Tensor
 
 
 _APPEND = [Rows * n for n in range(APPEND_MAX + 1)]
@@ -105,6 +120,8 @@ _SIGS = {
                           ctypes.c_int),
     "bkv_mass_workspace_bytes": ([_D], _S),
     "bkv_evict_mass": ([_D, _I, _P, _P, _P, _P, _P, _S, _P], ctypes.c_int),
+    "bkv_store_mx": ([_D, _P, _P, _I, _I, _P, ctypes.POINTER(_MxPtrs), _P], ctypes.c_int),
+    "bkv_load_mx": ([_D, ctypes.POINTER(_MxPtrs), _I, _I, _P, _P, _P, _P], ctypes.c_int),
     "bkv_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "bkv_abi_version": ([], ctypes.c_int32),
 }
@@ -413,6 +430,56 @@ def evict_mass(d: Dims, K, V, mass, ws, kept=None, fill: bool = False):
     st = lib().bkv_evict_mass(ctypes.byref(d), EVICT_FILL if fill else 0, kp, vp, mp, op, wp, wn,
                               torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_evict_mass")
+
+
+# ---- the cache in 4 bits ----------------------------------------------------------
+def mx_cache(d: Dims, device="cuda") -> MxCache:
+    """Allocate (through torch) a 4-bit cache of `d`; rows hold nothing until they
+    are stored."""
+    return MxCache(*(torch.empty(d.B, d.Hkv, d.N_cap, n, dtype=torch.uint8, device=device)
+                     for n in (d.D // 2, d.D // 32) * 2))
+
+
+def _arg_mx(d, cache, dev):
+    if not isinstance(cache, MxCache):
+        raise ValueError("cache must be an MxCache")
+    p = _MxPtrs()
+    for name, n in (("K", d.D // 2), ("KS", d.D // 32), ("V", d.D // 2), ("VS", d.D // 32)):
+        setattr(p, name, _arg(getattr(cache, name), (d.B, d.Hkv, d.N_cap, n), torch.uint8, "cache." + name, dev))
+    return p
+
+
+def _mx_args(d, k, v, cache, at):
+    t = k if k is not None else v
+    if t is None:
+        raise ValueError("k or v is required")
+    dev = _device_of(t, "k" if k is not None else "v")
+    if t.dim() != 4:
+        raise ValueError("k and v must be tensors [B, Hkv, T, D]")
+    T, dt = t.shape[2], _tdtype(d)
+    shape = (d.B, d.Hkv, T, d.D)
+    kp = None if k is None else _arg(k, shape, dt, "k", dev)
+    vp = None if v is None else _arg(v, shape, dt, "v", dev)
+    if isinstance(at, torch.Tensor):
+        first, ap = 0, _arg(at, (d.B,), torch.int32, "at", dev)
+    else:
+        first, ap = int(at), None
+    return kp, vp, T, first, ap, _arg_mx(d, cache, dev), torch._C._cuda_getCurrentRawStream(dev)
+
+
+def store_mx(d: Dims, k, v, cache: MxCache, at=0):
+    """Rows k, v [B,Hkv,T,D] into rows at.. of the 4-bit cache; at: a position, or
+    [B] int32 with one for each sequence (rows outside of the cache are not
+    stored).  k or v may be None: that side is left as it was."""
+    kp, vp, T, first, ap, cp, s = _mx_args(d, k, v, cache, at)
+    _check(lib().bkv_store_mx(ctypes.byref(d), kp, vp, T, first, ap, ctypes.byref(cp), s), "bkv_store_mx")
+
+
+def load_mx(d: Dims, cache: MxCache, k, v, at=0):
+    """The values of rows at.. of the 4-bit cache into k, v [B,Hkv,T,D], exact;
+    k or v may be None."""
+    kp, vp, T, first, ap, cp, s = _mx_args(d, k, v, cache, at)
+    _check(lib().bkv_load_mx(ctypes.byref(d), ctypes.byref(cp), T, first, ap, kp, vp, s), "bkv_load_mx")
 
 
 # ---- appending a step's rows -------------------------------------------------------

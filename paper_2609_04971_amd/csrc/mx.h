@@ -1,0 +1,50 @@
+// The 4-bit cache: blocks of 32 coordinates of a row, each coordinate a code of
+// one sign, two exponent and one mantissa bit (0, 0.5, 1, 1.5, 2, 3, 4, 6), and
+// one byte e + 127 a block; a value is code 2^e.  Coordinate i of a row is in byte
+// i / 2, even ones in its low half.  gfx950 turns two codes into bf16 or fp32
+// values, times the power of two, in one instruction, and every value is exact
+// in either (two significant bits).
+#pragma once
+
+#include "device_common.h"
+
+namespace bkv {
+namespace mx {
+
+constexpr int kBlock = 32;
+// e + 127: subnormal coordinates fall below half of the smallest code, and the
+// largest code stays finite.
+constexpr int kLeast = 3, kMost = 252;
+
+template <int D>
+struct Row {
+    static constexpr int kCodes = D / 2;        // bytes
+    static constexpr int kScales = D / kBlock;  // bytes
+};
+
+// 2^e of a block's byte.
+__device__ __forceinline__ float scale(unsigned byte) { return __uint_as_float(byte << 23); }
+
+// The byte of a block whose largest magnitude is `top`: the smallest e with top
+// <= 7 2^e.  7 rounds to 6, no worse than the half step between 4 and 6, and
+// from there on the next power is the closer one.
+__device__ __forceinline__ unsigned scale_byte(float top) {
+    const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 2;
+    return (unsigned)min(max(e, kLeast), kMost);
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Values of byte B of `codes`: two bf16 in a word, or two floats.
+template <int B>
+__device__ __forceinline__ unsigned pair_bf16(unsigned codes, float scale) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, B));
+}
+template <int B>
+__device__ __forceinline__ f32x2 pair_f32(unsigned codes, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, B);
+}
+
+}  // namespace mx
+}  // namespace bkv
