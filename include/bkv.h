@@ -371,6 +371,17 @@ bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, in
                              const void* V, const int32_t* lens, float scale, void* out, float* lse, float* mass,
                              void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* bkv_attend where a query sees its last `window` tokens and the first `sinks`
+ * ones: query t, the cache's token p = len - T + t (the T queries are its newest
+ * tokens, oldest first), sees the tokens j <= p with j > p - window or j < sinks.
+ * Only those are read, up to whole groups of 64.  window >= 1 and sinks >= 0
+ * (BKV_ERR_SHAPE).  Everything else as in bkv_attend, the workspace too (that of
+ * bkv_attend_workspace_bytes(d, T, 0, 0, 0) for every window and sinks); weights
+ * are not summed. */
+bkv_status bkv_attend_window(const bkv_dims* d, const void* q, int32_t T, const void* K, const void* V, int32_t window,
+                             int32_t sinks, const int32_t* lens, float scale, void* out, float* lse, void* ws,
+                             size_t ws_bytes, hipStream_t stream);
+
 /* Eviction by accumulated attention weight: bkv_topk's rule on mass [B, Hkv,
  * N_cap] in the place of the scores (the first n_prefix and the last W tokens,
  * then the largest masses, ties to the lower index, -0 equal to +0; a NaN of
@@ -432,6 +443,18 @@ bkv_status bkv_store_mx(const bkv_dims* d, const void* k, const void* v, int32_t
  * in k and v; k or v may be NULL.  Everything else as in bkv_store_mx. */
 bkv_status bkv_load_mx(const bkv_dims* d, const bkv_mx_cache* cache, int32_t T, int32_t first, const int32_t* at, void* k,
                        void* v, hipStream_t stream);
+
+/* bkv_attend (flags, lens, lse, mass, scale, workspace and all else as there) over
+ * a 4-bit cache, with the keys and values that its rows stand for; dtype of the
+ * dims: that of q and out, bf16 or fp32.  Products and weights are rounded as on a
+ * plain cache of that type.
+ *   window  0: none, and sinks is not used.  >= 1: queries see what they see in
+ *           bkv_attend_window; then T > 1 needs BKV_ATTEND_CAUSAL, and mass has
+ *           to be NULL (BKV_ERR_INVALID).
+ * The cache may be NULL when N is 0. */
+bkv_status bkv_attend_mx(const bkv_dims* d, int32_t flags, const void* q, int32_t T, const bkv_mx_cache* cache,
+                         int32_t window, int32_t sinks, const int32_t* lens, float scale, void* out, float* lse,
+                         float* mass, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Static description of a status code. */
 const char* bkv_status_string(bkv_status s);

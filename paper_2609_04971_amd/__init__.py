@@ -28,7 +28,8 @@ EXPORTS = ("bkv_validate", "bkv_workspace_bytes", "bkv_workspace_init", "bkv_dev
            "bkv_score_ex", "bkv_evict_ex", "bkv_fps", "bkv_fps_gather", "bkv_status_string",
            "bkv_abi_version", "bkv_compact_fill", "bkv_evict_noalloc", "bkv_append_rows",
            "bkv_attend", "bkv_attend_shared", "bkv_attend_workspace_bytes", "bkv_evict_mass",
-           "bkv_mass_workspace_bytes", "bkv_store_mx", "bkv_load_mx")
+           "bkv_mass_workspace_bytes", "bkv_store_mx", "bkv_load_mx", "bkv_attend_mx",
+           "bkv_attend_window")
 APPEND_MAX = 4
 SCORE_MEAN, SCORE_CAUSAL = 1, 2
 ATTEND_CAUSAL = 1
@@ -122,6 +123,9 @@ _SIGS = {
     "bkv_evict_mass": ([_D, _I, _P, _P, _P, _P, _P, _S, _P], ctypes.c_int),
     "bkv_store_mx": ([_D, _P, _P, _I, _I, _P, ctypes.POINTER(_MxPtrs), _P], ctypes.c_int),
     "bkv_load_mx": ([_D, ctypes.POINTER(_MxPtrs), _I, _I, _P, _P, _P, _P], ctypes.c_int),
+    "bkv_attend_mx": ([_D, _I, _P, _I, ctypes.POINTER(_MxPtrs), _I, _I, _P, ctypes.c_float, _P, _P, _P, _P, _S, _P],
+                      ctypes.c_int),
+    "bkv_attend_window": ([_D, _P, _I, _P, _P, _I, _I, _P, ctypes.c_float, _P, _P, _P, _S, _P], ctypes.c_int),
     "bkv_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "bkv_abi_version": ([], ctypes.c_int32),
 }
@@ -362,17 +366,24 @@ def attend_workspace(d: Dims, T: int = 1, mass: bool = False, groups: int = 0, P
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
-def _attend_args(d, q, K, V, out, lens, lse, mass, dev):
+def _attend_rows(d, q, out, lens, lse, mass, dev):
+    """What every attention takes beside its cache: T, the rows' type, and the addresses."""
     if q.dim() != 4:
         raise ValueError("q must be a tensor [B, Hq, T, D]")
     B, Hq, T, D = rows = q.shape
-    dt, cache = _tdtype(d), (d.B, d.Hkv, d.N_cap, d.D)
+    dt = _tdtype(d)
     if (B, Hq, D) != (d.B, d.Hq, d.D):
         raise ValueError(f"q must have shape {(d.B, d.Hq, T, d.D)}, got {tuple(q.shape)}")
-    return T, dt, (_arg(q, rows, dt, "q", dev), _arg(K, cache, dt, "K", dev), _arg(V, cache, dt, "V", dev),
-                   None if lens is None else _arg(lens, (B,), torch.int32, "lens", dev), _arg(out, rows, dt, "out", dev),
+    return T, dt, (_arg(q, rows, dt, "q", dev), None if lens is None else _arg(lens, (B,), torch.int32, "lens", dev),
+                   _arg(out, rows, dt, "out", dev),
                    None if lse is None else _arg(lse, (B, Hq, T), torch.float32, "lse", dev),
-                   None if mass is None else _arg(mass, cache[:3], torch.float32, "mass", dev))
+                   None if mass is None else _arg(mass, (B, d.Hkv, d.N_cap), torch.float32, "mass", dev))
+
+
+def _attend_args(d, q, K, V, out, lens, lse, mass, dev):
+    T, dt, (qp, lp, op, ep, mp) = _attend_rows(d, q, out, lens, lse, mass, dev)
+    cache = (d.B, d.Hkv, d.N_cap, d.D)
+    return T, dt, (qp, _arg(K, cache, dt, "K", dev), _arg(V, cache, dt, "V", dev), lp, op, ep, mp)
 
 
 def attend(d: Dims, q, K, V, out, ws, lens=None, lse=None, mass=None, scale: float = 0.0, causal: bool = False):
@@ -406,6 +417,18 @@ def attend_shared(d: Dims, q, PK, PV, K, V, out, ws, P: int | None = None, p_len
                                  P_cap if P is None else int(P), P_cap, pl, kp, vp, lp, scale, op, ep, mp, wp, wn,
                                  torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_shared")
+
+
+def attend_window(d: Dims, q, K, V, out, ws, window: int, sinks: int = 0, lens=None, lse=None, scale: float = 0.0):
+    """attend() where query t, the cache's token p = len - T + t, sees the tokens
+    j <= p with j > p - window or j < sinks.  The workspace is that of
+    attend_workspace(d, T)."""
+    dev = _device_of(q, "q")
+    T, _, (qp, kp, vp, lp, op, ep, _) = _attend_args(d, q, K, V, out, lens, lse, None, dev)
+    wp, wn = _arg_ws(ws, dev)
+    st = lib().bkv_attend_window(ctypes.byref(d), qp, T, kp, vp, window, sinks, lp, scale, op, ep, wp, wn,
+                                 torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "bkv_attend_window")
 
 
 def mass_workspace(d: Dims, device="cuda") -> torch.Tensor:
@@ -480,6 +503,19 @@ def load_mx(d: Dims, cache: MxCache, k, v, at=0):
     k or v may be None."""
     kp, vp, T, first, ap, cp, s = _mx_args(d, k, v, cache, at)
     _check(lib().bkv_load_mx(ctypes.byref(d), ctypes.byref(cp), T, first, ap, kp, vp, s), "bkv_load_mx")
+
+
+def attend_mx(d: Dims, q, cache: MxCache, out, ws, lens=None, lse=None, mass=None, scale: float = 0.0,
+              causal: bool = False, window: int = 0, sinks: int = 0):
+    """attend() over a 4-bit cache; q and out have the dims' type.  window > 0: as
+    attend_window() (then causal, and without mass)."""
+    dev = _device_of(q, "q")
+    T, _, (qp, lp, op, ep, mp) = _attend_rows(d, q, out, lens, lse, mass, dev)
+    cp = _arg_mx(d, cache, dev)
+    wp, wn = _arg_ws(ws, dev)
+    st = lib().bkv_attend_mx(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, ctypes.byref(cp), window, sinks, lp, scale,
+                             op, ep, mp, wp, wn, torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "bkv_attend_mx")
 
 
 # ---- appending a step's rows -------------------------------------------------------

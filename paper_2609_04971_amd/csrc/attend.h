@@ -44,6 +44,9 @@ struct Args {
     int rows;             // B * Hq * T
     int ns;               // partials per row; 1: the outputs are written directly
     float scale2;         // scale * log2(e)
+    const uint8_t* KS;    // a 4-bit cache's bytes (seg[1], whose K and V are then its codes)
+    const uint8_t* VS;
+    int window, sinks;    // windowed kernels: a query sees its last `window` keys and the first `sinks`
 };
 
 // How a call is cut.  N and P choose between kernels, row blocks, splits and
@@ -60,7 +63,13 @@ struct Plan {
     int parts;                // or: workgroups that share a block of keys
     size_t part_o, part_ml, row_lse2, logits, parts_at, end;
 };
-Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int P, int P_cap);
+struct Shape {  // what a call is cut by
+    bool causal, mass;
+    int groups, P, P_cap;
+    int window, sinks;  // window 0: none
+    bool mx;            // a 4-bit cache
+};
+Plan make_plan(const bkv_dims& d, int T, const Shape& c);
 
 // A row of a segment's unit: which query it is.
 struct Row {
@@ -134,6 +143,24 @@ __device__ __forceinline__ int turning_unit(const Segment& sg, int item, int Hkv
     const int unit = item % sg.units;
     return sg.lens && sg.units > Hkv ? (unit + item / sg.units / kTurns) % sg.units : unit;
 }
+
+// The keys that the rows of an item see through their windows, put end to end:
+// the first ones, up to a whole number of groups of KG keys, and those from the
+// first row's window on; place v is key v + (v < head ? 0 : skip).
+struct Walk {
+    int head, skip, n;  // n: places
+    // least, most: keys that the item's first and last rows see up to
+    template <int KG>
+    __device__ __forceinline__ static Walk over(const Args& a, int least, int most) {
+        Walk w;
+        const int from = max(least - a.window, 0) / KG * KG;
+        w.head = (int)min(((long long)a.sinks + KG - 1) / KG * KG, (long long)from);
+        w.skip = from - w.head;
+        w.n = max(most - w.skip, 0);
+        return w;
+    }
+    __device__ __forceinline__ int key(int v) const { return v < head ? v : v + skip; }
+};
 
 // What a row's sums come to.  z is 0 for a row that saw nothing and at least 1
 // otherwise (or NaN, where it saw one, and then so are its results).
@@ -218,5 +245,11 @@ hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipS
 // And of more rows, added to the mass, or, where parts > 1, to part [parts][units][n], whose sums the third adds.
 hipError_t launch_attend_tile_mass(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s);
 hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s);
+
+// The same on a 4-bit cache (dtype: the queries').
+hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, bool wide, hipStream_t s);
+hipError_t launch_attend_tile_mx(const attend::Args& a, const attend::Segment& sg, hipStream_t s);
+hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s);
+hipError_t launch_attend_tile_mass_mx(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s);
 
 }  // namespace bkv

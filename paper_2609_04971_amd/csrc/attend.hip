@@ -215,19 +215,7 @@ hipError_t launch_attend_join(const attend::Args& a, int dtype, hipStream_t s) {
 }
 hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipStream_t s) {
     using namespace attend;
-    const dim3 grid((unsigned)(a.seg[1].units * ns)), block(kThreads);
-    if (a.R <= 64) {
-        if (a.D == 128)
-            hipLaunchKernelGGL((row_mass_kernel<128, 4>), grid, block, 0, s, a, chunk);
-        else
-            hipLaunchKernelGGL((row_mass_kernel<64, 4>), grid, block, 0, s, a, chunk);
-    } else {
-        if (a.D == 128)
-            hipLaunchKernelGGL((row_mass_kernel<128, 6>), grid, block, 0, s, a, chunk);
-        else
-            hipLaunchKernelGGL((row_mass_kernel<64, 6>), grid, block, 0, s, a, chunk);
-    }
-    return hipGetLastError();
+    return a.D == 128 ? row_mass<Bf16<128>, 128>(a, ns, chunk, s) : row_mass<Bf16<64>, 64>(a, ns, chunk, s);
 }
 hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s) {
     using namespace attend;

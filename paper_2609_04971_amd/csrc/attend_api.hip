@@ -1,9 +1,11 @@
 // Entry points of the attention over the cache (bkv_attend,
-// bkv_attend_shared): argument checks, how the work is cut, the launches.
+// bkv_attend_shared, bkv_attend_window, bkv_attend_mx): argument checks, how the
+// work is cut, the launches.
 #include <math.h>
 #include <string.h>
 
 #include "attend.h"
+#include "mx.h"
 
 namespace bkv {
 namespace attend {
@@ -128,9 +130,19 @@ void cut(int n, int ns, int* out_ns, int* chunk) {
 }
 }  // namespace
 
-Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int P, int P_cap) {
+// Places of the longest walk of an item of rb rows: the first keys and those of
+// the rows' windows, each up to a whole number of tiles.
+int walk_places(const bkv_dims& d, int rb, const Shape& c) {
+    const long long kTile = 64, G = d.Hq / d.Hkv;
+    const long long n = (long long)up((size_t)c.sinks, kTile) + c.window + (rb - 1) / G + 1 + kTile;
+    return (int)(n < d.N ? n : d.N);
+}
+
+Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
     Plan p;
     memset(&p, 0, sizeof p);
+    const bool mass = c.mass;
+    const int groups = c.groups, P = c.P, P_cap = c.P_cap;
     const long long G = d.Hq / d.Hkv, R = G * T;
     const long long rows = (long long)d.B * d.Hq * T;
     const long long pre_rows = groups > 0 ? d.B / groups * R : 0;
@@ -144,6 +156,7 @@ Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
     const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
+    const int N = c.window > 0 ? walk_places(d, own_rb, c) : d.N;  // keys, or places, of an item
     // room for every N and P within the capacities: P decides between the kernels
     // and so the size of the row blocks, and the splits are most with the fewest items
     const int widest = p.own_tile ? 128 : 32;
@@ -151,21 +164,21 @@ Plan make_plan(const bkv_dims& d, int T, bool causal, bool mass, int groups, int
     if (groups > 0) p.ns_room += most_splits(pre_units * ((pre_rows + 127) / 128), P_cap);
     int own_ns, pre_ns = 1;
     if (groups > 0 && P > 0 && !p.own_tile && !p.pre_tile) {  // one launch takes both
-        const long long all = own * d.N + pre * P;
-        own_ns = shared_splits(own, d.N, all);
+        const long long all = own * N + pre * P;
+        own_ns = shared_splits(own, N, all);
         pre_ns = shared_splits(pre, P, all);
     } else {
         // a short cache goes in one piece: joining splits would be a launch of
         // its own.  Not by the mass: outputs do not depend on whether it is asked for
         const bool whole = groups == 0 && !p.own_tile &&
-                           (long long)d.N * d.D * (d.dtype == BKV_BF16 ? 2 : 4) <= kWhole;
-        const bool prompt = p.own_tile && causal && T <= d.N && T > d.N / 5;
+                           (long long)N * (c.mx ? d.D / 2 + d.D / mx::kBlock : d.D * (d.dtype == BKV_BF16 ? 2 : 4)) <= kWhole;
+        const bool prompt = p.own_tile && c.causal && c.window == 0 && T <= N && T > N / 5;
         own_ns = whole    ? 1
-                 : prompt ? prompt_splits(own, d.N, T, rows, d.D)
-                          : best_splits(p.own_tile, own, d.N, rows, d.D);
+                 : prompt ? prompt_splits(own, N, T, rows, d.D)
+                          : best_splits(p.own_tile, own, N, rows, d.D);
         if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile, pre, P, rows, d.D);
     }
-    cut(d.N, own_ns, &p.own_ns, &p.own_chunk);
+    cut(N, own_ns, &p.own_ns, &p.own_chunk);
     if (groups > 0 && P > 0) cut(P, pre_ns, &p.pre_ns, &p.pre_chunk);
     p.keep = mass && R <= kFewRows;
     if (mass && !p.keep && tiles && R <= kRegRows)
@@ -219,32 +232,61 @@ bkv_status check_shape(const bkv_dims* d, int32_t T, int32_t groups, int32_t P, 
     return BKV_OK;
 }
 
-bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32_t groups, const void* PK,
-               const void* PV, int32_t P, int32_t P_cap, const int32_t* p_lens, const void* K, const void* V,
-               const int32_t* lens, float scale, void* out, float* lse, float* mass, void* ws, size_t ws_bytes,
-               hipStream_t stream) {
+// What a call of any entry point passes; zero is what it has not.
+struct Call {
+    int32_t flags;
+    const void* q;
+    int32_t T, groups;
+    const void *PK, *PV;
+    int32_t P, P_cap;
+    const int32_t* p_lens;
+    const void *K, *V;  // a 4-bit cache's codes where mx
+    bool mx;
+    const uint8_t *KS, *VS;
+    int32_t window, sinks;
+    const int32_t* lens;
+    float scale;
+    void* out;
+    float *lse, *mass;
+    void* ws;
+    size_t ws_bytes;
+};
+
+bkv_status run(const bkv_dims* d, const Call& c, hipStream_t stream) {
+    const int32_t flags = c.flags, T = c.T, groups = c.groups, P = c.P, P_cap = c.P_cap, window = c.window;
+    const void *q = c.q, *PK = c.PK, *PV = c.PV, *K = c.K, *V = c.V;
+    const int32_t *lens = c.lens, *p_lens = c.p_lens;
+    const float scale = c.scale;
+    void *out = c.out, *ws = c.ws;
+    float *lse = c.lse, *mass = c.mass;
+    const size_t ws_bytes = c.ws_bytes;
     if (flags & ~BKV_ATTEND_CAUSAL) return BKV_ERR_INVALID;
     const bkv_status st = check_shape(d, T, groups, P, P_cap);
     if (st != BKV_OK) return st;
+    if (window < 0 || (window > 0 && c.sinks < 0)) return BKV_ERR_SHAPE;
+    // a window counts back from the query's own token; its weights are not summed
+    if (window > 0 && (mass || (T > 1 && !(flags & BKV_ATTEND_CAUSAL)))) return BKV_ERR_INVALID;
     if (d->B == 0 || T == 0) return BKV_OK;
     if (!q || !out || !aligned(q) || !aligned(out)) return BKV_ERR_INVALID;
     if (d->N > 0 && (!K || !V || !aligned(K) || !aligned(V))) return BKV_ERR_INVALID;
+    if (c.mx && d->N > 0 && (!c.KS || !c.VS || !aligned(c.KS) || !aligned(c.VS))) return BKV_ERR_INVALID;
     if (groups > 0 && P > 0 && (!PK || !PV || !aligned(PK) || !aligned(PV))) return BKV_ERR_INVALID;
     const float scale2 = (scale == 0.0f ? 1.0f / sqrtf((float)d->D) : scale) * 1.4426950408889634f;
     if (!(scale >= 0.0f) || isinf(scale2)) return BKV_ERR_INVALID;  // 0 times infinity would be a NaN
-    const Plan p = make_plan(*d, T, flags & BKV_ATTEND_CAUSAL, mass != nullptr, groups, P, P_cap);
+    const Plan p = make_plan(*d, T, {(flags & BKV_ATTEND_CAUSAL) != 0, mass != nullptr, groups, P, P_cap, window, c.sinks, c.mx});
     if (p.end > 0 && (!ws || ws_bytes < p.end || !aligned(ws))) return BKV_ERR_WORKSPACE;
     if (p.own_ns + p.pre_ns > p.ns_room) return BKV_ERR_WORKSPACE;  // (the room covers every N and P)
     // what is written, then what is only read; of the last head the tokens that are there
-    const size_t row = (size_t)d->D * (d->dtype == BKV_BF16 ? 2 : 4), queries = (size_t)d->B * d->Hq * T;
+    const size_t row = (size_t)d->D * (d->dtype == BKV_BF16 ? 2 : 4), cache_row = c.mx ? (size_t)d->D / 2 : row, queries = (size_t)d->B * d->Hq * T;
     auto tokens = [](size_t units, size_t n, size_t cap) { return n > 0 ? (units - 1) * cap + n : 0; };
     const size_t own_tokens = tokens((size_t)d->B * d->Hkv, d->N, d->N_cap);
     const size_t pre_tokens = groups > 0 ? tokens((size_t)groups * d->Hkv, P, P_cap) : 0;
     const Span spans[] = {{out, queries * row},        {lse, queries * sizeof(float)}, {mass, own_tokens * sizeof(float)},
-                          {ws, p.end},                 {q, queries * row},             {K, own_tokens * row},
-                          {V, own_tokens * row},       {PK, pre_tokens * row},         {PV, pre_tokens * row},
-                          {lens, d->B * sizeof(int32_t)}, {p_lens, groups * sizeof(int32_t)}};
-    if (!apart(spans, 11, 4)) return BKV_ERR_INVALID;
+                          {ws, p.end},                 {q, queries * row},             {K, own_tokens * cache_row},
+                          {V, own_tokens * cache_row}, {PK, pre_tokens * row},         {PV, pre_tokens * row},
+                          {lens, d->B * sizeof(int32_t)}, {p_lens, groups * sizeof(int32_t)},
+                          {c.KS, own_tokens * (d->D / mx::kBlock)}, {c.VS, own_tokens * (d->D / mx::kBlock)}};
+    if (!apart(spans, 13, 4)) return BKV_ERR_INVALID;
     char* w = static_cast<char*>(ws);
     Args a;
     memset(&a, 0, sizeof a);
@@ -261,6 +303,10 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     a.lse = lse;
     a.mass = mass;
     a.scale2 = scale2;
+    a.KS = c.KS;
+    a.VS = c.VS;
+    a.window = window;
+    a.sinks = c.sinks;
     Segment& own = a.seg[1];
     own.K = K;
     own.V = V;
@@ -306,17 +352,21 @@ bkv_status run(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32
     if (p.keep && stream_lds(a) > kLdsRoom) a.keep = kKeepStore;
     if (join_grid(a).blocks > kMaxBlocks) return BKV_ERR_SHAPE;
     if (p.pre_tile && launch_attend_tile(a, pre, stream) != hipSuccess) return BKV_ERR_HIP;
-    if (p.own_tile && launch_attend_tile(a, own, stream) != hipSuccess) return BKV_ERR_HIP;
+    const auto tile = c.mx ? launch_attend_tile_mx : launch_attend_tile;
+    if (p.own_tile && tile(a, own, stream) != hipSuccess) return BKV_ERR_HIP;
     if (!p.own_tile) {  // rows of the prefix are no fewer than a sequence's own
         a.items0 = p.pre_tile ? 0 : (int)items0;
-        if (launch_attend_stream(a, d->dtype, p.wide, stream) != hipSuccess) return BKV_ERR_HIP;
+        const auto run_stream = c.mx ? launch_attend_stream_mx : launch_attend_stream;
+        if (run_stream(a, d->dtype, p.wide, stream) != hipSuccess) return BKV_ERR_HIP;
     }
     if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
     if (p.mass_ns > 0 && d->N > 0) {
-        if (launch_attend_row_mass(a, p.mass_ns, p.mass_chunk, stream) != hipSuccess) return BKV_ERR_HIP;
+        const auto row_mass = c.mx ? launch_attend_row_mass_mx : launch_attend_row_mass;
+        if (row_mass(a, p.mass_ns, p.mass_chunk, stream) != hipSuccess) return BKV_ERR_HIP;
     } else if (mass && !p.keep && d->N > 0) {
         float* part = reinterpret_cast<float*>(w + p.parts_at);
-        if (launch_attend_tile_mass(a, d->dtype, part, p.parts, stream) != hipSuccess) return BKV_ERR_HIP;
+        const auto tile_mass = c.mx ? launch_attend_tile_mass_mx : launch_attend_tile_mass;
+        if (tile_mass(a, d->dtype, part, p.parts, stream) != hipSuccess) return BKV_ERR_HIP;
         if (p.parts > 1 && launch_attend_add_parts(a, part, p.parts, stream) != hipSuccess) return BKV_ERR_HIP;
     }
     return BKV_OK;
@@ -328,14 +378,26 @@ extern "C" {
 
 size_t bkv_attend_workspace_bytes(const bkv_dims* d, int32_t T, int32_t mass, int32_t groups, int32_t P_cap) {
     if (check_shape(d, T, groups, 0, P_cap) != BKV_OK || d->B == 0 || T == 0) return 0;
-    return make_plan(*d, T, false, mass != 0, groups, 0, P_cap).end;
+    return make_plan(*d, T, {false, mass != 0, groups, 0, P_cap, 0, 0, false}).end;
 }
 
 bkv_status bkv_attend(const bkv_dims* d, int32_t flags, const void* q, int32_t T, const void* K, const void* V,
                       const int32_t* lens, float scale, void* out, float* lse, float* mass, void* ws, size_t ws_bytes,
                       hipStream_t stream) {
-    return run(d, flags, q, T, 0, nullptr, nullptr, 0, 0, nullptr, K, V, lens, scale, out, lse, mass, ws, ws_bytes,
-               stream);
+    Call c{};
+    c.flags = flags;
+    c.q = q;
+    c.T = T;
+    c.K = K;
+    c.V = V;
+    c.lens = lens;
+    c.scale = scale;
+    c.out = out;
+    c.lse = lse;
+    c.mass = mass;
+    c.ws = ws;
+    c.ws_bytes = ws_bytes;
+    return run(d, c, stream);
 }
 
 bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, int32_t T, int32_t groups, const void* PK,
@@ -343,8 +405,73 @@ bkv_status bkv_attend_shared(const bkv_dims* d, int32_t flags, const void* q, in
                              const void* V, const int32_t* lens, float scale, void* out, float* lse, float* mass,
                              void* ws, size_t ws_bytes, hipStream_t stream) {
     if (groups < 1) return d ? BKV_ERR_SHAPE : BKV_ERR_INVALID;
-    return run(d, flags, q, T, groups, PK, PV, P, P_cap, p_lens, K, V, lens, scale, out, lse, mass, ws, ws_bytes,
-               stream);
+    Call c{};
+    c.flags = flags;
+    c.q = q;
+    c.T = T;
+    c.groups = groups;
+    c.PK = PK;
+    c.PV = PV;
+    c.P = P;
+    c.P_cap = P_cap;
+    c.p_lens = p_lens;
+    c.K = K;
+    c.V = V;
+    c.lens = lens;
+    c.scale = scale;
+    c.out = out;
+    c.lse = lse;
+    c.mass = mass;
+    c.ws = ws;
+    c.ws_bytes = ws_bytes;
+    return run(d, c, stream);
+}
+
+bkv_status bkv_attend_window(const bkv_dims* d, const void* q, int32_t T, const void* K, const void* V, int32_t window,
+                             int32_t sinks, const int32_t* lens, float scale, void* out, float* lse, void* ws,
+                             size_t ws_bytes, hipStream_t stream) {
+    if (window < 1) return d ? BKV_ERR_SHAPE : BKV_ERR_INVALID;
+    Call c{};
+    c.flags = BKV_ATTEND_CAUSAL;
+    c.q = q;
+    c.T = T;
+    c.K = K;
+    c.V = V;
+    c.window = window;
+    c.sinks = sinks;
+    c.lens = lens;
+    c.scale = scale;
+    c.out = out;
+    c.lse = lse;
+    c.ws = ws;
+    c.ws_bytes = ws_bytes;
+    return run(d, c, stream);
+}
+
+bkv_status bkv_attend_mx(const bkv_dims* d, int32_t flags, const void* q, int32_t T, const bkv_mx_cache* cache,
+                         int32_t window, int32_t sinks, const int32_t* lens, float scale, void* out, float* lse,
+                         float* mass, void* ws, size_t ws_bytes, hipStream_t stream) {
+    Call c{};
+    c.flags = flags;
+    c.q = q;
+    c.T = T;
+    c.mx = true;
+    if (cache) {
+        c.K = cache->K;
+        c.V = cache->V;
+        c.KS = cache->KS;
+        c.VS = cache->VS;
+    }
+    c.window = window;
+    c.sinks = sinks;
+    c.lens = lens;
+    c.scale = scale;
+    c.out = out;
+    c.lse = lse;
+    c.mass = mass;
+    c.ws = ws;
+    c.ws_bytes = ws_bytes;
+    return run(d, c, stream);
 }
 
 }  // extern "C"

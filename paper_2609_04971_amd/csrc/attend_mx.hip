@@ -1,0 +1,170 @@
+// Attention over a 4-bit cache for gfx950: the streaming kernel's types and its
+// launches, and the weights' sums of rows that stay in registers.
+//
+// A group's codes and bytes are what is streamed; they become bf16 (or, for fp32
+// queries, fp32) operands in registers, exactly, and from there on the products
+// are those of a plain cache.  The contraction over a row's coordinates may run
+// in any order that keys and queries share: lane group g takes the D/4 that
+// follow one another from (D/4) g on, so that a lane's part of a key is one load
+// and lies in one block.
+#include "attend_stream.h"
+#include "mx.h"
+
+namespace bkv {
+namespace attend {
+namespace {
+
+struct MxSrc {
+    const uint8_t* c;
+    const uint8_t* s;
+};
+template <int D>
+__device__ __forceinline__ MxSrc mx_rows(const void* codes, const uint8_t* bytes, long long row) {
+    return {static_cast<const uint8_t*>(codes) + row * mx::Row<D>::kCodes, bytes + row * mx::Row<D>::kScales};
+}
+
+// What the two types share: a lane's part of one key, kW words of codes, and of
+// one value row, D/16 coordinates.
+template <int D>
+struct MxRows {
+    static constexpr int kW = D / 32, kDV = D / 16;
+    static constexpr int kCodes = mx::Row<D>::kCodes, kScales = mx::Row<D>::kScales;
+    struct Key { unsigned c[kW], s; };
+    struct Value { unsigned c, s; };
+    __device__ __forceinline__ static Key key(MxSrc p, long long row, int g) {
+        Key k;
+        const unsigned* c = reinterpret_cast<const unsigned*>(p.c + row * kCodes + (kCodes / 4) * g);
+        if constexpr (kW == 4) {
+            const dev::u32x4 x = *reinterpret_cast<const dev::u32x4*>(c);
+            dev::static_for<4>([&](auto i) { k.c[decltype(i)::value] = x[decltype(i)::value]; });
+        } else {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(c);
+            dev::static_for<2>([&](auto i) { k.c[decltype(i)::value] = x[decltype(i)::value]; });
+        }
+        k.s = p.s[row * kScales + g * kScales / 4];
+        return k;
+    }
+    __device__ __forceinline__ static Value value(MxSrc p, long long row, int m) {
+        Value v;
+        const uint8_t* c = p.c + row * kCodes + (kDV / 2) * m;
+        if constexpr (kDV == 8)
+            v.c = *reinterpret_cast<const unsigned*>(c);
+        else
+            v.c = *reinterpret_cast<const uint16_t*>(c);
+        v.s = p.s[row * kScales + m * kScales / 16];
+        return v;
+    }
+};
+
+// bf16 queries.
+template <int D>
+struct Mx : Bf16<D> {
+    using P = Bf16<D>;
+    using R = MxRows<D>;
+    static constexpr int kKeys = P::kKeys, kTiles = P::kTiles, kKK = P::kKK, kDV = P::kDV;
+    struct K { typename R::Key k[kTiles]; };
+    struct V { typename R::Value v[8]; };
+    typedef MxSrc Src;
+    __device__ static Src keys(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.K, a.KS, row); }
+    __device__ static Src values_of(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.V, a.VS, row); }
+    __device__ static int chunk(int kk, int g) { return D / 4 * g + 8 * kk; }
+    struct Off {};
+    __device__ static Off offsets(int) { return {}; }
+    __device__ static void load_k(K& k, Src p, int k0, int last, Off, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        dev::static_for<kTiles>([&](auto ac) {
+            constexpr int a = decltype(ac)::value;
+            k.k[a] = R::key(p, min(k0 + 16 * a + m, last), g);
+        });
+    }
+    __device__ static void load_v(V& v, Src p, int k0, int last, Off, int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        dev::static_for<8>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            v.v[j] = R::value(p, min(k0 + 16 * (j / 4) + 4 * g + j % 4, last), m);
+        });
+    }
+    __device__ static typename P::K plain(const K& k) {
+        typename P::K x;
+        dev::static_for<kTiles * kKK>([&](auto c) {
+            constexpr int a = decltype(c)::value / kKK, kk = decltype(c)::value % kKK;
+            const unsigned w = k.k[a].c[kk];
+            const float s = mx::scale(k.k[a].s);
+            x.v[a][kk] = mx::eight_bf16(w, s);
+        });
+        return x;
+    }
+    __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const typename P::Q& q) { P::logits(s, plain(k), q); }
+    template <int NR, int RT>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
+        typename P::V x;
+        dev::static_for<8 * kDV / 2>([&](auto c) {
+            constexpr int j = decltype(c)::value / (kDV / 2), i = decltype(c)::value % (kDV / 2);
+            x.v[j][i] = mx::pair_bf16<i>(v.v[j].c, mx::scale(v.v[j].s));
+        });
+        P::template values<NR>(o, x, p);
+    }
+};
+
+// fp32 queries.
+template <int D>
+struct MxF32 : F32<D> {
+    using P = F32<D>;
+    using R = MxRows<D>;
+    static constexpr int kKeys = P::kKeys, kKK = P::kKK, kDV = P::kDV;
+    struct K { typename R::Key k; };
+    struct V { typename R::Value v[4]; };
+    typedef MxSrc Src;
+    __device__ static Src keys(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.K, a.KS, row); }
+    __device__ static Src values_of(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.V, a.VS, row); }
+    __device__ static int chunk(int kk, int g) { return D / 4 * g + 4 * kk; }
+    struct Off {};
+    __device__ static Off offsets(int) { return {}; }
+    __device__ static void load_k(K& k, Src p, int k0, int last, Off, int lane) {
+        k.k = R::key(p, min(k0 + (lane & 15), last), lane >> 4);
+    }
+    __device__ static void load_v(V& v, Src p, int k0, int last, Off, int lane) {
+        dev::static_for<4>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            v.v[j] = R::value(p, min(k0 + 4 * (lane >> 4) + j, last), lane & 15);
+        });
+    }
+    // Half of a word: four coordinates.
+    template <int H>
+    __device__ static f32x4 half(unsigned w, float s) {
+        const mx::f32x2 a = mx::pair_f32<2 * H>(w, s), b = mx::pair_f32<2 * H + 1>(w, s);
+        return f32x4{a[0], a[1], b[0], b[1]};
+    }
+    __device__ static void logits(f32x4 (&s)[1], const K& k, const typename P::Q& q) {
+        typename P::K x;
+        dev::static_for<kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            x.v[0][kk] = half<kk % 2>(k.k.c[kk / 2], mx::scale(k.k.s));
+        });
+        P::logits(s, x, q);
+    }
+    template <int NR, int RT>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][1]) {
+        typename P::V x;
+        dev::static_for<4 * kDV / 4>([&](auto c) {
+            constexpr int j = decltype(c)::value / (kDV / 4), i = decltype(c)::value % (kDV / 4);
+            x.v[j][i] = half<i>(v.v[j].c, mx::scale(v.v[j].s));
+        });
+        P::template values<NR>(o, x, p);
+    }
+};
+
+}  // namespace
+}  // namespace attend
+
+hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, bool wide, hipStream_t s) {
+    using namespace attend;
+    if (dtype == BKV_BF16) return a.D == 128 ? stream<Mx<128>, 128>(a, wide, s) : stream<Mx<64>, 64>(a, wide, s);
+    return a.D == 128 ? stream<MxF32<128>, 128>(a, wide, s) : stream<MxF32<64>, 64>(a, wide, s);
+}
+hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s) {
+    using namespace attend;
+    return a.D == 128 ? row_mass<Mx<128>, 128>(a, ns, chunk, s) : row_mass<Mx<64>, 64>(a, ns, chunk, s);
+}
+
+}  // namespace bkv

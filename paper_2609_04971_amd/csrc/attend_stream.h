@@ -47,6 +47,11 @@ struct Bf16 {
     struct Q { dev::u32x4 v[kKK]; };
     struct K { dev::u32x4 v[kTiles][kKK]; };
     struct V { unsigned v[8][kDV / 2]; };
+    typedef const elem* Src;  // the rows of a unit's keys or values
+    __device__ static Src keys(const Args&, const Segment& sg, long long row) { return static_cast<const elem*>(sg.K) + row * D; }
+    __device__ static Src values_of(const Args&, const Segment& sg, long long row) {
+        return static_cast<const elem*>(sg.V) + row * D;
+    }
 
     // Which 16-byte chunk of a row (in elements) load kk of lane group g takes.
     __device__ static int chunk(int kk, int g) { return 32 * kk + 8 * g; }
@@ -108,6 +113,7 @@ struct Bf16 {
             dev::static_for<2>([&](auto c) { v.v[J][decltype(c)::value] = x[decltype(c)::value]; });
         }
     }
+    __device__ static const K& plain(const K& k) { return k; }
     __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const Q& q) {
         dev::static_for<kTiles>([&](auto ac) {
             constexpr int a = decltype(ac)::value;
@@ -168,6 +174,11 @@ struct F32 {
     struct Q { f32x4 v[kKK]; };
     struct K { f32x4 v[1][kKK]; };
     struct V { f32x4 v[4][kDV / 4]; };
+    typedef const elem* Src;
+    __device__ static Src keys(const Args&, const Segment& sg, long long row) { return static_cast<const elem*>(sg.K) + row * D; }
+    __device__ static Src values_of(const Args&, const Segment& sg, long long row) {
+        return static_cast<const elem*>(sg.V) + row * D;
+    }
 
     __device__ static int chunk(int kk, int g) { return 16 * kk + 4 * g; }
 
@@ -282,7 +293,9 @@ typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 // (6.1), 128 of 4224 in two 47 (6.0).  More rows (fp32 caches, prefixes of few
 // items) come in row blocks and are bound by the products: fp32, 2048 causal
 // queries of 32 heads 350 us (98 TFLOP/s of what is seen, products alone 154).
-template <class E, int D, int RT>
+// WIN: rows see their windows (causal, one segment, no logits kept), and the
+// splits are of the walk's places.
+template <class E, int D, int RT, bool WIN>
 __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     constexpr int KG = E::kKeys, NT = E::kTiles, DV = E::kDV;
     constexpr int DP = D + kPadO;  // padded row of the joined sums
@@ -340,10 +353,11 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     least = __builtin_amdgcn_readfirstlane(least);
     const int k_lo = split * sg.chunk;
     // with the logits kept, keys that no row sees are written too (as -inf)
-    const int keep = own ? a.keep : kKeepNone;
-    const int k_hi = min(k_lo + sg.chunk, keep ? len : most);
-    const typename E::elem* K = static_cast<const typename E::elem*>(sg.K) + (long long)unit * sg.cap * D;
-    const typename E::elem* V = static_cast<const typename E::elem*>(sg.V) + (long long)unit * sg.cap * D;
+    const int keep = own && !WIN ? a.keep : kKeepNone;
+    Walk w{};
+    if constexpr (WIN) w = Walk::over<KG>(a, least, most);
+    const int k_hi = min(k_lo + sg.chunk, WIN ? w.n : keep ? len : most);
+    const typename E::Src K = E::keys(a, sg, (long long)unit * sg.cap), V = E::values_of(a, sg, (long long)unit * sg.cap);
     lds_float* const s_l = s_o + kWaves * a.o_rows * DP;
     const int lds_stride = sg.chunk + kPadL;
     float* const glob = keep ? a.logits + (long long)unit * a.R * a.lstride : nullptr;
@@ -353,27 +367,34 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         constexpr int NR = decltype(nc)::value;
         int k0 = k_lo + KG * wave;
         if (k0 >= k_hi) return;
-        const int last = k_hi - 1;  // rows past it repeat it: nothing behind a sequence is read
+        const int last = WIN ? most - 1 : k_hi - 1;  // rows past it repeat it: nothing behind a sequence is read
+        auto key = [&](int v) { return WIN ? w.key(v) : v; };
         typename E::K kr;
         typename E::V vr;
         const typename E::Off off = E::offsets(lane);
-        E::load_k(kr, K, k0, last, off, lane);
-        E::load_v(vr, V, k0, last, off, lane);
+        E::load_k(kr, K, key(k0), last, off, lane);
+        E::load_v(vr, V, key(k0), last, off, lane);
         for (; k0 < k_hi; k0 += KG * kWaves) {
+            const int at0 = key(k0);
             f32x4 p[RT][NT];
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 E::logits(p[rt], kr, q[rt]);
             });
-            E::load_k(kr, K, k0 + KG * kWaves, last, off, lane);
-            const bool edge = k0 + KG > min(least, k_hi);
+            E::load_k(kr, K, key(k0 + KG * kWaves), last, off, lane);
+            const bool edge = WIN ? at0 + KG > least || (at0 < most - a.window && at0 + KG > a.sinks) : k0 + KG > min(least, k_hi);
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 float top = kLowest;
                 dev::static_for<NT * 4>([&](auto ic) {
                     constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
                     float l = p[rt][ti][i] * a.scale2;
-                    if (edge && k0 + 16 * ti + 4 * g + i >= min(lim[rt], k_hi)) l = -INFINITY;
+                    if constexpr (WIN) {
+                        const int j = at0 + 16 * ti + 4 * g + i;
+                        if (edge && (j >= min(lim[rt], most) || (j < lim[rt] - a.window && j >= a.sinks))) l = -INFINITY;
+                    } else if (edge && k0 + 16 * ti + 4 * g + i >= min(lim[rt], k_hi)) {
+                        l = -INFINITY;
+                    }
                     p[rt][ti][i] = l;
                     top = fmaxf(top, l);
                 });
@@ -402,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                 });
             });
             E::template values<NR>(o, vr, p);
-            E::load_v(vr, V, k0 + KG * kWaves, last, off, lane);
+            E::load_v(vr, V, key(k0 + KG * kWaves), last, off, lane);
         }
     };
     if constexpr (RT == 2) {
@@ -494,9 +515,8 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
 // reads and the chain of a wave: 54 heads of 48110 tokens and 56 rows 134 us
 // (5.0 TB/s; blocks of keys in registers and the rows past them 593), 1504
 // heads of 560 and 40 rows 50 (4.3 TB/s; 210).
-template <int D, int RT>
+template <class E, int D, int RT>
 __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk) {
-    using E = Bf16<D>;
     __shared__ __attribute__((aligned(16))) float s_norm[16 * RT];
     __shared__ __attribute__((aligned(16))) int s_lim[16 * RT];  // keys that the row sees
     typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -507,7 +527,7 @@ __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk
     const int len = unit_len(sg, unit, a.Hkv);
     const int k_lo = split * chunk, k_hi = min(k_lo + chunk, len);
     if (k_lo >= k_hi) return;
-    const uint16_t* K = static_cast<const uint16_t*>(sg.K) + (long long)unit * sg.cap * D;
+    const typename E::Src K = E::keys(a, sg, (long long)unit * sg.cap);
     float* mass = a.mass + (long long)unit * a.N_cap;
     const typename E::Off off = E::offsets(lane);
     struct Group {
@@ -523,14 +543,14 @@ __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk
     Group one, two;
     load(one, k_lo + E::kKeys * wave);
     const long long row0 = (long long)unit * a.R;
-    const uint16_t* q = static_cast<const uint16_t*>(a.q) + row0 * D + 8 * g;
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + row0 * D + E::chunk(0, g);
     typename E::Q y[RT];
     dev::static_for<RT>([&](auto rc) {
         constexpr int rt = decltype(rc)::value;
         const int r = 16 * rt + col;
         dev::static_for<E::kKK>([&](auto c) {
             constexpr int kk = decltype(c)::value;
-            y[rt].v[kk] = r < a.R ? *reinterpret_cast<const dev::u32x4*>(q + (long long)r * D + 32 * kk) : dev::u32x4{};
+            y[rt].v[kk] = r < a.R ? *reinterpret_cast<const dev::u32x4*>(q + (long long)r * D + E::chunk(kk, 0)) : dev::u32x4{};
         });
     });
     if ((int)threadIdx.x < 16 * RT) {
@@ -542,6 +562,7 @@ __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk
     const int all = sg.causal ? len - a.T + 1 : len;  // keys that every row sees
     auto step = [&](const Group& x, int k0) __attribute__((always_inline)) {
         f32x4 sum[E::kTiles] = {};
+        const auto& k = E::plain(x.k);
         const bool edge = k0 + E::kKeys > all;
         asm volatile("" ::: "memory");  // or every row's normaliser would be kept in a register
         dev::static_for<RT>([&](auto rc) {
@@ -551,7 +572,7 @@ __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk
             dev::static_for<E::kKK * E::kTiles>([&](auto c) {
                 constexpr int kk = decltype(c)::value / E::kTiles, t = decltype(c)::value % E::kTiles;
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, y[rt].v[kk]),
-                                                               __builtin_bit_cast(bf16x8_t, x.k.v[t][kk]), s[t], 0, 0, 0);
+                                                               __builtin_bit_cast(bf16x8_t, k.v[t][kk]), s[t], 0, 0, 0);
             });
             dev::static_for<E::kTiles>([&](auto tc) {
                 constexpr int t = decltype(tc)::value;
@@ -590,13 +611,28 @@ __global__ __launch_bounds__(kThreads, 2) void row_mass_kernel(Args a, int chunk
 }
 
 template <class E, int D>
+hipError_t row_mass(const Args& a, int ns, int chunk, hipStream_t s) {
+    const dim3 grid((unsigned)(a.seg[1].units * ns)), block(kThreads);
+    if (a.R <= 64)
+        hipLaunchKernelGGL((row_mass_kernel<E, D, 4>), grid, block, 0, s, a, chunk);
+    else
+        hipLaunchKernelGGL((row_mass_kernel<E, D, 6>), grid, block, 0, s, a, chunk);
+    return hipGetLastError();
+}
+
+template <class E, int D>
 hipError_t stream(const Args& a, bool wide, hipStream_t s) {
     const long long items = a.items0 + (long long)a.seg[1].units * a.seg[1].nrb * a.seg[1].ns;
     if (items == 0) return hipSuccess;
-    if (wide)
-        hipLaunchKernelGGL((stream_kernel<E, D, 2>), dim3((unsigned)items), dim3(kThreads), stream_lds(a), s, a);
+    const dim3 grid((unsigned)items), block(kThreads);
+    if (a.window > 0 && wide)
+        hipLaunchKernelGGL((stream_kernel<E, D, 2, true>), grid, block, stream_lds(a), s, a);
+    else if (a.window > 0)
+        hipLaunchKernelGGL((stream_kernel<E, D, 1, true>), grid, block, stream_lds(a), s, a);
+    else if (wide)
+        hipLaunchKernelGGL((stream_kernel<E, D, 2, false>), grid, block, stream_lds(a), s, a);
     else
-        hipLaunchKernelGGL((stream_kernel<E, D, 1>), dim3((unsigned)items), dim3(kThreads), stream_lds(a), s, a);
+        hipLaunchKernelGGL((stream_kernel<E, D, 1, false>), grid, block, stream_lds(a), s, a);
     return hipGetLastError();
 }
 

@@ -120,6 +120,31 @@ struct Bf16 {
     __device__ __forceinline__ static f32x16 dot(frag a, frag b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
+    typedef const elem* Src;  // the rows of a unit's keys or values
+    __device__ __forceinline__ static Src keys(const Args&, const Segment& sg, long long row) {
+        return static_cast<const elem*>(sg.K) + row * D;
+    }
+    __device__ __forceinline__ static Src values_of(const Args&, const Segment& sg, long long row) {
+        return static_cast<const elem*>(sg.V) + row * D;
+    }
+    // Rows [k0, k_hi) of a tile on their way into LDS; nothing is left to do when
+    // the tile before has been worked off.
+    struct Stage {
+        __device__ __forceinline__ void fetch(Src K, Src V, int k0, int k_hi, elem* ks, elem* vs, int wave, int lane) {
+            load_tile<Bf16, kKeys>(K + (long long)k0 * D, k_hi - k0, ks, wave, lane);
+            load_tile<Bf16, kKeys>(V + (long long)k0 * D, k_hi - k0, vs, wave, lane);
+        }
+        __device__ __forceinline__ void commit(elem*, elem*, int, int) {}
+    };
+    // Chunk 2 kk + h of a key.
+    struct KeyAt {
+        const elem* p;
+        __device__ __forceinline__ KeyAt(Src K, int row, int h) : p(K + (long long)row * D + EPC * h) {}
+        template <int KK>
+        __device__ __forceinline__ frag operator()(std::integral_constant<int, KK>) const {
+            return *reinterpret_cast<const frag*>(p + 2 * EPC * KK);
+        }
+    };
     struct Values { int v[D / 32][2]; };    // coordinates 32 dt + lane % 32, keys 4 h + L / 4 and 8 more
     __device__ __forceinline__ static Values values(int lane) {
         // lanes 4 i .. 4 i + 3 of a group of 16 read 16 coordinates of key i, and
@@ -200,6 +225,18 @@ struct F32 {
     static constexpr int kRowAts = 1;
     static constexpr int kMassResident = 2;
 
+    typedef const elem* Src;
+    __device__ __forceinline__ static Src keys(const Args&, const Segment& sg, long long row) {
+        return static_cast<const elem*>(sg.K) + row * D;
+    }
+    struct KeyAt {
+        const elem* p;
+        __device__ __forceinline__ KeyAt(Src K, int row, int h) : p(K + (long long)row * D + EPC * h) {}
+        template <int KK>
+        __device__ __forceinline__ frag operator()(std::integral_constant<int, KK>) const {
+            return *reinterpret_cast<const frag*>(p + 2 * EPC * KK);
+        }
+    };
     __device__ __forceinline__ static f32x16 dot(frag a, frag b, f32x16 c) {
         dev::static_for<4>([&](auto ec) {
             constexpr int e = decltype(ec)::value;
@@ -231,11 +268,12 @@ struct State {
 constexpr float kMost = 1024.f;
 
 // One tile of keys [k0, k0 + kKeys) against the wave's rows.  edge: some row
-// does not see some key (lim: keys that the lane's row sees).
-template <class E>
+// does not see some key (lim: keys that the lane's row sees; WIN: of those the
+// first `sinks` and the ones from `low` on).
+template <class E, bool WIN>
 __device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, const typename E::Values& at_v,
                                           const typename E::elem* ks, const typename E::elem* vs, int k0, int lim,
-                                          bool edge, float scale2, int lane) {
+                                          bool edge, float scale2, int lane, int low = 0, int sinks = 0) {
     constexpr int N = 16 * E::kTiles;
     f32x16 s[E::kTiles];
     const RowAt<E> at_k = at.opaque();
@@ -253,7 +291,12 @@ __device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, cons
         const int h4 = 4 * (lane >> 5);
         dev::static_for<N>([&](auto ic) {
             constexpr int kt = decltype(ic)::value / 16, i = decltype(ic)::value % 16;
-            if (k0 + 32 * kt + 8 * (i / 4) + h4 + i % 4 >= lim) s[kt][i] = -INFINITY;
+            if constexpr (WIN) {
+                const int j = k0 + 32 * kt + 8 * (i / 4) + h4 + i % 4;
+                if (j >= lim || (j < low && j >= sinks)) s[kt][i] = -INFINITY;
+            } else {
+                if (k0 + 32 * kt + 8 * (i / 4) + h4 + i % 4 >= lim) s[kt][i] = -INFINITY;
+            }
         });
     }
     // The exponentials are taken against the running maximum as it stands: the
@@ -295,7 +338,8 @@ __device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, cons
 // product of 8192^3 1.21), and by the exponentials at D 64: 500 queries of 28
 // heads against 24001 keys 100 us (850 TFLOP/s).  With 35 to 56 rows it reads
 // keys and values at 4.8 to 6.0 TB/s.
-template <class E>
+// WIN: rows see their windows (causal), and the splits are of the walk's places.
+template <class E, bool WIN>
 __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     using elem = typename E::elem;
     constexpr int D = E::D, DT = D / 32, kKeys = E::kKeys;
@@ -347,34 +391,48 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     // their splits are alike and none is empty; others share their tiles in L2
     int chunk = sg.chunk;
     const bool prompt = sg.causal && a.T > sg.n / 5;
-    if (prompt || sg.lens) {
-        const int each = ((prompt ? all : len) + sg.ns - 1) / sg.ns;
+    Walk w{};
+    if constexpr (WIN) {
+        const int first = len - a.T + 1 + r0 / a.G;  // keys up to the first row's own
+        w = Walk::over<kKeys>(a, __builtin_amdgcn_readfirstlane(max(0, first)), all);
+        all = w.n;
+    }
+    if (prompt || sg.lens || WIN) {
+        const int each = ((prompt || WIN ? all : len) + sg.ns - 1) / sg.ns;
         chunk = __builtin_amdgcn_readfirstlane(max(128, (each + 63) / 64 * 64));
     }
     const int k_lo = split * chunk, k_hi = min(k_lo + chunk, all);
-    const elem* K = static_cast<const elem*>(sg.K) + (long long)unit * sg.cap * D;
-    const elem* V = static_cast<const elem*>(sg.V) + (long long)unit * sg.cap * D;
+    auto key = [&](int v) { return WIN ? w.key(v) : v; };  // the key at a place
+    const typename E::Src K = E::keys(a, sg, (long long)unit * sg.cap), V = E::values_of(a, sg, (long long)unit * sg.cap);
+    typename E::Stage stage;
     auto load = [&](int k0, elem* ks, elem* vs) {
-        if (k0 < k_hi) {
-            load_tile<E, kKeys>(K + (long long)k0 * D, k_hi - k0, ks, wave, lane);
-            load_tile<E, kKeys>(V + (long long)k0 * D, k_hi - k0, vs, wave, lane);
-        }
+        if (k0 < k_hi) stage.fetch(K, V, key(k0), WIN ? key(k_hi - 1) + 1 : k_hi, ks, vs, wave, lane);
     };
     const RowAt<E> at_k(lane);
     const typename E::Values at_v = E::values(lane);
     auto step = [&](int k0, const elem* ks, const elem* vs) {
-        if (k0 < most)
-            tile_step<E>(st, at_k, at_v, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
+        if constexpr (WIN) {
+            const int j0 = key(k0);
+            if (j0 < most && (j0 < a.sinks || j0 + kKeys > least - a.window))
+                tile_step<E, true>(st, at_k, at_v, ks, vs, j0, min(lim, key(k_hi - 1) + 1),
+                                   j0 + kKeys > least || (j0 < most - a.window && j0 + kKeys > a.sinks), a.scale2, lane,
+                                   lim - a.window, a.sinks);
+        } else if (k0 < most) {
+            tile_step<E, false>(st, at_k, at_v, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
+        }
     };
     load(k_lo, k_a, v_a);
+    if (k_lo < k_hi) stage.commit(k_a, v_a, wave, lane);
     for (int k0 = k_lo; k0 < k_hi; k0 += 2 * kKeys) {
         turn();  // tile a has landed, tile b is free
         load(k0 + kKeys, k_b, v_b);
         step(k0, k_a, v_a);
         if (k0 + kKeys >= k_hi) break;
+        stage.commit(k_b, v_b, wave, lane);
         turn();
         load(k0 + 2 * kKeys, k_a, v_a);
         step(k0 + kKeys, k_b, v_b);
+        if (k0 + 2 * kKeys < k_hi) stage.commit(k_a, v_a, wave, lane);
     }
     if (!valid) return;
     const auto zr = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.z), __float_as_uint(st.z), false, false);
@@ -438,15 +496,12 @@ __global__ __launch_bounds__(kThreads, E::kMassResident) void tile_mass_kernel(A
     const int len = unit_len(sg, unit, a.Hkv);
     if (k0 >= len) return;
     const int key0 = k0 + 64 * kw;
-    const elem* K = static_cast<const elem*>(sg.K) + (long long)unit * sg.cap * D;
+    const typename E::Src K = E::keys(a, sg, (long long)unit * sg.cap);
     typename E::frag kr[2][E::KK];
     dev::static_for<2>([&](auto tc) {
         constexpr int kt = decltype(tc)::value;
-        const elem* kp = K + (long long)min(key0 + 32 * kt + (lane & 31), len - 1) * D + E::EPC * h;
-        dev::static_for<E::KK>([&](auto kc) {
-            constexpr int kk = decltype(kc)::value;
-            kr[kt][kk] = *reinterpret_cast<const typename E::frag*>(kp + 2 * E::EPC * kk);
-        });
+        const typename E::KeyAt key(K, min(key0 + 32 * kt + (lane & 31), len - 1), h);
+        dev::static_for<E::KK>([&](auto kc) { kr[kt][decltype(kc)::value] = key(kc); });
     });
     f32x4 sum[2] = {};
     const MassRows rows(a, sg.causal, len, k0, kMassKeys, pt, parts);
@@ -533,7 +588,23 @@ __global__ __launch_bounds__(kThreads, E::kMassResident) void tile_mass_kernel(A
         a.mass[(long long)unit * a.N_cap + k0 + i] += mine + s_sum[i];
 }
 
+template <class E>
+hipError_t tile(const Args& a, const Segment& sg, hipStream_t s) {
+    const long long items = (long long)sg.units * sg.nrb * sg.ns;
+    if (items == 0) return hipSuccess;
+    if (a.window > 0)
+        hipLaunchKernelGGL((tile_kernel<E, true>), dim3((unsigned)items), dim3(kThreads), 0, s, a, sg);
+    else
+        hipLaunchKernelGGL((tile_kernel<E, false>), dim3((unsigned)items), dim3(kThreads), 0, s, a, sg);
+    return hipGetLastError();
+}
+
+template <class E>
+hipError_t tile_mass(const Args& a, float* part, int parts, hipStream_t s) {
+    hipLaunchKernelGGL(tile_mass_kernel<E>, dim3((unsigned)mass_blocks(a, parts)), dim3(kThreads), 0, s, a, part, parts);
+    return hipGetLastError();
+}
+
 }  // namespace
 }  // namespace attend
-
 }  // namespace bkv

@@ -1,0 +1,133 @@
+// Attention of many query rows over a 4-bit cache for gfx950, and the sums of
+// their weights: the tile kernels (attend_tile.h) with keys and values that become
+// bf16 (the sums' keys for fp32 queries fp32) on their way.
+//
+// A tile's codes are requested before the tile in front of it is worked off and
+// put into LDS as bf16 values after it, where the products find them as they do
+// a plain cache's.  A thread takes whole blocks: 16 bytes of codes, 16
+// conversions, four chunks of a row in LDS.  Threads are dealt to blocks so that
+// the 16 lanes that LDS serves at once write 16 different positions of 16 bytes.
+#include "attend_tile.h"
+#include "mx.h"
+
+namespace bkv {
+namespace attend {
+namespace {
+
+struct MxSrc {
+    const uint8_t* c;
+    const uint8_t* s;
+};
+template <int D>
+__device__ __forceinline__ MxSrc mx_rows(const void* codes, const uint8_t* bytes, long long row) {
+    return {static_cast<const uint8_t*>(codes) + row * mx::Row<D>::kCodes, bytes + row * mx::Row<D>::kScales};
+}
+
+template <int D_>
+struct Mx : Bf16<D_> {
+    using P = Bf16<D_>;
+    static constexpr int D = D_, kKeys = P::kKeys;
+    static constexpr int kCodes = mx::Row<D>::kCodes, kScales = mx::Row<D>::kScales;
+    typedef typename P::elem elem;
+    typedef typename P::frag frag;
+    typedef MxSrc Src;
+    __device__ __forceinline__ static Src keys(const Args& a, const Segment& sg, long long row) {
+        return mx_rows<D>(sg.K, a.KS, row);
+    }
+    __device__ __forceinline__ static Src values_of(const Args& a, const Segment& sg, long long row) {
+        return mx_rows<D>(sg.V, a.VS, row);
+    }
+    // D 128: a block of the keys and one of the values a thread.  D 64: one block,
+    // waves 0 and 1 the keys', 2 and 3 the values'.
+    struct Stage {
+        static constexpr int kSides = kKeys * (D / mx::kBlock) / 128;  // of K and V that a thread takes blocks of
+        dev::u32x4 c[kSides];
+        unsigned s[kSides];
+        // the thread's row of the tile, and its block of that row
+        __device__ __forceinline__ static int row(int wave, int lane) {
+            if constexpr (D == 128) return 16 * wave + 4 * ((lane >> 2) & 3) + (lane >> 4);
+            return 32 * (wave & 1) + 16 * (lane >> 5) + 4 * ((lane >> 2) & 3) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        }
+        __device__ __forceinline__ static int block(int lane) { return lane & (D / mx::kBlock - 1); }
+        // rows at or past k_hi repeat the last one: nothing behind a sequence is read
+        __device__ __forceinline__ void fetch(Src K, Src V, int k0, int k_hi, elem*, elem*, int wave, int lane) {
+            const long long r = min(k0 + row(wave, lane), k_hi - 1);
+            const int b = block(lane);
+            dev::static_for<kSides>([&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                const bool values = kSides == 2 ? i == 1 : wave >= 2;
+                const Src p = {values ? V.c : K.c, values ? V.s : K.s};
+                c[i] = *reinterpret_cast<const dev::u32x4*>(p.c + r * kCodes + 16 * b);
+                s[i] = p.s[r * kScales + b];
+            });
+        }
+        __device__ __forceinline__ void commit(elem* ks, elem* vs, int wave, int lane) {
+            const int r = row(wave, lane), b = block(lane);
+            dev::static_for<kSides>([&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                elem* stage = (kSides == 2 ? i == 1 : wave >= 2) ? vs : ks;
+                const float x = mx::scale(s[i]);
+                dev::static_for<4>([&](auto jc) {
+                    constexpr int j = decltype(jc)::value;
+                    *reinterpret_cast<dev::u32x4*>(stage + r * D + ((4 * b + j) ^ swz<P>(r)) * 8) = mx::eight_bf16(c[i][j], x);
+                });
+            });
+        }
+    };
+    // Chunk 2 kk + h of a key: a word of codes.
+    struct KeyAt {
+        const unsigned* c;
+        const uint8_t* s;
+        int h;
+        __device__ __forceinline__ KeyAt(Src K, int row, int h_)
+            : c(reinterpret_cast<const unsigned*>(K.c + (long long)row * kCodes)), s(K.s + (long long)row * kScales), h(h_) {}
+        template <int KK>
+        __device__ __forceinline__ frag operator()(std::integral_constant<int, KK>) const {
+            return __builtin_bit_cast(frag, mx::eight_bf16(c[2 * KK + h], mx::scale(s[KK / 2])));
+        }
+    };
+};
+
+// fp32 queries, for the weights' sums.
+template <int D_>
+struct MxF32 : F32<D_> {
+    using P = F32<D_>;
+    static constexpr int D = D_;
+    static constexpr int kCodes = mx::Row<D>::kCodes, kScales = mx::Row<D>::kScales;
+    typedef typename P::frag frag;
+    typedef MxSrc Src;
+    __device__ __forceinline__ static Src keys(const Args& a, const Segment& sg, long long row) {
+        return mx_rows<D>(sg.K, a.KS, row);
+    }
+    // Chunk 2 kk + h of a key: half a word of codes.
+    struct KeyAt {
+        const uint16_t* c;
+        const uint8_t* s;
+        int h;
+        __device__ __forceinline__ KeyAt(Src K, int row, int h_)
+            : c(reinterpret_cast<const uint16_t*>(K.c + (long long)row * kCodes)), s(K.s + (long long)row * kScales), h(h_) {}
+        template <int KK>
+        __device__ __forceinline__ frag operator()(std::integral_constant<int, KK>) const {
+            const unsigned w = c[2 * KK + h];
+            const float x = mx::scale(s[KK / 4]);
+            const mx::f32x2 lo = mx::pair_f32<0>(w, x), hi = mx::pair_f32<1>(w, x);
+            return frag{lo[0], lo[1], hi[0], hi[1]};
+        }
+    };
+};
+
+}  // namespace
+}  // namespace attend
+
+hipError_t launch_attend_tile_mx(const attend::Args& a, const attend::Segment& sg, hipStream_t s) {
+    using namespace attend;
+    return a.D == 128 ? tile<Mx<128>>(a, sg, s) : tile<Mx<64>>(a, sg, s);
+}
+
+hipError_t launch_attend_tile_mass_mx(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s) {
+    using namespace attend;
+    if (dtype == BKV_BF16) return a.D == 128 ? tile_mass<Mx<128>>(a, part, parts, s) : tile_mass<Mx<64>>(a, part, parts, s);
+    return a.D == 128 ? tile_mass<MxF32<128>>(a, part, parts, s) : tile_mass<MxF32<64>>(a, part, parts, s);
+}
+
+}  // namespace bkv

@@ -45,6 +45,11 @@ template <int B>
 __device__ __forceinline__ f32x2 pair_f32(unsigned codes, float scale) {
     return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, B);
 }
+// All eight of a word.
+__device__ __forceinline__ dev::u32x4 eight_bf16(unsigned codes, float scale) {
+    return dev::u32x4{pair_bf16<0>(codes, scale), pair_bf16<1>(codes, scale), pair_bf16<2>(codes, scale),
+                      pair_bf16<3>(codes, scale)};
+}
 
 }  // namespace mx
 }  // namespace bkv

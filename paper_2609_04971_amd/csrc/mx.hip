@@ -88,9 +88,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(MxArgs a) {
 }
 
 __device__ __forceinline__ void put(uint16_t* p, unsigned w, float s) {
-    __builtin_nontemporal_store(dev::u32x4{mx::pair_bf16<0>(w, s), mx::pair_bf16<1>(w, s), mx::pair_bf16<2>(w, s),
-                                           mx::pair_bf16<3>(w, s)},
-                                reinterpret_cast<dev::u32x4*>(p));
+    __builtin_nontemporal_store(mx::eight_bf16(w, s), reinterpret_cast<dev::u32x4*>(p));
 }
 __device__ __forceinline__ void put(float* p, unsigned w, float s) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
