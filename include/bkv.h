@@ -456,6 +456,19 @@ bkv_status bkv_attend_mx(const bkv_dims* d, int32_t flags, const void* q, int32_
                          int32_t window, int32_t sinks, const int32_t* lens, float scale, void* out, float* lse,
                          float* mass, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* bkv_compact of a 4-bit cache: row i of codes and bytes, of K and V, becomes row
+ * kept[i] (what bkv_topk emits; for scores, bkv_load_mx gives the keys), bit for
+ * bit; the workspace and all else as there.  The cache's arrays, kept and the
+ * workspace must not overlap (BKV_ERR_INVALID). */
+bkv_status bkv_compact_mx(const bkv_dims* d, const bkv_mx_cache* cache, const int32_t* kept, void* ws, size_t ws_bytes,
+                          hipStream_t stream);
+
+/* bkv_evict_mass of a 4-bit cache: selection, layouts, masses, kept, the
+ * workspace (bkv_mass_workspace_bytes) and all else as there; none of the arrays
+ * may overlap. */
+bkv_status bkv_evict_mass_mx(const bkv_dims* d, int32_t flags, const bkv_mx_cache* cache, float* mass, int32_t* kept,
+                             void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* bkv_status_string(bkv_status s);
 

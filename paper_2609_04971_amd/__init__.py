@@ -29,7 +29,7 @@ EXPORTS = ("bkv_validate", "bkv_workspace_bytes", "bkv_workspace_init", "bkv_dev
            "bkv_abi_version", "bkv_compact_fill", "bkv_evict_noalloc", "bkv_append_rows",
            "bkv_attend", "bkv_attend_shared", "bkv_attend_workspace_bytes", "bkv_evict_mass",
            "bkv_mass_workspace_bytes", "bkv_store_mx", "bkv_load_mx", "bkv_attend_mx",
-           "bkv_attend_window")
+           "bkv_attend_window", "bkv_compact_mx", "bkv_evict_mass_mx")
 APPEND_MAX = 4
 SCORE_MEAN, SCORE_CAUSAL = 1, 2
 ATTEND_CAUSAL = 1
@@ -126,6 +126,8 @@ _SIGS = {
     "bkv_attend_mx": ([_D, _I, _P, _I, ctypes.POINTER(_MxPtrs), _I, _I, _P, ctypes.c_float, _P, _P, _P, _P, _S, _P],
                       ctypes.c_int),
     "bkv_attend_window": ([_D, _P, _I, _P, _P, _I, _I, _P, ctypes.c_float, _P, _P, _P, _S, _P], ctypes.c_int),
+    "bkv_compact_mx": ([_D, ctypes.POINTER(_MxPtrs), _P, _P, _S, _P], ctypes.c_int),
+    "bkv_evict_mass_mx": ([_D, _I, ctypes.POINTER(_MxPtrs), _P, _P, _P, _S, _P], ctypes.c_int),
     "bkv_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "bkv_abi_version": ([], ctypes.c_int32),
 }
@@ -516,6 +518,28 @@ def attend_mx(d: Dims, q, cache: MxCache, out, ws, lens=None, lse=None, mass=Non
     st = lib().bkv_attend_mx(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, ctypes.byref(cp), window, sinks, lp, scale,
                              op, ep, mp, wp, wn, torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_mx")
+
+
+def compact_mx(d: Dims, cache: MxCache, kept, ws):
+    """compact() of a 4-bit cache."""
+    dev = _device_of(kept, "kept")
+    cp = _arg_mx(d, cache, dev)
+    wp, wn = _arg_ws(ws, dev)
+    kp = _arg(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", dev)
+    _check(lib().bkv_compact_mx(ctypes.byref(d), ctypes.byref(cp), kp, wp, wn, torch._C._cuda_getCurrentRawStream(dev)),
+           "bkv_compact_mx")
+
+
+def evict_mass_mx(d: Dims, cache: MxCache, mass, ws, kept=None, fill: bool = False):
+    """evict_mass() of a 4-bit cache."""
+    dev = _device_of(mass, "mass")
+    cp = _arg_mx(d, cache, dev)
+    mp = _arg(mass, (d.B, d.Hkv, d.N_cap), torch.float32, "mass", dev)
+    op = None if kept is None else _arg(kept, (d.B, d.Hkv, d.n_keep), torch.int32, "kept", dev)
+    wp, wn = _arg_ws(ws, dev)
+    st = lib().bkv_evict_mass_mx(ctypes.byref(d), EVICT_FILL if fill else 0, ctypes.byref(cp), mp, op, wp, wn,
+                                 torch._C._cuda_getCurrentRawStream(dev))
+    _check(st, "bkv_evict_mass_mx")
 
 
 # ---- appending a step's rows -------------------------------------------------------

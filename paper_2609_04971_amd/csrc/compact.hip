@@ -18,8 +18,12 @@
 // segment writes), so the hand-off needs no cache maintenance: a segment's
 // loads have returned before its flag is stored, and a writer stores only
 // after it has seen the flag.
+//
+// A 4-bit cache's rows are D/2 bytes of codes, moved as above, and 2 or 4 bytes
+// of scales: with 128 rows a segment, K and V, one to each thread.
 #include "device_common.h"
 #include "internal.h"
+#include "mx.h"
 
 namespace bkv {
 namespace {
@@ -35,10 +39,14 @@ struct Args {
     int* flags;  // [P][nseg] read-done flags
     int P, budget, N, n_keep, nseg, total;
     size_t head_stride;  // bytes between heads (N_cap * row bytes)
+    uint8_t* KS;         // a 4-bit cache's scales, N_cap rows a head
+    uint8_t* VS;
+    int N_cap;
 };
 
-// RB = row bytes (D * element size); VPR = 16-byte vectors per row.
-template <int RB>
+// RB = row bytes (D * element size); VPR = 16-byte vectors per row; SB = bytes
+// of scales per row (0: none).
+template <int RB, int SB>
 __global__ __launch_bounds__(kThreads) void compact_kernel(Args a) {
     constexpr int VPR = RB / 16;
     constexpr int NV = 2 * kSegRows * VPR / kThreads;  // vectors per thread (K and V)
@@ -98,6 +106,15 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Args a) {
             }
         });
     }
+    typedef std::conditional_t<SB == 4, uint32_t, uint16_t> Scales;
+    static_assert(SB == 0 || 2 * kSegRows == kThreads, "a row of scales to a thread");
+    Scales* sh = nullptr;
+    Scales scales = 0;
+    const int sr = tid % kSegRows;
+    if constexpr (SB != 0) {
+        sh = reinterpret_cast<Scales*>(tid < kSegRows ? a.KS : a.VS) + (size_t)h * a.N_cap;
+        if (move && sr < rows && s_src[sr] != i0 + sr) scales = sh[s_src[sr]];
+    }
     // Every load of the workgroup has returned before the flag goes up.
     dev::wait_all_memory();
     __syncthreads();
@@ -131,6 +148,8 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Args a) {
                     __builtin_nontemporal_store(buf[k], reinterpret_cast<dev::u32x4*>(base + (size_t)(i0 + r) * RB) + v);
                 }
             });
+            if constexpr (SB != 0)
+                if (sr < rows && s_src[sr] != i0 + sr) sh[i0 + sr] = scales;
         }
     }
     // The last item to finish clears the control block for the next launch.
@@ -148,10 +167,10 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Args a) {
 
 }  // namespace
 
-hipError_t launch_compact(const bkv_dims& d, const WsLayout& L, void* K, void* V, const int32_t* kept, void* ws,
-                          hipStream_t s) {
+static Args compact_args(const bkv_dims& d, const WsLayout& L, void* K, void* V, int row_bytes, const int32_t* kept,
+                         void* ws) {
     char* w = static_cast<char*>(ws);
-    Args a;
+    Args a{};
     a.K = static_cast<char*>(K);
     a.V = static_cast<char*>(V);
     a.kept = kept;
@@ -164,16 +183,52 @@ hipError_t launch_compact(const bkv_dims& d, const WsLayout& L, void* K, void* V
     a.n_keep = d.N < d.budget ? d.N : d.budget;
     a.nseg = (a.n_keep + kSegRows - 1) / kSegRows;
     a.total = a.P * a.nseg;
-    const int es = d.dtype == BKV_BF16 ? 2 : 4;
-    const int rb = d.D * es;
-    a.head_stride = (size_t)d.N_cap * rb;
+    a.head_stride = (size_t)d.N_cap * row_bytes;
+    a.N_cap = d.N_cap;
+    return a;
+}
+
+hipError_t launch_compact(const bkv_dims& d, const WsLayout& L, void* K, void* V, const int32_t* kept, void* ws,
+                          hipStream_t s) {
+    const int rb = d.D * (d.dtype == BKV_BF16 ? 2 : 4);
+    const Args a = compact_args(d, L, K, V, rb, kept, ws);
     if (a.total == 0) return hipSuccess;
     switch (rb) {
-        case 128: hipLaunchKernelGGL(compact_kernel<128>, dim3(a.total), dim3(kThreads), 0, s, a); break;
-        case 256: hipLaunchKernelGGL(compact_kernel<256>, dim3(a.total), dim3(kThreads), 0, s, a); break;
-        default: hipLaunchKernelGGL(compact_kernel<512>, dim3(a.total), dim3(kThreads), 0, s, a); break;
+        case 128: hipLaunchKernelGGL((compact_kernel<128, 0>), dim3(a.total), dim3(kThreads), 0, s, a); break;
+        case 256: hipLaunchKernelGGL((compact_kernel<256, 0>), dim3(a.total), dim3(kThreads), 0, s, a); break;
+        default: hipLaunchKernelGGL((compact_kernel<512, 0>), dim3(a.total), dim3(kThreads), 0, s, a); break;
     }
     return hipGetLastError();
 }
 
+hipError_t launch_compact_mx(const bkv_dims& d, const WsLayout& L, const bkv_mx_cache& c, const int32_t* kept, void* ws,
+                             hipStream_t s) {
+    Args a = compact_args(d, L, c.K, c.V, d.D / 2, kept, ws);
+    if (a.total == 0) return hipSuccess;
+    a.KS = c.KS;
+    a.VS = c.VS;
+    if (d.D == 128)
+        hipLaunchKernelGGL((compact_kernel<64, 4>), dim3(a.total), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((compact_kernel<32, 2>), dim3(a.total), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
 }  // namespace bkv
+
+extern "C" bkv_status bkv_compact_mx(const bkv_dims* d, const bkv_mx_cache* cache, const int32_t* kept, void* ws,
+                                     size_t ws_bytes, hipStream_t stream) {
+    using namespace bkv;
+    const bkv_status st = bkv_validate(d, BKV_OP_COMPACT);
+    if (st != BKV_OK) return st;
+    if (d->B == 0 || d->N == 0) return BKV_OK;
+    if (!cache || !kept || !mx::whole(*cache)) return BKV_ERR_INVALID;
+    const WsLayout L = ws_layout(*d);
+    if (!ws || ws_bytes < L.ctl_end || (reinterpret_cast<uintptr_t>(ws) & 15u)) return BKV_ERR_WORKSPACE;
+    const size_t tokens = (size_t)(L.P - 1) * d->N_cap + d->N;  // of the last head those that are there
+    const size_t codes = tokens * (d->D / 2), scales = tokens * (d->D / mx::kBlock);
+    const Span spans[] = {{cache->K, codes}, {cache->KS, scales}, {cache->V, codes}, {cache->VS, scales}, {ws, L.ctl_end},
+                          {kept, (size_t)L.P * (d->N < d->budget ? d->N : d->budget) * sizeof(int32_t)}};
+    if (!apart(spans, 6, 5)) return BKV_ERR_INVALID;
+    return launch_compact_mx(*d, L, *cache, kept, ws, stream) == hipSuccess ? BKV_OK : BKV_ERR_HIP;
+}

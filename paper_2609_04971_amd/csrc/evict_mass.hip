@@ -24,6 +24,7 @@
 // or few moves, and a second launch otherwise.
 #include "device_common.h"
 #include "internal.h"
+#include "mx.h"
 
 namespace bkv {
 namespace {
@@ -46,7 +47,7 @@ constexpr int kOwnMoves = kBins / 2;  // moves that the selecting workgroup's li
 constexpr int kCopyThreads = 256;
 constexpr int kCopyMoves = 64;  // rows per copy item
 
-enum Mode { kOrder, kFill, kFillCopy };
+enum Mode { kOrder, kFill, kFillCopy, kFillCopyMx };  // (the last of a 4-bit cache)
 
 struct MassArgs {
     float* mass;
@@ -68,6 +69,9 @@ struct MassArgs {
     char* V;
     size_t head_stride;  // bytes between heads
     int vec_shift;       // log2 of 16-byte vectors per row
+    uint8_t* KS;         // a 4-bit cache's scales, N_cap rows a head
+    uint8_t* VS;
+    int scale_bytes;     // of a row, 2 or 4
 };
 
 // Exclusive scan of one int per thread over the workgroup; *total is the sum.
@@ -132,6 +136,19 @@ __device__ __forceinline__ void move_rows(char* K, char* V, const int* src, cons
                 __builtin_nontemporal_store(b[decltype(kc)::value], reinterpret_cast<dev::u32x4*>(to));
             }
         });
+    }
+}
+
+// The same moves of a 4-bit cache's scales, head h.
+template <int NT>
+__device__ __forceinline__ void move_scales(const MassArgs& a, int h, const int* src, const int* dst, int n) {
+    for (int e = threadIdx.x; e < 2 * n; e += NT) {
+        uint8_t* head = (e & 1 ? a.VS : a.KS) + (size_t)h * a.N_cap * a.scale_bytes;
+        const size_t from = src[e >> 1], to = dst[e >> 1];
+        if (a.scale_bytes == 4)
+            reinterpret_cast<uint32_t*>(head)[to] = reinterpret_cast<const uint32_t*>(head)[from];
+        else
+            reinterpret_cast<uint16_t*>(head)[to] = reinterpret_cast<const uint16_t*>(head)[from];
     }
 }
 
@@ -346,10 +363,11 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
     } else {
         // kept rows from n on, in order, go to the holes below n, in order
         const int c = runs[n >> 6] + __builtin_popcountll(ballots[n >> 6] & ((1ull << (n & 63)) - 1ull));  // kept below n
-        int* src = MODE == kFillCopy ? hist : a.mv_src + (size_t)h * a.max_moves;
-        int* dst = MODE == kFillCopy ? hist + kOwnMoves : a.mv_dst + (size_t)h * a.max_moves;
+        constexpr bool kOwn = MODE == kFillCopy || MODE == kFillCopyMx;
+        int* src = kOwn ? hist : a.mv_src + (size_t)h * a.max_moves;
+        int* dst = kOwn ? hist + kOwnMoves : a.mv_dst + (size_t)h * a.max_moves;
         // a moved mass waits in its move's slot of dst until its hole's thread takes it
-        int* mv = MODE == kFillCopy ? dst : a.mv_val + (size_t)h * a.max_moves;
+        int* mv = kOwn ? dst : a.mv_val + (size_t)h * a.max_moves;
         each([&](int run, int j, float v) {
             const unsigned long long k = ballots[run];
             if (j >= n && ((k >> lane) & 1)) {
@@ -372,10 +390,11 @@ __global__ __launch_bounds__(NT) void mass_select_kernel(MassArgs a) {
             kept[j] = from;
         });
         if (MODE == kFill && tid == 0) a.mv_n[h] = n - c;
-        if constexpr (MODE == kFillCopy) {
+        if constexpr (kOwn) {
             __syncthreads();
             move_rows<NT>(a.K + (size_t)h * a.head_stride, a.V + (size_t)h * a.head_stride, src, dst, n - c, a.vec_shift);
         }
+        if constexpr (MODE == kFillCopyMx) move_scales<NT>(a, h, src, dst, n - c);
     }
     if (PER == 0) __syncthreads();  // every mass has been read
     for (int j = n + tid; j < N; j += NT) mass[j] = 0.f;  // the rows that the next tokens take
@@ -389,21 +408,27 @@ __global__ void mass_identity_kernel(int32_t* kept, int n, long long total) {
 
 // The moves of the hole-filling layout where there are few heads: kCopyMoves
 // of a head's list a workgroup.
+template <bool MX>
 __global__ __launch_bounds__(kCopyThreads) void mass_copy_kernel(MassArgs a, int nchunk) {
     if (!dev::stamp_ok(a.hdr, a.P, a.budget)) return;  // the lists were not written
     const int h = blockIdx.x / nchunk, m0 = (blockIdx.x - h * nchunk) * kCopyMoves;
     const size_t at = (size_t)h * a.max_moves + m0;
     move_rows<kCopyThreads>(a.K + (size_t)h * a.head_stride, a.V + (size_t)h * a.head_stride, a.mv_src + at,
                             a.mv_dst + at, min(kCopyMoves, a.mv_n[h] - m0), a.vec_shift);
+    if (MX) move_scales<kCopyThreads>(a, h, a.mv_src + at, a.mv_dst + at, min(kCopyMoves, a.mv_n[h] - m0));
 }
 
 template <int NT, int PER>
 hipError_t select(const MassArgs& a, int P, int mode, hipStream_t s) {
-    constexpr int kFilling = NT == kShortThreads ? kFillCopy : kFill;
+    const dim3 grid((unsigned)P), block(NT);
     if (mode == kOrder)
-        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kOrder>), dim3((unsigned)P), dim3(NT), 0, s, a);
+        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kOrder>), grid, block, 0, s, a);
+    else if constexpr (NT != kShortThreads)
+        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kFill>), grid, block, 0, s, a);
+    else if (a.KS)
+        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kFillCopyMx>), grid, block, 0, s, a);
     else
-        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kFilling>), dim3((unsigned)P), dim3(NT), 0, s, a);
+        hipLaunchKernelGGL((mass_select_kernel<NT, PER, kFillCopy>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
@@ -444,26 +469,17 @@ MassLayout mass_layout(const bkv_dims& d) {
     return m;
 }
 
-}  // namespace
-}  // namespace bkv
-
-extern "C" {
-
-size_t bkv_mass_workspace_bytes(const bkv_dims* d) {
-    using namespace bkv;
-    if (bkv_validate(d, BKV_OP_COMPACT) != BKV_OK) return 0;
-    return mass_layout(*d).end;
-}
-
-bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, float* mass, int32_t* kept, void* ws,
-                          size_t ws_bytes, hipStream_t stream) {
-    using namespace bkv;
+// K, V and, of a 4-bit cache, KS and VS.
+bkv_status evict_run(const bkv_dims* d, int32_t flags, const bkv_mx_cache& c, bool four, float* mass, int32_t* kept, void* ws,
+                     size_t ws_bytes, hipStream_t stream) {
+    void *K = c.K, *V = c.V;
     if (flags & ~BKV_EVICT_FILL) return BKV_ERR_INVALID;
     const bkv_status st = bkv_validate(d, BKV_OP_COMPACT);
     if (st != BKV_OK) return st;
     if (d->B == 0 || d->N == 0) return BKV_OK;
     if (!K || !V || !mass || ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15u))
         return BKV_ERR_INVALID;
+    if (four && !mx::whole(c)) return BKV_ERR_INVALID;
     // every launch's threads are counted in 32 bits
     if ((long long)d->B * d->Hkv > 0xffffffffLL / kLongThreads) return BKV_ERR_SHAPE;
     const MassLayout m = mass_layout(*d);
@@ -472,11 +488,13 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     const int P = d->B * d->Hkv;
     const int n = d->N < d->budget ? d->N : d->budget;
     if (d->N <= d->budget && !kept) return BKV_OK;
-    const int rb = d->D * (d->dtype == BKV_BF16 ? 2 : 4);
+    const int rb = four ? d->D / 2 : d->D * (d->dtype == BKV_BF16 ? 2 : 4), sb = four ? d->D / mx::kBlock : 0;
     const size_t tokens = (size_t)(P - 1) * d->N_cap + d->N;  // of the last head those that are there
     const Span k = {K, tokens * rb}, v = {V, tokens * rb};
-    const Span spans[] = {{mass, tokens * sizeof(float)}, {kept, (size_t)P * n * sizeof(int32_t)}, {ws, m.end}, k, v};
-    if (!apart(spans, 5, 3)) return BKV_ERR_INVALID;
+    const Span spans[] = {{mass, tokens * sizeof(float)}, {kept, (size_t)P * n * sizeof(int32_t)}, {ws, m.end}, k, v,
+                          {c.KS, tokens * sb}, {c.VS, tokens * sb}};
+    if (!apart(spans, 7, 3)) return BKV_ERR_INVALID;
+    if (four && !apart(spans + 3, 4, 4)) return BKV_ERR_INVALID;
     // K and V may be one array, whose rows then move once more to the same places,
     // or take turns, the tokens of one behind the other's in every head's rows
     const size_t head = (size_t)d->N_cap * rb, used = (size_t)d->N * rb;
@@ -489,7 +507,7 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
                            dim3(kCopyThreads), 0, stream, kept, n, total);
         return hipGetLastError() == hipSuccess ? BKV_OK : BKV_ERR_HIP;
     }
-    MassArgs a;
+    MassArgs a{};
     a.mass = mass;
     a.kept = kept ? kept : reinterpret_cast<int32_t*>(w + m.kept);
     a.mv_src = reinterpret_cast<int32_t*>(w + m.src);
@@ -511,7 +529,12 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     a.K = static_cast<char*>(K);
     a.V = static_cast<char*>(V);
     a.head_stride = (size_t)d->N_cap * rb;
-    a.vec_shift = rb == 128 ? 3 : rb == 256 ? 4 : 5;
+    for (a.vec_shift = 0; 16 << a.vec_shift < rb;) ++a.vec_shift;
+    if (four) {
+        a.KS = c.KS;
+        a.VS = c.VS;
+        a.scale_bytes = sb;
+    }
     const bool fill = flags & BKV_EVICT_FILL;
     const int most = n < a.N - n ? n : a.N - n;  // moves of a head at most
     const int nchunk = (most + kCopyMoves - 1) / kCopyMoves;
@@ -535,11 +558,39 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
     else
         e = select<kLongThreads, 0>(a, P, mode, stream);
     if (e != hipSuccess) return BKV_ERR_HIP;
-    if (mode == kOrder)
-        return launch_compact(*d, ws_layout(*d), K, V, a.kept, ws, stream) == hipSuccess ? BKV_OK : BKV_ERR_HIP;
-    if (mode == kFill)
-        hipLaunchKernelGGL(mass_copy_kernel, dim3((unsigned)(P * nchunk)), dim3(kCopyThreads), 0, stream, a, nchunk);
+    if (mode == kOrder) {
+        e = four ? launch_compact_mx(*d, ws_layout(*d), c, a.kept, ws, stream)
+                 : launch_compact(*d, ws_layout(*d), K, V, a.kept, ws, stream);
+        return e == hipSuccess ? BKV_OK : BKV_ERR_HIP;
+    }
+    const dim3 copies((unsigned)(P * nchunk));
+    if (mode == kFill && four)
+        hipLaunchKernelGGL(mass_copy_kernel<true>, copies, dim3(kCopyThreads), 0, stream, a, nchunk);
+    else if (mode == kFill)
+        hipLaunchKernelGGL(mass_copy_kernel<false>, copies, dim3(kCopyThreads), 0, stream, a, nchunk);
     return hipGetLastError() == hipSuccess ? BKV_OK : BKV_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace bkv
+
+extern "C" {
+
+size_t bkv_mass_workspace_bytes(const bkv_dims* d) {
+    using namespace bkv;
+    if (bkv_validate(d, BKV_OP_COMPACT) != BKV_OK) return 0;
+    return mass_layout(*d).end;
+}
+
+bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, float* mass, int32_t* kept, void* ws,
+                          size_t ws_bytes, hipStream_t stream) {
+    const bkv_mx_cache c = {static_cast<uint8_t*>(K), nullptr, static_cast<uint8_t*>(V), nullptr};
+    return bkv::evict_run(d, flags, c, false, mass, kept, ws, ws_bytes, stream);
+}
+
+bkv_status bkv_evict_mass_mx(const bkv_dims* d, int32_t flags, const bkv_mx_cache* cache, float* mass, int32_t* kept, void* ws,
+                             size_t ws_bytes, hipStream_t stream) {
+    return bkv::evict_run(d, flags, cache ? *cache : bkv_mx_cache{}, true, mass, kept, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

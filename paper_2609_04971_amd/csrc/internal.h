@@ -222,6 +222,9 @@ hipError_t launch_compact_fill(const bkv_dims& d, void* K, void* V, const int32_
 
 hipError_t launch_compact(const bkv_dims& d, const WsLayout& L, void* K, void* V,
                           const int32_t* kept, void* ws, hipStream_t s);
+// The same of a 4-bit cache.
+hipError_t launch_compact_mx(const bkv_dims& d, const WsLayout& L, const bkv_mx_cache& c,
+                             const int32_t* kept, void* ws, hipStream_t s);
 
 // FPS over H heads of src [H][src_rows][D], k = min(m, n) picks per head;
 // dst (optional) receives the picked rows, counts (optional) the occupancy.

@@ -22,6 +22,14 @@ struct Row {
     static constexpr int kScales = D / kBlock;  // bytes
 };
 
+// Whether a cache has all of its arrays, aligned.
+inline bool whole(const bkv_mx_cache& c) {
+    const uintptr_t all[] = {(uintptr_t)c.K, (uintptr_t)c.KS, (uintptr_t)c.V, (uintptr_t)c.VS};
+    for (uintptr_t p : all)
+        if (!p || (p & 15u)) return false;
+    return true;
+}
+
 // 2^e of a block's byte.
 __device__ __forceinline__ float scale(unsigned byte) { return __uint_as_float(byte << 23); }
 
