@@ -25,35 +25,54 @@ __device__ __forceinline__ MxSrc mx_rows(const void* codes, const uint8_t* bytes
 
 // What the two types share: a lane's part of one key, kW words of codes, and of
 // one value row, D/16 coordinates.
+// A group's rows are read through a descriptor that ends behind the last key:
+// what lies there reads as zeros (a value of 0), so that no row has to be clamped
+// and all addresses are a uniform base and lane offsets that never change.
 template <int D>
 struct MxRows {
     static constexpr int kW = D / 32, kDV = D / 16;
     static constexpr int kCodes = mx::Row<D>::kCodes, kScales = mx::Row<D>::kScales;
     struct Key { unsigned c[kW], s; };
     struct Value { unsigned c, s; };
-    __device__ __forceinline__ static Key key(MxSrc p, long long row, int g) {
-        Key k;
-        const unsigned* c = reinterpret_cast<const unsigned*>(p.c + row * kCodes + (kCodes / 4) * g);
-        if constexpr (kW == 4) {
-            const dev::u32x4 x = *reinterpret_cast<const dev::u32x4*>(c);
-            dev::static_for<4>([&](auto i) { k.c[decltype(i)::value] = x[decltype(i)::value]; });
-        } else {
-            const u32x2 x = *reinterpret_cast<const u32x2*>(c);
-            dev::static_for<2>([&](auto i) { k.c[decltype(i)::value] = x[decltype(i)::value]; });
+    struct Off { int kc, ks, vc, vs; };  // of key m and value row 4 g
+    __device__ __forceinline__ static Off offsets(int lane) {
+        const int m = lane & 15, g = lane >> 4;
+        return {m * kCodes + kCodes / 4 * g, m * kScales + g * kScales / 4, 4 * g * kCodes + kDV / 2 * m,
+                4 * g * kScales + m * kScales / 16};
+    }
+#if defined(__HIP_DEVICE_COMPILE__)
+    // Rows [k0, k0 + rows), of which those up to `last` are there.
+    struct Group {
+        __amdgpu_buffer_rsrc_t c, s;
+        __device__ __forceinline__ Group(MxSrc p, int k0, int rows, int last) {
+            k0 = __builtin_amdgcn_readfirstlane(k0);  // (uniform as it is)
+            const int n = __builtin_amdgcn_readfirstlane(max(0, min(rows, last + 1 - k0)));
+            c = __builtin_amdgcn_make_buffer_rsrc((void*)(p.c + (long long)k0 * kCodes), (short)0, n * kCodes, 0x00020000);
+            s = __builtin_amdgcn_make_buffer_rsrc((void*)(p.s + (long long)k0 * kScales), (short)0, n * kScales, 0x00020000);
         }
-        k.s = p.s[row * kScales + g * kScales / 4];
-        return k;
-    }
-    __device__ __forceinline__ static Value value(MxSrc p, long long row, int m) {
-        Value v;
-        const uint8_t* c = p.c + row * kCodes + (kDV / 2) * m;
-        if constexpr (kDV == 8)
-            v.c = *reinterpret_cast<const unsigned*>(c);
-        else
-            v.c = *reinterpret_cast<const uint16_t*>(c);
-        v.s = p.s[row * kScales + m * kScales / 16];
-        return v;
-    }
+        __device__ __forceinline__ Key key(int row, Off o) const {
+            Key k;
+            if constexpr (kW == 4) {
+                const dev::u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(c, o.kc + row * kCodes, 0, 0);
+                dev::static_for<4>([&](auto i) { k.c[decltype(i)::value] = x[decltype(i)::value]; });
+            } else {
+                const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(c, o.kc + row * kCodes, 0, 0);
+                dev::static_for<2>([&](auto i) { k.c[decltype(i)::value] = x[decltype(i)::value]; });
+            }
+            k.s = __builtin_amdgcn_raw_buffer_load_b8(s, o.ks + row * kScales, 0, 0);
+            return k;
+        }
+        __device__ __forceinline__ Value value(int row, Off o) const {
+            Value v;
+            if constexpr (kDV == 8)
+                v.c = __builtin_amdgcn_raw_buffer_load_b32(c, o.vc + row * kCodes, 0, 0);
+            else
+                v.c = __builtin_amdgcn_raw_buffer_load_b16(c, o.vc + row * kCodes, 0, 0);
+            v.s = __builtin_amdgcn_raw_buffer_load_b8(s, o.vs + row * kScales, 0, 0);
+            return v;
+        }
+    };
+#endif
 };
 
 // bf16 queries.
@@ -68,21 +87,22 @@ struct Mx : Bf16<D> {
     __device__ static Src keys(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.K, a.KS, row); }
     __device__ static Src values_of(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.V, a.VS, row); }
     __device__ static int chunk(int kk, int g) { return D / 4 * g + 8 * kk; }
-    struct Off {};
-    __device__ static Off offsets(int) { return {}; }
-    __device__ static void load_k(K& k, Src p, int k0, int last, Off, int lane) {
-        const int m = lane & 15, g = lane >> 4;
-        dev::static_for<kTiles>([&](auto ac) {
-            constexpr int a = decltype(ac)::value;
-            k.k[a] = R::key(p, min(k0 + 16 * a + m, last), g);
-        });
+    using Off = typename R::Off;
+    __device__ static Off offsets(int lane) { return R::offsets(lane); }
+    __device__ static void load_k(K& k, Src p, int k0, int last, Off o, int) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const typename R::Group x(p, k0, kKeys, last);
+        dev::static_for<kTiles>([&](auto ac) { k.k[decltype(ac)::value] = x.key(16 * decltype(ac)::value, o); });
+#endif
     }
-    __device__ static void load_v(V& v, Src p, int k0, int last, Off, int lane) {
-        const int m = lane & 15, g = lane >> 4;
+    __device__ static void load_v(V& v, Src p, int k0, int last, Off o, int) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const typename R::Group x(p, k0, kKeys, last);
         dev::static_for<8>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
-            v.v[j] = R::value(p, min(k0 + 16 * (j / 4) + 4 * g + j % 4, last), m);
+            v.v[j] = x.value(16 * (j / 4) + j % 4, o);
         });
+#endif
     }
     __device__ static typename P::K plain(const K& k) {
         typename P::K x;
@@ -106,6 +126,47 @@ struct Mx : Bf16<D> {
     }
 };
 
+// The streaming kernel takes 64 keys at a time: a wave's requests under way are
+// then 8.5 KB, and the search for maxima and the branches come half as often.
+template <int D>
+struct MxWide : Mx<D> {
+    using M = Mx<D>;
+    static constexpr int kKeys = 2 * M::kKeys, kTiles = 2 * M::kTiles, kDV = M::kDV;
+    static constexpr bool kLazy = true;
+    struct K { typename M::K h[2]; };
+    struct V { typename M::V h[2]; };
+    typedef MxSrc Src;
+    using Off = typename M::Off;
+    __device__ static void load_k(K& k, Src p, int k0, int last, Off o, int lane) {
+        M::load_k(k.h[0], p, k0, last, o, lane);
+        M::load_k(k.h[1], p, k0 + M::kKeys, last, o, lane);
+    }
+    __device__ static void load_v(V& v, Src p, int k0, int last, Off o, int lane) {
+        M::load_v(v.h[0], p, k0, last, o, lane);
+        M::load_v(v.h[1], p, k0 + M::kKeys, last, o, lane);
+    }
+    __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const typename M::P::Q& q) {
+        dev::static_for<2>([&](auto hc) {
+            constexpr int h = decltype(hc)::value;
+            f32x4 x[M::kTiles];
+            M::logits(x, k.h[h], q);
+            dev::static_for<M::kTiles>([&](auto c) { s[M::kTiles * h + decltype(c)::value] = x[decltype(c)::value]; });
+        });
+    }
+    template <int NR, int RT>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
+        dev::static_for<2>([&](auto hc) {
+            constexpr int h = decltype(hc)::value;
+            f32x4 x[RT][M::kTiles];
+            dev::static_for<NR * M::kTiles>([&](auto c) {
+                constexpr int r = decltype(c)::value / M::kTiles, t = decltype(c)::value % M::kTiles;
+                x[r][t] = p[r][M::kTiles * h + t];
+            });
+            M::template values<NR>(o, v.h[h], x);
+        });
+    }
+};
+
 // fp32 queries.
 template <int D>
 struct MxF32 : F32<D> {
@@ -118,16 +179,18 @@ struct MxF32 : F32<D> {
     __device__ static Src keys(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.K, a.KS, row); }
     __device__ static Src values_of(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.V, a.VS, row); }
     __device__ static int chunk(int kk, int g) { return D / 4 * g + 4 * kk; }
-    struct Off {};
-    __device__ static Off offsets(int) { return {}; }
-    __device__ static void load_k(K& k, Src p, int k0, int last, Off, int lane) {
-        k.k = R::key(p, min(k0 + (lane & 15), last), lane >> 4);
+    using Off = typename R::Off;
+    __device__ static Off offsets(int lane) { return R::offsets(lane); }
+    __device__ static void load_k(K& k, Src p, int k0, int last, Off o, int) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        k.k = typename R::Group(p, k0, kKeys, last).key(0, o);
+#endif
     }
-    __device__ static void load_v(V& v, Src p, int k0, int last, Off, int lane) {
-        dev::static_for<4>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            v.v[j] = R::value(p, min(k0 + 4 * (lane >> 4) + j, last), lane & 15);
-        });
+    __device__ static void load_v(V& v, Src p, int k0, int last, Off o, int) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const typename R::Group x(p, k0, kKeys, last);
+        dev::static_for<4>([&](auto jc) { v.v[decltype(jc)::value] = x.value(decltype(jc)::value, o); });
+#endif
     }
     // Half of a word: four coordinates.
     template <int H>
@@ -159,7 +222,7 @@ struct MxF32 : F32<D> {
 
 hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, bool wide, hipStream_t s) {
     using namespace attend;
-    if (dtype == BKV_BF16) return a.D == 128 ? stream<Mx<128>, 128>(a, wide, s) : stream<Mx<64>, 64>(a, wide, s);
+    if (dtype == BKV_BF16) return a.D == 128 ? stream<MxWide<128>, 128>(a, wide, s) : stream<MxWide<64>, 64>(a, wide, s);
     return a.D == 128 ? stream<MxF32<128>, 128>(a, wide, s) : stream<MxF32<64>, 64>(a, wide, s);
 }
 hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s) {

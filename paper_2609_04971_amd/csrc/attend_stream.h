@@ -41,6 +41,7 @@ template <int D>
 struct Bf16 {
     typedef uint16_t elem;
     static constexpr int kKeys = 32;    // keys per group
+    static constexpr bool kLazy = false;  // maxima are looked for only where weights get large
     static constexpr int kTiles = 2;    // S tiles of 16 keys
     static constexpr int kKK = D / 32;  // 16-byte loads per lane and key tile
     static constexpr int kDV = D / 16;
@@ -168,6 +169,7 @@ template <int D>
 struct F32 {
     typedef float elem;
     static constexpr int kKeys = 16;
+    static constexpr bool kLazy = false;
     static constexpr int kTiles = 1;
     static constexpr int kKK = D / 16;
     static constexpr int kDV = D / 16;
@@ -256,6 +258,7 @@ __device__ __forceinline__ typename E::Q load_q(const Args& a, const Row& x, boo
     return q;
 }
 
+constexpr float kMost = 1024.f;  // of a lane's weights of one group, where maxima are lazy
 constexpr int kKeptRows = 32;  // rows per unit of kept logits, at most
 
 // Four tokens' weights of one row; what a row that sees nothing has (norm
@@ -383,6 +386,58 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
             });
             E::load_k(kr, K, key(k0 + KG * kWaves), last, off, lane);
             const bool edge = WIN ? at0 + KG > least || (at0 < most - a.window && at0 + KG > a.sinks) : k0 + KG > min(least, k_hi);
+            if constexpr (E::kLazy) {
+                // weights against the running maximum as it stands (floats: they may be
+                // far above 1); only where a row's new ones sum to more than kMost, as the
+                // first group's do, is the maximum looked for and all brought down to it
+                if (edge)
+                    dev::static_for<NR * NT * 4>([&](auto ic) {
+                        constexpr int rt = decltype(ic)::value / (NT * 4), ti = decltype(ic)::value / 4 % NT, i = decltype(ic)::value % 4;
+                        const int j = at0 + 16 * ti + 4 * g + i;
+                        if (j >= min(lim[rt], WIN ? most : k_hi) || (WIN && j < lim[rt] - a.window && j >= a.sinks))
+                            p[rt][ti][i] = -INFINITY;
+                    });
+                dev::static_for<NR>([&](auto rc) {
+                    constexpr int rt = decltype(rc)::value;
+                    if (keep && 16 * rt + col < sg.rows)
+                        dev::static_for<NT>([&](auto tc) {
+                            constexpr int ti = decltype(tc)::value;
+                            const int at = k0 + 16 * ti + 4 * g;
+                            if (at >= k_hi) return;  // a group may end behind the rows' room
+                            if (keep == kKeepLds)
+                                *(lds_f32x4*)(s_l + ((16 * rt + col) * lds_stride + (at - k_lo))) = p[rt][ti] * a.scale2;
+                            else
+                                *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = p[rt][ti] * a.scale2;
+                        });
+                    f32x4 e[NT];
+                    float sum;
+                    auto weights = [&]() __attribute__((always_inline)) {
+                        sum = 0.f;
+                        dev::static_for<NT * 4>([&](auto ic) {
+                            constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                            e[ti][i] = exp2_hw(__builtin_fmaf(p[rt][ti][i], a.scale2, -m[rt]));
+                            sum += e[ti][i];
+                        });
+                    };
+                    weights();
+                    if (__any(!(sum <= kMost))) {
+                        float top = p[rt][0][0];
+                        dev::static_for<NT * 4 - 1>([&](auto ic) {
+                            constexpr int x = decltype(ic)::value + 1;
+                            top = fmaxf(top, p[rt][x / 4][x % 4]);
+                        });
+                        top = fmaxf(top, dev::shfl_xor_f(top, 16));
+                        top = fmaxf(top, dev::shfl_xor_f(top, 32)) * a.scale2;
+                        const float mn = fmaxf(m[rt], top), f = exp2_hw(m[rt] - mn);
+                        m[rt] = mn;
+                        z[rt] *= f;
+                        dev::static_for<DV>([&](auto dc) { o[rt][decltype(dc)::value] *= f; });
+                        weights();
+                    }
+                    z[rt] += sum;
+                    dev::static_for<NT>([&](auto tc) { p[rt][decltype(tc)::value] = e[decltype(tc)::value]; });
+                });
+            } else {
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 float top = kLowest;
@@ -422,6 +477,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     z[rt] += e;
                 });
             });
+            }
             E::template values<NR>(o, vr, p);
             E::load_v(vr, V, key(k0 + KG * kWaves), last, off, lane);
         }
