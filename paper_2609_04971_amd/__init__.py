@@ -468,27 +468,25 @@ def mx_cache(d: Dims, device="cuda") -> MxCache:
 def _arg_mx(d, cache, dev):
     if not isinstance(cache, MxCache):
         raise ValueError("cache must be an MxCache")
-    p = _MxPtrs()
-    for name, n in (("K", d.D // 2), ("KS", d.D // 32), ("V", d.D // 2), ("VS", d.D // 32)):
-        setattr(p, name, _arg(getattr(cache, name), (d.B, d.Hkv, d.N_cap, n), torch.uint8, "cache." + name, dev))
-    return p
+    K, KS, V, VS = cache
+    rows, D, u8 = (d.B, d.Hkv, d.N_cap), d.D, torch.uint8
+    codes, scales = (*rows, D // 2), (*rows, D // 32)
+    return _MxPtrs(_arg(K, codes, u8, "cache.K", dev), _arg(KS, scales, u8, "cache.KS", dev), _arg(V, codes, u8, "cache.V", dev),
+                   _arg(VS, scales, u8, "cache.VS", dev))
 
 
 def _mx_args(d, k, v, cache, at):
-    t = k if k is not None else v
+    t, name = (k, "k") if k is not None else (v, "v")
     if t is None:
         raise ValueError("k or v is required")
-    dev = _device_of(t, "k" if k is not None else "v")
+    dev = _device_of(t, name)
     if t.dim() != 4:
-        raise ValueError("k and v must be tensors [B, Hkv, T, D]")
-    T, dt = t.shape[2], _tdtype(d)
-    shape = (d.B, d.Hkv, T, d.D)
+        raise ValueError(f"{name} must be a tensor [B, Hkv, T, D]")
+    B, T, dt = d.B, t.shape[2], _tdtype(d)
+    shape = (B, d.Hkv, T, d.D)
     kp = None if k is None else _arg(k, shape, dt, "k", dev)
     vp = None if v is None else _arg(v, shape, dt, "v", dev)
-    if isinstance(at, torch.Tensor):
-        first, ap = 0, _arg(at, (d.B,), torch.int32, "at", dev)
-    else:
-        first, ap = int(at), None
+    first, ap = (0, _arg(at, (B,), torch.int32, "at", dev)) if isinstance(at, torch.Tensor) else (at, None)
     return kp, vp, T, first, ap, _arg_mx(d, cache, dev), torch._C._cuda_getCurrentRawStream(dev)
 
 

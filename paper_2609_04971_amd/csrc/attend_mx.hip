@@ -114,7 +114,13 @@ struct Mx : Bf16<D> {
         });
         return x;
     }
-    __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const typename P::Q& q) { P::logits(s, plain(k), q); }
+    static constexpr bool kLazy = true;
+    // The keys against the first NR row tiles.
+    template <int NR, int RT>
+    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, const typename P::Q (&q)[RT]) {
+        const typename P::K x = plain(k);
+        dev::static_for<NR>([&](auto rc) { P::logits(s[decltype(rc)::value], x, q[decltype(rc)::value]); });
+    }
     template <int NR, int RT>
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
         typename P::V x;
@@ -132,7 +138,6 @@ template <int D>
 struct MxWide : Mx<D> {
     using M = Mx<D>;
     static constexpr int kKeys = 2 * M::kKeys, kTiles = 2 * M::kTiles, kDV = M::kDV;
-    static constexpr bool kLazy = true;
     struct K { typename M::K h[2]; };
     struct V { typename M::V h[2]; };
     typedef MxSrc Src;
@@ -145,12 +150,16 @@ struct MxWide : Mx<D> {
         M::load_v(v.h[0], p, k0, last, o, lane);
         M::load_v(v.h[1], p, k0 + M::kKeys, last, o, lane);
     }
-    __device__ static void logits(f32x4 (&s)[kTiles], const K& k, const typename M::P::Q& q) {
+    template <int NR, int RT>
+    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, const typename M::P::Q (&q)[RT]) {
         dev::static_for<2>([&](auto hc) {
             constexpr int h = decltype(hc)::value;
-            f32x4 x[M::kTiles];
-            M::logits(x, k.h[h], q);
-            dev::static_for<M::kTiles>([&](auto c) { s[M::kTiles * h + decltype(c)::value] = x[decltype(c)::value]; });
+            f32x4 x[RT][M::kTiles];
+            M::template logits_rows<NR>(x, k.h[h], q);
+            dev::static_for<NR * M::kTiles>([&](auto c) {
+                constexpr int r = decltype(c)::value / M::kTiles, t = decltype(c)::value % M::kTiles;
+                s[r][M::kTiles * h + t] = x[r][t];
+            });
         });
     }
     template <int NR, int RT>

@@ -380,10 +380,13 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         for (; k0 < k_hi; k0 += KG * kWaves) {
             const int at0 = key(k0);
             f32x4 p[RT][NT];
-            dev::static_for<NR>([&](auto rc) {
-                constexpr int rt = decltype(rc)::value;
-                E::logits(p[rt], kr, q[rt]);
-            });
+            if constexpr (E::kLazy)
+                E::template logits_rows<NR>(p, kr, q);
+            else
+                dev::static_for<NR>([&](auto rc) {
+                    constexpr int rt = decltype(rc)::value;
+                    E::logits(p[rt], kr, q[rt]);
+                });
             E::load_k(kr, K, key(k0 + KG * kWaves), last, off, lane);
             const bool edge = WIN ? at0 + KG > least || (at0 < most - a.window && at0 + KG > a.sinks) : k0 + KG > min(least, k_hi);
             if constexpr (E::kLazy) {
@@ -676,20 +679,21 @@ hipError_t row_mass(const Args& a, int ns, int chunk, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <class E, int D>
-hipError_t stream(const Args& a, bool wide, hipStream_t s) {
+template <class E, int D, bool WIN>
+hipError_t stream_as(const Args& a, bool wide, hipStream_t s) {
     const long long items = a.items0 + (long long)a.seg[1].units * a.seg[1].nrb * a.seg[1].ns;
     if (items == 0) return hipSuccess;
     const dim3 grid((unsigned)items), block(kThreads);
-    if (a.window > 0 && wide)
-        hipLaunchKernelGGL((stream_kernel<E, D, 2, true>), grid, block, stream_lds(a), s, a);
-    else if (a.window > 0)
-        hipLaunchKernelGGL((stream_kernel<E, D, 1, true>), grid, block, stream_lds(a), s, a);
-    else if (wide)
-        hipLaunchKernelGGL((stream_kernel<E, D, 2, false>), grid, block, stream_lds(a), s, a);
+    if (wide)
+        hipLaunchKernelGGL((stream_kernel<E, D, 2, WIN>), grid, block, stream_lds(a), s, a);
     else
-        hipLaunchKernelGGL((stream_kernel<E, D, 1, false>), grid, block, stream_lds(a), s, a);
+        hipLaunchKernelGGL((stream_kernel<E, D, 1, WIN>), grid, block, stream_lds(a), s, a);
     return hipGetLastError();
+}
+
+template <class E, int D>
+hipError_t stream(const Args& a, bool wide, hipStream_t s) {
+    return a.window > 0 ? stream_as<E, D, true>(a, wide, s) : stream_as<E, D, false>(a, wide, s);
 }
 
 }  // namespace

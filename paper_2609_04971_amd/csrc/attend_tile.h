@@ -127,15 +127,7 @@ struct Bf16 {
     __device__ __forceinline__ static Src values_of(const Args&, const Segment& sg, long long row) {
         return static_cast<const elem*>(sg.V) + row * D;
     }
-    // Rows [k0, k_hi) of a tile on their way into LDS; nothing is left to do when
-    // the tile before has been worked off.
-    struct Stage {
-        __device__ __forceinline__ void fetch(Src K, Src V, int k0, int k_hi, elem* ks, elem* vs, int wave, int lane) {
-            load_tile<Bf16, kKeys>(K + (long long)k0 * D, k_hi - k0, ks, wave, lane);
-            load_tile<Bf16, kKeys>(V + (long long)k0 * D, k_hi - k0, vs, wave, lane);
-        }
-        __device__ __forceinline__ void commit(elem*, elem*, int, int) {}
-    };
+    static constexpr int kStages = 0;  // tiles go straight into LDS
     // Chunk 2 kk + h of a key.
     struct KeyAt {
         const elem* p;
@@ -404,9 +396,13 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
     const int k_lo = split * chunk, k_hi = min(k_lo + chunk, all);
     auto key = [&](int v) { return WIN ? w.key(v) : v; };  // the key at a place
     const typename E::Src K = E::keys(a, sg, (long long)unit * sg.cap), V = E::values_of(a, sg, (long long)unit * sg.cap);
-    typename E::Stage stage;
     auto load = [&](int k0, elem* ks, elem* vs) {
-        if (k0 < k_hi) stage.fetch(K, V, key(k0), WIN ? key(k_hi - 1) + 1 : k_hi, ks, vs, wave, lane);
+        if constexpr (E::kStages == 0)
+            if (k0 < k_hi) {
+                const int k = key(k0), rows = (WIN ? key(k_hi - 1) + 1 : k_hi) - k;
+                load_tile<E, kKeys>(K + (long long)k * D, rows, ks, wave, lane);
+                load_tile<E, kKeys>(V + (long long)k * D, rows, vs, wave, lane);
+            }
     };
     const RowAt<E> at_k(lane);
     const typename E::Values at_v = E::values(lane);
@@ -421,18 +417,36 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
             tile_step<E, false>(st, at_k, at_v, ks, vs, k0, min(lim, k_hi), k0 + kKeys > min(least, k_hi), a.scale2, lane);
         }
     };
-    load(k_lo, k_a, v_a);
-    if (k_lo < k_hi) stage.commit(k_a, v_a, wave, lane);
-    for (int k0 = k_lo; k0 < k_hi; k0 += 2 * kKeys) {
-        turn();  // tile a has landed, tile b is free
-        load(k0 + kKeys, k_b, v_b);
-        step(k0, k_a, v_a);
-        if (k0 + kKeys >= k_hi) break;
-        stage.commit(k_b, v_b, wave, lane);
-        turn();
-        load(k0 + 2 * kKeys, k_a, v_a);
-        step(k0 + kKeys, k_b, v_b);
-        if (k0 + 2 * kKeys < k_hi) stage.commit(k_a, v_a, wave, lane);
+    if constexpr (E::kStages == 0) {
+        load(k_lo, k_a, v_a);
+        for (int k0 = k_lo; k0 < k_hi; k0 += 2 * kKeys) {
+            turn();  // tile a has landed, tile b is free
+            load(k0 + kKeys, k_b, v_b);
+            step(k0, k_a, v_a);
+            if (k0 + kKeys >= k_hi) break;
+            turn();
+            load(k0 + 2 * kKeys, k_a, v_a);
+            step(k0 + kKeys, k_b, v_b);
+        }
+    } else {
+        // the next tile on its way in registers while one is worked off
+        typename E::Stage next;
+        auto fetch = [&](int k0) {
+            if (k0 < k_hi) next.fetch(K, V, key(k0), WIN ? key(k_hi - 1) + 1 : k_hi, wave, lane);
+        };
+        fetch(k_lo);
+        if (k_lo < k_hi) next.commit(k_a, v_a, wave, lane);
+        for (int k0 = k_lo; k0 < k_hi; k0 += 2 * kKeys) {
+            __syncthreads();  // tile a is whole, tile b is free
+            fetch(k0 + kKeys);
+            step(k0, k_a, v_a);
+            if (k0 + kKeys >= k_hi) break;
+            next.commit(k_b, v_b, wave, lane);
+            __syncthreads();
+            fetch(k0 + 2 * kKeys);
+            step(k0 + kKeys, k_b, v_b);
+            if (k0 + 2 * kKeys < k_hi) next.commit(k_a, v_a, wave, lane);
+        }
     }
     if (!valid) return;
     const auto zr = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.z), __float_as_uint(st.z), false, false);

@@ -39,6 +39,7 @@ struct Mx : Bf16<D_> {
     }
     // D 128: a block of the keys and one of the values a thread.  D 64: one block,
     // waves 0 and 1 the keys', 2 and 3 the values'.
+    static constexpr int kStages = 1;
     struct Stage {
         static constexpr int kSides = kKeys * (D / mx::kBlock) / 128;  // of K and V that a thread takes blocks of
         dev::u32x4 c[kSides];
@@ -50,7 +51,7 @@ struct Mx : Bf16<D_> {
         }
         __device__ __forceinline__ static int block(int lane) { return lane & (D / mx::kBlock - 1); }
         // rows at or past k_hi repeat the last one: nothing behind a sequence is read
-        __device__ __forceinline__ void fetch(Src K, Src V, int k0, int k_hi, elem*, elem*, int wave, int lane) {
+        __device__ __forceinline__ void fetch(Src K, Src V, int k0, int k_hi, int wave, int lane) {
             const long long r = min(k0 + row(wave, lane), k_hi - 1);
             const int b = block(lane);
             dev::static_for<kSides>([&](auto ic) {
@@ -62,14 +63,17 @@ struct Mx : Bf16<D_> {
             });
         }
         __device__ __forceinline__ void commit(elem* ks, elem* vs, int wave, int lane) {
-            const int r = row(wave, lane), b = block(lane);
+            // the four chunks' places, worked out anew for every tile: kept, as they are
+            // for each of four arrays, they would cost 16 registers
+            int r = row(wave, lane), b = 4 * block(lane);
+            asm volatile("" : "+v"(r), "+v"(b));
             dev::static_for<kSides>([&](auto ic) {
                 constexpr int i = decltype(ic)::value;
                 elem* stage = (kSides == 2 ? i == 1 : wave >= 2) ? vs : ks;
                 const float x = mx::scale(s[i]);
                 dev::static_for<4>([&](auto jc) {
                     constexpr int j = decltype(jc)::value;
-                    *reinterpret_cast<dev::u32x4*>(stage + r * D + ((4 * b + j) ^ swz<P>(r)) * 8) = mx::eight_bf16(c[i][j], x);
+                    *reinterpret_cast<dev::u32x4*>(stage + r * D + ((b + j) ^ swz<P>(r)) * 8) = mx::eight_bf16(c[i][j], x);
                 });
             });
         }
