@@ -26,6 +26,12 @@ constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a 
 // 7.9 / 9.9; fp32 D 64 256 6.5 / 7.4 and 7.6 / 9.8, 512 9.5 / 9.3 and 7.6 / 9.9; D
 // 128 256 9.2 / 9.0 and 9.3 / 9.8, 384 11.6 / 11.5 and 9.5 / 10.3).
 constexpr long long kWhole = 128 << 10;
+// The same of a 4-bit cache in bf16: keys, whose bytes are not what takes the time
+// (us launched one by one, in one piece and split, 8 heads: D 128 1024 tokens 9.0 and
+// 10.9, 1500 10.7 and 10.9, 2048 12.9 and 10.9; D 64 1024 8.8 and 10.8, 2048 10.9 and
+// 10.9).  fp32 ones are as plain ones (D 64 512 10.4 and 10.8, D 128 256 9.5 and 10.7,
+// 512 15.3 and 10.8).
+constexpr int kWholeMx = 1280;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
 // Items of 32 rows and kMinChunk keys up to which a prefix of more rows is
@@ -171,7 +177,7 @@ Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
         // a short cache goes in one piece: joining splits would be a launch of
         // its own.  Not by the mass: outputs do not depend on whether it is asked for
         const bool whole = groups == 0 && !p.own_tile &&
-                           (long long)N * (c.mx ? d.D / 2 + d.D / mx::kBlock : d.D * (d.dtype == BKV_BF16 ? 2 : 4)) <= kWhole;
+                           (c.mx && tiles ? N <= kWholeMx : (long long)N * d.D * (tiles ? 2 : 4) <= kWhole);
         const bool prompt = p.own_tile && c.causal && c.window == 0 && T <= N && T > N / 5;
         own_ns = whole    ? 1
                  : prompt ? prompt_splits(own, N, T, rows, d.D)
