@@ -43,6 +43,14 @@ every mode and before any eviction, into `out` [LB, Hq, D] (and `lse`); mode
 that is held once and never evicted (bkv_attend_shared): the B sequences are
 samples of one prompt, and what each of them writes is its own cache.
 
+cache="mx" holds keys and values in 4 bits (bkv_store_mx), in every mode: tokens
+are stored as they come, attention reads the 4-bit rows (bkv_attend_mx), and
+evictions move them (bkv_evict_mass_mx, bkv_compact_mx).  The scoring modes
+score each layer on its keys' plain values, read back (bkv_load_mx) into one
+layer's scratch.  window > 0, with attention=True: a step sees the last `window`
+cached tokens up to its own and the first `sinks` ones (bkv_attend_window); it
+counts cached tokens, so those that evictions took leave the window.
+
 compaction "fill" evicts with bkv_score, bkv_topk and bkv_compact_fill
 instead of bkv_evict_ex: the cache keeps the same rows but only the kept
 rows past B_min move (into the evicted rows below it), so rows are no
@@ -65,7 +73,7 @@ class PeriodicEviction:
     def __init__(self, layers: int, B: int, Hq: int, Hkv: int, D: int, B_max: int, rope_table, n_beacon: int = 16,
                  n_recent: int = 16, n_prefix: int = 0, mode: str = "beacon", dtype=torch.bfloat16,
                  device="cuda", record: bool = False, timing: bool = False, compaction: str = "order",
-                 attention: bool = False):
+                 attention: bool = False, cache: str = "plain", window: int = 0, sinks: int = 0):
         """rope_table(t) -> (cos, sin), fp32 [D/2] device tensors of the
         model's rotate-half RoPE at absolute position t (the beacons are
         rotated to the step at which eviction runs).  record keeps every
@@ -77,6 +85,17 @@ class PeriodicEviction:
             raise ValueError("B_max must be a multiple of 8 (B_min = 7/8 B_max)")
         if compaction not in ("order", "fill"):
             raise ValueError("compaction is 'order' or 'fill'")
+        if cache not in ("plain", "mx"):
+            raise ValueError("cache is 'plain' or 'mx'")
+        if cache == "mx" and compaction == "fill" and mode != "mass":
+            raise ValueError("the scoring modes compact a 4-bit cache in order")
+        if window < 0 or sinks < 0:
+            raise ValueError("window and sinks are not negative")
+        if window and (not attention or mode == "mass"):
+            raise ValueError("a window needs attention=True, and sums no weights for mode 'mass'")
+        if window and compaction == "fill":
+            raise ValueError("a window needs the tokens in order")
+        self.window, self.sinks = window, sinks
         self.compaction = compaction
         self.mode = mode
         self.layers = layers
@@ -91,8 +110,11 @@ class PeriodicEviction:
         self.rope_table = rope_table
         dt, dev = dtype, device
         LB = self.LB
-        self.K = torch.zeros(LB, Hkv, B_max, D, dtype=dt, device=dev)
-        self.V = torch.zeros_like(self.K)
+        self.dt = dt
+        self.K = self.V = self.cache = None  # keys and values, or both in 4 bits
+        if cache == "plain":
+            self.K = torch.zeros(LB, Hkv, B_max, D, dtype=dt, device=dev)
+            self.V = torch.zeros_like(self.K)
         self.L = 0  # cached tokens per head
         self.t = 0  # absolute position of the next token
         nb, nr = self.nb, self.nr
@@ -107,8 +129,14 @@ class PeriodicEviction:
         self.dims = bkv.dims(B=LB, Hq=Hq, Hkv=Hkv, D=D, N=B_max, N_cap=B_max, W=nr, C=self.G * nb,
                              budget=self.B_min, n_prefix=n_prefix, dtype="bf16" if dt == torch.bfloat16 else "fp32")
         self.mass = torch.zeros(LB, Hkv, B_max, dtype=torch.float32, device=dev) if mode == "mass" else None
+        if cache == "mx":
+            self.cache = bkv.mx_cache(self.dims, device=dev)
+            if mode != "mass":  # scoring, one layer at a time
+                self.ldims = self.dims.replace(B=B)
+                self.lkeys = torch.empty(B, Hkv, B_max, D, dtype=dt, device=dev)
+                self.lws = bkv.workspace(self.ldims, bkv.OP_SCORE, device=dev)
         self.ws = bkv.mass_workspace(self.dims, device=dev) if mode == "mass" else \
-            bkv.workspace(self.dims, bkv.OP_EVICT, device=dev)
+            bkv.workspace(self.dims, bkv.OP_EVICT if cache == "plain" else bkv.OP_COMPACT, device=dev)
         self.kept = torch.empty(LB, Hkv, self.B_min, dtype=torch.int32, device=dev)
         # top-k output before filling
         self.sel = torch.empty_like(self.kept) if compaction == "fill" and mode != "mass" else None
@@ -153,6 +181,8 @@ class PeriodicEviction:
         prefill; the sequences' own tokens start at position P."""
         if not self.attention:
             raise ValueError("a shared prefix needs attention=True or mode 'mass'")
+        if self.cache is not None or self.window:
+            raise ValueError("a shared prefix goes with a plain cache and no window")
         if self.t != 0:
             raise ValueError("the prefix comes before every other token")
         if K.shape != V.shape or K.dim() != 4 or tuple(K.shape[:2]) != (self.layers, self.Hkv) or K.shape[3] != self.D:
@@ -167,7 +197,13 @@ class PeriodicEviction:
     def _attend(self, q, out, lse, ws):
         self.adims.N = self.L
         kw = {"lse": lse, "mass": self.mass, "causal": True}
-        if self.prefix is None:
+        if self.cache is not None:
+            kw |= {"window": self.window, "sinks": self.sinks}
+            self._call("attend", lambda: bkv.attend_mx(self.adims, q, self.cache, out, ws, **kw))
+        elif self.window:
+            self._call("attend", lambda: bkv.attend_window(self.adims, q, self.K, self.V, out, ws, self.window, sinks=self.sinks,
+                                                           lse=lse))
+        elif self.prefix is None:
             self._call("attend", lambda: bkv.attend(self.adims, q, self.K, self.V, out, ws, **kw))
         else:
             self._call("attend", lambda: bkv.attend_shared(self.adims, q, *self.prefix, self.K, self.V, out, ws, **kw))
@@ -185,11 +221,14 @@ class PeriodicEviction:
             raise ValueError("mode 'mass' needs the prompt's post-RoPE queries")
         if self.attention and q_rope is not None:
             want = (self.LB, self.Hq, T, self.D)
-            if tuple(q_rope.shape) != want or q_rope.dtype != self.K.dtype or q_rope.device != self.K.device:
-                raise ValueError(f"q_rope must be {want}, {self.K.dtype} on {self.K.device}: got {tuple(q_rope.shape)}, "
+            if tuple(q_rope.shape) != want or q_rope.dtype != self.dt or q_rope.device != self.kept.device:
+                raise ValueError(f"q_rope must be {want}, {self.dt} on {self.kept.device}: got {tuple(q_rope.shape)}, "
                                  f"{q_rope.dtype} on {q_rope.device}")
-        self.K[:, :, :T] = K
-        self.V[:, :, :T] = V
+        if self.cache is not None:
+            self._call("store", lambda: bkv.store_mx(self.dims, K.contiguous(), V.contiguous(), self.cache))
+        else:
+            self.K[:, :, :T] = K
+            self.V[:, :, :T] = V
         self.L = T
         self.t = T + (self.prefix[0].shape[2] if self.prefix else 0)
         if self.mass is not None:
@@ -228,7 +267,12 @@ class PeriodicEviction:
         # the step's rows: the token into the cache, its queries into the
         # buffer (up to the freeze) or into the recent set (after it)
         L, nb, nr = self.L + 1, self.nb, self.nr
-        writes = [(self.K, self.L, k), (self.V, self.L, v)]
+        writes = []
+        if self.cache is None:
+            writes = [(self.K, self.L, k), (self.V, self.L, v)]
+        else:
+            self._call("store", lambda: bkv.store_mx(self.dims, k.unsqueeze(2).contiguous(), v.unsqueeze(2).contiguous(), self.cache,
+                                                     self.L))
         recent = self.B_max - nr < L <= self.B_max and self.mode != "mass"
         if recent:
             writes += [(self.recent_rope, self.n_rec, q_rope), (self.recent_pre, self.n_rec, q_pre)]
@@ -263,17 +307,36 @@ class PeriodicEviction:
             return True
         return False
 
+    def _evict_mx(self, rc, rs):
+        """Scores of every layer's keys as the 4-bit cache holds them, one
+        selection, one compaction."""
+        B = self.ldims.B
+        for i in range(self.layers):
+            at = slice(i * B, (i + 1) * B)
+            bkv.load_mx(self.ldims, bkv.MxCache(*(x[at] for x in self.cache)), self.lkeys, None)
+            bkv.score(self.ldims, self.lkeys, self.recent_rope[at], self.beacons[at], self.counts[at], self.scores[at], self.lws,
+                      rope_cos=rc, rope_sin=rs)
+        bkv.topk(self.dims, self.scores, self.kept)
+        bkv.compact_mx(self.dims, self.cache, self.kept, self.ws)
+
     def _evict(self):
-        pre = (self.K.clone(), self.V.clone()) if self.record else None
+        pre = None
+        if self.record:
+            pre = (self.K.clone(), self.V.clone()) if self.cache is None else bkv.MxCache(*(x.clone() for x in self.cache))
         if self.mode == "mass":
             mass = self.mass.clone() if self.record else None
-            self._call("evict", lambda: bkv.evict_mass(self.dims, self.K, self.V, self.mass, self.ws, kept=self.kept,
-                                                       fill=self.compaction == "fill"))
+            kw = {"kept": self.kept, "fill": self.compaction == "fill"}
+            if self.cache is None:
+                self._call("evict", lambda: bkv.evict_mass(self.dims, self.K, self.V, self.mass, self.ws, **kw))
+            else:
+                self._call("evict", lambda: bkv.evict_mass_mx(self.dims, self.cache, self.mass, self.ws, **kw))
             self._log("evict", before=pre, mass=mass, kept=self.kept.clone())
             self.L = self.B_min
             return
         rc, rs = self.rope_table(self.t - 1)  # beacons rotated to the current step
-        if self.compaction == "order":
+        if self.cache is not None:
+            self._call("evict", lambda: self._evict_mx(rc, rs))
+        elif self.compaction == "order":
             self._call("evict", lambda: bkv.evict(self.dims, self.K, self.V, self.recent_rope, self.beacons,
                                                   self.counts, self.ws, kept=self.kept, scores=self.scores,
                                                   rope_cos=rc, rope_sin=rs))
