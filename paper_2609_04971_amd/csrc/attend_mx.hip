@@ -121,14 +121,24 @@ struct Mx : Bf16<D> {
         const typename P::K x = plain(k);
         dev::static_for<NR>([&](auto rc) { P::logits(s[decltype(rc)::value], x, q[decltype(rc)::value]); });
     }
-    template <int NR, int RT>
-    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
+    // next: the codes are operands now, and the next ones may be requested.
+    template <int NR, int RT, class F>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles], F&& next) {
+        const typename P::V x = plain_values(v);
+        next(std::integral_constant<int, 0>{});
+        P::template values<NR>(o, x, p);
+    }
+    template <int H>
+    __device__ static void load_half(V& v, Src p, int k0, int last, Off o, int lane) {
+        load_v(v, p, k0, last, o, lane);
+    }
+    __device__ static typename P::V plain_values(const V& v) {
         typename P::V x;
         dev::static_for<8 * kDV / 2>([&](auto c) {
             constexpr int j = decltype(c)::value / (kDV / 2), i = decltype(c)::value % (kDV / 2);
             x.v[j][i] = mx::pair_bf16<i>(v.v[j].c, mx::scale(v.v[j].s));
         });
-        P::template values<NR>(o, x, p);
+        return x;
     }
 };
 
@@ -147,8 +157,12 @@ struct MxWide : Mx<D> {
         M::load_k(k.h[1], p, k0 + M::kKeys, last, o, lane);
     }
     __device__ static void load_v(V& v, Src p, int k0, int last, Off o, int lane) {
-        M::load_v(v.h[0], p, k0, last, o, lane);
-        M::load_v(v.h[1], p, k0 + M::kKeys, last, o, lane);
+        load_half<0>(v, p, k0, last, o, lane);
+        load_half<1>(v, p, k0, last, o, lane);
+    }
+    template <int H>
+    __device__ static void load_half(V& v, Src p, int k0, int last, Off o, int lane) {
+        M::load_v(v.h[H], p, k0 + H * M::kKeys, last, o, lane);
     }
     template <int NR, int RT>
     __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, const typename M::P::Q (&q)[RT]) {
@@ -162,16 +176,19 @@ struct MxWide : Mx<D> {
             });
         });
     }
-    template <int NR, int RT>
-    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
+    // next(h): half h's codes are operands now, and the next ones may be requested.
+    template <int NR, int RT, class F>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles], F&& next) {
         dev::static_for<2>([&](auto hc) {
             constexpr int h = decltype(hc)::value;
+            const typename M::P::V plain = M::plain_values(v.h[h]);
+            next(hc);
             f32x4 x[RT][M::kTiles];
             dev::static_for<NR * M::kTiles>([&](auto c) {
                 constexpr int r = decltype(c)::value / M::kTiles, t = decltype(c)::value % M::kTiles;
                 x[r][t] = p[r][M::kTiles * h + t];
             });
-            M::template values<NR>(o, v.h[h], x);
+            M::P::template values<NR>(o, plain, x);
         });
     }
 };
@@ -229,9 +246,19 @@ struct MxF32 : F32<D> {
 }  // namespace
 }  // namespace attend
 
+namespace attend {
+namespace {
+template <int D>
+hipError_t stream_mx(const Args& a, bool wide, hipStream_t s) {
+    if (a.window > 0) return wide ? stream_rows<Mx<D>, D, 2, true>(a, s) : stream_rows<MxWide<D>, D, 1, true>(a, s);
+    return wide ? stream_rows<Mx<D>, D, 2, false>(a, s) : stream_rows<MxWide<D>, D, 1, false>(a, s);
+}
+}  // namespace
+}  // namespace attend
+
 hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, bool wide, hipStream_t s) {
     using namespace attend;
-    if (dtype == BKV_BF16) return a.D == 128 ? stream<MxWide<128>, 128>(a, wide, s) : stream<MxWide<64>, 64>(a, wide, s);
+    if (dtype == BKV_BF16) return a.D == 128 ? stream_mx<128>(a, wide, s) : stream_mx<64>(a, wide, s);
     return a.D == 128 ? stream<MxF32<128>, 128>(a, wide, s) : stream<MxF32<64>, 64>(a, wide, s);
 }
 hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s) {

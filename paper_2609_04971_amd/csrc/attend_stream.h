@@ -486,8 +486,15 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                 });
             });
             }
-            E::template values<NR>(o, vr, p);
-            E::load_v(vr, V, key(k0 + KG * kWaves), last, off, lane);
+            if constexpr (E::kLazy) {
+                E::template values<NR>(o, vr, p, [&](auto hc) __attribute__((always_inline)) {
+                    E::template load_half<decltype(hc)::value>(vr, V, key(k0 + KG * kWaves), last, off, lane);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            } else {
+                E::template values<NR>(o, vr, p);
+                E::load_v(vr, V, key(k0 + KG * kWaves), last, off, lane);
+            }
         }
     };
     if constexpr (RT == 2) {
@@ -686,21 +693,18 @@ hipError_t row_mass(const Args& a, int ns, int chunk, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <class E, int D, bool WIN>
-hipError_t stream_as(const Args& a, bool wide, hipStream_t s) {
+template <class E, int D, int RT, bool WIN>
+hipError_t stream_rows(const Args& a, hipStream_t s) {
     const long long items = a.items0 + (long long)a.seg[1].units * a.seg[1].nrb * a.seg[1].ns;
     if (items == 0) return hipSuccess;
-    const dim3 grid((unsigned)items), block(kThreads);
-    if (wide)
-        hipLaunchKernelGGL((stream_kernel<E, D, 2, WIN>), grid, block, stream_lds(a), s, a);
-    else
-        hipLaunchKernelGGL((stream_kernel<E, D, 1, WIN>), grid, block, stream_lds(a), s, a);
+    hipLaunchKernelGGL((stream_kernel<E, D, RT, WIN>), dim3((unsigned)items), dim3(kThreads), stream_lds(a), s, a);
     return hipGetLastError();
 }
 
 template <class E, int D>
 hipError_t stream(const Args& a, bool wide, hipStream_t s) {
-    return a.window > 0 ? stream_as<E, D, true>(a, wide, s) : stream_as<E, D, false>(a, wide, s);
+    if (a.window > 0) return wide ? stream_rows<E, D, 2, true>(a, s) : stream_rows<E, D, 1, true>(a, s);
+    return wide ? stream_rows<E, D, 2, false>(a, s) : stream_rows<E, D, 1, false>(a, s);
 }
 
 }  // namespace
