@@ -55,6 +55,7 @@ struct Args {
 struct Plan {
     bool own_tile, pre_tile;  // the tile kernel takes the segment
     bool wide;                // the streaming kernel takes 32 rows an item, else 16
+    int rt;                   // on a 4-bit cache: tiles of 16 rows of an item
     int own_nrb, pre_nrb;
     int own_ns, own_chunk, pre_ns, pre_chunk;
     int ns_room;              // partials of a row that the workspace holds
@@ -246,8 +247,8 @@ hipError_t launch_attend_row_mass(const attend::Args& a, int ns, int chunk, hipS
 hipError_t launch_attend_tile_mass(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s);
 hipError_t launch_attend_add_parts(const attend::Args& a, const float* part, int parts, hipStream_t s);
 
-// The same on a 4-bit cache (dtype: the queries').
-hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, bool wide, hipStream_t s);
+// The same on a 4-bit cache (dtype: the queries'; streamed, 16 rt rows an item).
+hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, int rt, hipStream_t s);
 hipError_t launch_attend_tile_mx(const attend::Args& a, const attend::Segment& sg, hipStream_t s);
 hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s);
 hipError_t launch_attend_tile_mass_mx(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s);

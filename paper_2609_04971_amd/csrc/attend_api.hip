@@ -34,6 +34,11 @@ constexpr long long kWhole = 128 << 10;
 constexpr int kWholeMx = 1280;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
+// Rows per unit up to which a 4-bit cache's keys are streamed.  In tiles only as
+// many waves as there are 32 rows have work, and keys are a quarter of the
+// bytes, so that this bounds.
+constexpr int kFewMxRows = 64;
+
 // Items of 32 rows and kMinChunk keys up to which a prefix of more rows is
 // streamed all the same, in one launch with the sequences' own caches: its keys
 // are read by every row block, but from L2, and the tiles' launch is spared.  Up
@@ -71,11 +76,23 @@ int most_splits(long long base, int n) {
 // 64 50, 96 53, 256 57; 192 x 4000 1 78, 3 78, 4* 67, 6 76; 160 x 6000 (ragged)
 // 2 105, 3* 79, 7 74; 296 x 2000 fp32 1 143, 2 127, 3* 123, 4 119; tile: 112
 // blocks of 500 x 7 queries against 24000 3 146, 4 119, 5 135, 9* 113, 19 138.
-int best_splits(bool tile, long long base, int n, long long rows, int D) {
+// Streamed items of a 4-bit cache and more than 32 rows are bound by their
+// products, as tiles are, and two of them share a compute unit where registers
+// allow it (8 x 4 heads of up to 16001 tokens, ragged: 35 rows 8 29.1, 16* 26.1; 63
+// rows 7 39.8, 8* 37.2, 16 48.6; D 64, 16 x 4 heads of 8000, 64 rows 4 28.2, 8* 23.5).
+struct Items {
+    int resident;  // at once on a compute unit, as far as that shares anything
+    float around;  // keys in the time that an item costs around its own
+};
+Items items_of(const Plan& p, int D, bool mx) {
+    if (p.own_tile) return {D == 128 ? 2 : 3, 100.f};
+    return {mx && (p.rt == 3 || (p.rt == 4 && D == 64)) ? 2 : 1, 64.f};
+}
+int best_splits(Items it, long long base, int n, long long rows, int D) {
     constexpr float kRound[4] = {0.f, 1.f, 1.7f, 2.4f};
     constexpr float kJoinKeys = 43.f * 8.f / 4e6f;  // keys in the time that 8 bytes take at 4 TB/s
-    const int resident = !tile ? 1 : D == 128 ? 2 : 3;
-    const float around = tile ? 100.f : 64.f;
+    const int resident = it.resident;
+    const float around = it.around;
     const int most = most_splits(base, n);
     int best = 1;
     float least = 0.f;
@@ -153,12 +170,13 @@ Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
     const long long rows = (long long)d.B * d.Hq * T;
     const long long pre_rows = groups > 0 ? d.B / groups * R : 0;
     const bool tiles = d.dtype == BKV_BF16;
-    p.own_tile = tiles && R > kFewRows;
+    p.own_tile = tiles && R > (c.mx ? kFewMxRows : kFewRows);
     const long long pre_units = (long long)groups * d.Hkv, few_rb = (pre_rows + 31) / 32;
     const long long few_items = pre_units * few_rb * ((P + kMinChunk - 1) / kMinChunk);
     p.pre_tile = tiles && pre_rows > kFewRows && (p.own_tile || few_items > kFewItems);
     p.wide = (!p.own_tile && R > 16) || (!p.pre_tile && pre_rows > 16);
-    const int own_rb = p.own_tile ? 128 : p.wide ? 32 : 16, pre_rb = p.pre_tile ? 128 : p.wide ? 32 : 16;
+    p.rt = R <= 16 ? 1 : R <= 32 || !tiles ? 2 : (int)((R + 15) / 16);
+    const int own_rb = p.own_tile ? 128 : c.mx ? 16 * p.rt : p.wide ? 32 : 16, pre_rb = p.pre_tile ? 128 : p.wide ? 32 : 16;
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
     const long long own = (long long)d.B * d.Hkv * p.own_nrb, pre = (long long)groups * d.Hkv * p.pre_nrb;
@@ -177,18 +195,18 @@ Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
         // a short cache goes in one piece: joining splits would be a launch of
         // its own.  Not by the mass: outputs do not depend on whether it is asked for
         const bool whole = groups == 0 && !p.own_tile &&
-                           (c.mx && tiles ? N <= kWholeMx : (long long)N * d.D * (tiles ? 2 : 4) <= kWhole);
+                           (c.mx && tiles ? N <= kWholeMx && R <= kFewRows : (long long)N * d.D * (tiles ? 2 : 4) <= kWhole);
         const bool prompt = p.own_tile && c.causal && c.window == 0 && T <= N && T > N / 5;
         own_ns = whole    ? 1
                  : prompt ? prompt_splits(own, N, T, rows, d.D)
-                          : best_splits(p.own_tile, own, N, rows, d.D);
-        if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile, pre, P, rows, d.D);
+                          : best_splits(items_of(p, d.D, c.mx), own, N, rows, d.D);
+        if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile ? Items{d.D == 128 ? 2 : 3, 100.f} : Items{1, 64.f}, pre, P, rows, d.D);
     }
     cut(N, own_ns, &p.own_ns, &p.own_chunk);
     if (groups > 0 && P > 0) cut(P, pre_ns, &p.pre_ns, &p.pre_chunk);
     p.keep = mass && R <= kFewRows;
     if (mass && !p.keep && tiles && R <= kRegRows)
-        cut(d.N, best_splits(false, (long long)d.B * d.Hkv, d.N, 0, d.D), &p.mass_ns, &p.mass_chunk);
+        cut(d.N, best_splits({1, 64.f}, (long long)d.B * d.Hkv, d.N, 0, d.D), &p.mass_ns, &p.mass_chunk);
     size_t off = 0;
     p.part_o = off;
     if (p.ns_room > 1) off = up(off + sizeof(float) * (size_t)rows * p.ns_room * d.D, kAlign);
@@ -362,8 +380,9 @@ bkv_status run(const bkv_dims* d, const Call& c, hipStream_t stream) {
     if (p.own_tile && tile(a, own, stream) != hipSuccess) return BKV_ERR_HIP;
     if (!p.own_tile) {  // rows of the prefix are no fewer than a sequence's own
         a.items0 = p.pre_tile ? 0 : (int)items0;
-        const auto run_stream = c.mx ? launch_attend_stream_mx : launch_attend_stream;
-        if (run_stream(a, d->dtype, p.wide, stream) != hipSuccess) return BKV_ERR_HIP;
+        const hipError_t e = c.mx ? launch_attend_stream_mx(a, d->dtype, p.rt, stream)
+                                  : launch_attend_stream(a, d->dtype, p.wide, stream);
+        if (e != hipSuccess) return BKV_ERR_HIP;
     }
     if (launch_attend_join(a, d->dtype, stream) != hipSuccess) return BKV_ERR_HIP;
     if (p.mass_ns > 0 && d->N > 0) {

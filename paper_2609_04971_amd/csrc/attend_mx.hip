@@ -115,18 +115,18 @@ struct Mx : Bf16<D> {
         return x;
     }
     static constexpr bool kLazy = true;
-    // The keys against the first NR row tiles.
-    template <int NR, int RT>
-    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, const typename P::Q (&q)[RT]) {
+    // The keys against the first NR row tiles; query(r): tile r's operands.
+    template <int NR, int RT, class F>
+    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, F&& query) {
         const typename P::K x = plain(k);
-        dev::static_for<NR>([&](auto rc) { P::logits(s[decltype(rc)::value], x, q[decltype(rc)::value]); });
+        dev::static_for<NR>([&](auto rc) { P::logits(s[decltype(rc)::value], x, query(rc)); });
     }
     // next: the codes are operands now, and the next ones may be requested.
     template <int NR, int RT, class F>
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles], F&& next) {
         const typename P::V x = plain_values(v);
         next(std::integral_constant<int, 0>{});
-        P::template values<NR>(o, x, p);
+        P::template values<NR, RT, (RT > 2)>(o, x, p);
     }
     template <int H>
     __device__ static void load_half(V& v, Src p, int k0, int last, Off o, int lane) {
@@ -164,12 +164,12 @@ struct MxWide : Mx<D> {
     __device__ static void load_half(V& v, Src p, int k0, int last, Off o, int lane) {
         M::load_v(v.h[H], p, k0 + H * M::kKeys, last, o, lane);
     }
-    template <int NR, int RT>
-    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, const typename M::P::Q (&q)[RT]) {
+    template <int NR, int RT, class F>
+    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const K& k, F&& query) {
         dev::static_for<2>([&](auto hc) {
             constexpr int h = decltype(hc)::value;
             f32x4 x[RT][M::kTiles];
-            M::template logits_rows<NR>(x, k.h[h], q);
+            M::template logits_rows<NR>(x, k.h[h], query);
             dev::static_for<NR * M::kTiles>([&](auto c) {
                 constexpr int r = decltype(c)::value / M::kTiles, t = decltype(c)::value % M::kTiles;
                 s[r][M::kTiles * h + t] = x[r][t];
@@ -248,18 +248,23 @@ struct MxF32 : F32<D> {
 
 namespace attend {
 namespace {
-template <int D>
-hipError_t stream_mx(const Args& a, bool wide, hipStream_t s) {
-    if (a.window > 0) return wide ? stream_rows<Mx<D>, D, 2, true>(a, s) : stream_rows<MxWide<D>, D, 1, true>(a, s);
-    return wide ? stream_rows<Mx<D>, D, 2, false>(a, s) : stream_rows<MxWide<D>, D, 1, false>(a, s);
+template <int D, bool WIN>
+hipError_t stream_mx(const Args& a, int rt, hipStream_t s) {
+    switch (rt) {
+        case 1: return stream_rows<MxWide<D>, D, 1, WIN>(a, s);
+        case 2: return stream_rows<Mx<D>, D, 2, WIN>(a, s);
+        case 3: return stream_rows<Mx<D>, D, 3, WIN>(a, s);
+        default: return stream_rows<Mx<D>, D, 4, WIN>(a, s);
+    }
 }
 }  // namespace
 }  // namespace attend
 
-hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, bool wide, hipStream_t s) {
+hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, int rt, hipStream_t s) {
     using namespace attend;
-    if (dtype == BKV_BF16) return a.D == 128 ? stream_mx<128>(a, wide, s) : stream_mx<64>(a, wide, s);
-    return a.D == 128 ? stream<MxF32<128>, 128>(a, wide, s) : stream<MxF32<64>, 64>(a, wide, s);
+    if (dtype == BKV_F32) return a.D == 128 ? stream<MxF32<128>, 128>(a, rt > 1, s) : stream<MxF32<64>, 64>(a, rt > 1, s);
+    if (a.window > 0) return a.D == 128 ? stream_mx<128, true>(a, rt, s) : stream_mx<64, true>(a, rt, s);
+    return a.D == 128 ? stream_mx<128, false>(a, rt, s) : stream_mx<64, false>(a, rt, s);
 }
 hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s) {
     using namespace attend;

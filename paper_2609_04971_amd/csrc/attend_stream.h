@@ -130,7 +130,8 @@ struct Bf16 {
     // o += V^T P^T.  The weights go in as two bf16 terms, high part and rest,
     // so that their rounding (2^-17) stays below the output's own: the
     // streaming kernel waits for memory, and the second product is free.
-    template <int NR, int RT>
+    // ONE: as one term (2^-8), where rows are so many that the products bound.
+    template <int NR, int RT, bool ONE = false>
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles]) {
         bf16x8_t hi[NR], lo[NR];
         dev::static_for<NR>([&](auto rc) {
@@ -140,7 +141,7 @@ struct Bf16 {
                 const float x = p[rt][j / 4][j % 4];
                 const __bf16 h = (__bf16)x;
                 hi[rt][j] = h;
-                lo[rt][j] = (__bf16)(x - (float)h);
+                if constexpr (!ONE) lo[rt][j] = (__bf16)(x - (float)h);
             });
         });
         dev::static_for<kDV>([&](auto dc) {
@@ -155,7 +156,7 @@ struct Bf16 {
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[rt], o[rt][dd], 0, 0, 0);
-                o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[rt], o[rt][dd], 0, 0, 0);
+                if constexpr (!ONE) o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[rt], o[rt][dd], 0, 0, 0);
             });
         });
     }
@@ -311,6 +312,10 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     // those of the item's keys, [R][chunk + kPadL]
     extern __shared__ __attribute__((aligned(16))) float dyn[];
     __shared__ float s_m[kWaves][16], s_z[kWaves][16], s_norm[kKeptRows];
+    // rows of more tiles than two leave their queries there, a lane's part each
+    constexpr bool kQLds = RT > 2;
+    static_assert(RT <= kWaves, "a wave loads one tile's queries");
+    __shared__ typename E::Q s_q[kQLds ? RT : 1][kQLds ? 64 : 1];
     lds_float* const s_o = (lds_float*)dyn;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -334,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     const int len = unit_len(sg, unit, a.Hkv);
     const int r0 = rb * 16 * RT;
 
-    typename E::Q q[RT];
+    typename E::Q q[kQLds ? 1 : RT];
     int lim[RT];  // keys the lane's row sees
     float m[RT], z[RT];
     f32x4 o[RT][DV];
@@ -344,7 +349,11 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         const int rr = r0 + 16 * rt + col;
         const bool valid = rr < sg.rows;
         const Row x = decode_row(a, unit, sg.seqs, valid ? rr : 0);
-        q[rt] = load_q<E, D>(a, x, valid, g);
+        if constexpr (kQLds) {
+            if (wave == rt) s_q[kQLds ? rt : 0][lane] = load_q<E, D>(a, x, valid, g);
+        } else {
+            q[rt] = load_q<E, D>(a, x, valid, g);
+        }
         lim[rt] = valid ? seen_by(a, sg, len, x.t) : 0x7fffffff;  // a row that is none masks nothing
         most = max(most, valid ? lim[rt] : 0);
         m[rt] = kLowest;
@@ -359,16 +368,29 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     }
     most = __builtin_amdgcn_readfirstlane(most);  // (every lane has them)
     least = __builtin_amdgcn_readfirstlane(least);
-    const int k_lo = split * sg.chunk;
+    int chunk = sg.chunk;
+    if constexpr (kQLds && !WIN)  // splits of a ragged sequence are alike
+        if (sg.lens) chunk = __builtin_amdgcn_readfirstlane(max(128, ((len + sg.ns - 1) / sg.ns + 127) / 128 * 128));
+    const int k_lo = split * chunk;
     // with the logits kept, keys that no row sees are written too (as -inf)
     const int keep = own && !WIN ? a.keep : kKeepNone;
     Walk w{};
     if constexpr (WIN) w = Walk::over<KG>(a, least, most);
-    const int k_hi = min(k_lo + sg.chunk, WIN ? w.n : keep ? len : most);
+    const int k_hi = min(k_lo + chunk, WIN ? w.n : keep ? len : most);
     const typename E::Src K = E::keys(a, sg, (long long)unit * sg.cap), V = E::values_of(a, sg, (long long)unit * sg.cap);
     lds_float* const s_l = s_o + kWaves * a.o_rows * DP;
     const int lds_stride = sg.chunk + kPadL;
     float* const glob = keep ? a.logits + (long long)unit * a.R * a.lstride : nullptr;
+
+    if constexpr (kQLds) __syncthreads();
+    auto query = [&](auto rc) __attribute__((always_inline)) {
+        if constexpr (kQLds) {
+            asm volatile("" ::: "memory");  // or all of them would be kept in registers
+            return s_q[decltype(rc)::value][lane];
+        } else {
+            return q[decltype(rc)::value];
+        }
+    };
 
     // the keys, for the first NR row tiles
     auto walk = [&](auto nc) __attribute__((always_inline)) {
@@ -386,7 +408,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
             const int at0 = key(k0);
             f32x4 p[RT][NT];
             if constexpr (E::kLazy)
-                E::template logits_rows<NR>(p, kr, q);
+                E::template logits_rows<NR>(p, kr, query);
             else
                 dev::static_for<NR>([&](auto rc) {
                     constexpr int rt = decltype(rc)::value;
@@ -503,7 +525,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         else
             walk(std::integral_constant<int, 2>{});
     } else {
-        walk(std::integral_constant<int, 1>{});
+        walk(std::integral_constant<int, RT>{});
     }
 
     // join the waves, one row tile at a time
