@@ -332,7 +332,9 @@ __device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, cons
 // keys and values at 4.8 to 6.0 TB/s.
 // WIN: rows see their windows (causal), and the splits are of the walk's places.
 template <class E, bool WIN>
-__global__ __launch_bounds__(kThreads, 2) void tile_kernel(Args a, Segment sg) {
+constexpr int tile_resident() { return E::D == 64 && (WIN || E::kStages > 0) ? 3 : 2; }
+template <class E, bool WIN>
+__global__ __launch_bounds__(kThreads, (tile_resident<E, WIN>())) void tile_kernel(Args a, Segment sg) {
     using elem = typename E::elem;
     constexpr int D = E::D, DT = D / 32, kKeys = E::kKeys;
     __shared__ __attribute__((aligned(16))) elem k_a[kKeys * D], v_a[kKeys * D], k_b[kKeys * D], v_b[kKeys * D];
