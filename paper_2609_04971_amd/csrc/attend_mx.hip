@@ -126,7 +126,11 @@ struct Mx : Bf16<D> {
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles], F&& next) {
         const typename P::V x = plain_values(v);
         next(std::integral_constant<int, 0>{});
-        P::template values<NR, RT, (RT > 2)>(o, x, p);
+        products<NR>(o, x, p);
+    }
+    template <int NR, int RT>
+    __device__ static void products(f32x4 (&o)[RT][kDV], const typename P::V& v, const f32x4 (&p)[RT][kTiles]) {
+        P::template values<NR, RT, (RT > 2)>(o, v, p);
     }
     template <int H>
     __device__ static void load_half(V& v, Src p, int k0, int last, Off o, int lane) {
@@ -142,11 +146,87 @@ struct Mx : Bf16<D> {
     }
 };
 
-// The streaming kernel takes 64 keys at a time: a wave's requests under way are
-// then 8.5 KB, and the search for maxima and the branches come half as often.
+// fp32 queries.  What the cache holds is exact in bf16, so fp32 operands of the
+// other side go through the bf16 products as three terms of eight bits each, cut
+// off one after another: all 24 bits, at 16 / 3 times the rate of fp32 products.
 template <int D>
-struct MxWide : Mx<D> {
+struct Mx3 : Mx<D> {
     using M = Mx<D>;
+    using P = Bf16<D>;
+    typedef float elem;
+    static constexpr int kTerms = 3, kKK = M::kKK, kTiles = M::kTiles, kDV = M::kDV;
+    struct Q { dev::u32x4 v[kTerms][kKK]; };
+    // The high halves of two floats, and what they leave.
+    __device__ static unsigned cut(float& x, float& y) {
+        const unsigned w = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+        x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+        return w;
+    }
+    __device__ static void query_terms(Q& q, const float* p, bool valid, int g) {
+        dev::static_for<kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            const f32x4* from = reinterpret_cast<const f32x4*>(p + M::chunk(kk, g));
+            f32x4 x[2] = {};
+            if (valid) {
+                x[0] = from[0];
+                x[1] = from[1];
+            }
+            dev::static_for<kTerms * 4>([&](auto ic) {
+                constexpr int t = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                float a = x[i / 2][2 * (i % 2)], b = x[i / 2][2 * (i % 2) + 1];
+                q.v[t][kk][i] = cut(a, b);
+                x[i / 2][2 * (i % 2)] = a;
+                x[i / 2][2 * (i % 2) + 1] = b;
+            });
+        });
+    }
+    template <int NR, int RT, class F>
+    __device__ static void logits_rows(f32x4 (&s)[RT][kTiles], const typename M::K& k, F&& query) {
+        const typename P::K x = M::plain(k);
+        dev::static_for<NR>([&](auto rc) {
+            constexpr int rt = decltype(rc)::value;
+            const Q q = query(rc);
+            f32x4 acc[kTiles] = {};
+            dev::static_for<kTerms * kKK * kTiles>([&](auto c) {  // the smallest terms first
+                constexpr int t = kTerms - 1 - decltype(c)::value / (kKK * kTiles), kk = decltype(c)::value / kTiles % kKK,
+                              a = decltype(c)::value % kTiles;
+                acc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.v[a][kk]),
+                                                                 __builtin_bit_cast(bf16x8_t, q.v[t][kk]), acc[a], 0, 0, 0);
+            });
+            dev::static_for<kTiles>([&](auto ac) { s[rt][decltype(ac)::value] = acc[decltype(ac)::value]; });
+        });
+    }
+    template <int NR, int RT, class F>
+    __device__ static void values(f32x4 (&o)[RT][kDV], const typename M::V& v, const f32x4 (&p)[RT][kTiles], F&& next) {
+        const typename P::V x = M::plain_values(v);
+        next(std::integral_constant<int, 0>{});
+        products<NR>(o, x, p);
+    }
+    template <int NR, int RT>
+    __device__ static void products(f32x4 (&o)[RT][kDV], const typename P::V& v, const f32x4 (&p)[RT][kTiles]) {
+        dev::u32x4 w[NR][kTerms];
+        dev::static_for<NR * 4>([&](auto ic) {
+            constexpr int rt = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+            float a = p[rt][i / 2][2 * (i % 2)], b = p[rt][i / 2][2 * (i % 2) + 1];
+            dev::static_for<kTerms>([&](auto tc) { w[rt][decltype(tc)::value][i] = cut(a, b); });
+        });
+        dev::static_for<kDV>([&](auto dc) {
+            constexpr int dd = decltype(dc)::value;
+            const bf16x8_t a = P::template coordinate<dd>(v);
+            dev::static_for<NR * kTerms>([&](auto rc) {
+                constexpr int rt = decltype(rc)::value / kTerms, t = kTerms - 1 - decltype(rc)::value % kTerms;
+                o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, w[rt][t]), o[rt][dd], 0, 0, 0);
+            });
+        });
+    }
+    __device__ static void store4(elem* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
+};
+
+// One row tile's items take 64 keys at a time: a wave's requests under way are
+// then 8.5 KB, and the search for maxima and the branches come half as often.
+template <class M>
+struct Wide : M {
     static constexpr int kKeys = 2 * M::kKeys, kTiles = 2 * M::kTiles, kDV = M::kDV;
     struct K { typename M::K h[2]; };
     struct V { typename M::V h[2]; };
@@ -181,90 +261,36 @@ struct MxWide : Mx<D> {
     __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][kTiles], F&& next) {
         dev::static_for<2>([&](auto hc) {
             constexpr int h = decltype(hc)::value;
-            const typename M::P::V plain = M::plain_values(v.h[h]);
+            const auto plain = M::plain_values(v.h[h]);
             next(hc);
             f32x4 x[RT][M::kTiles];
             dev::static_for<NR * M::kTiles>([&](auto c) {
                 constexpr int r = decltype(c)::value / M::kTiles, t = decltype(c)::value % M::kTiles;
                 x[r][t] = p[r][M::kTiles * h + t];
             });
-            M::P::template values<NR>(o, plain, x);
+            M::template products<NR>(o, plain, x);
         });
     }
 };
 
-// fp32 queries.
-template <int D>
-struct MxF32 : F32<D> {
-    using P = F32<D>;
-    using R = MxRows<D>;
-    static constexpr int kKeys = P::kKeys, kKK = P::kKK, kDV = P::kDV;
-    struct K { typename R::Key k; };
-    struct V { typename R::Value v[4]; };
-    typedef MxSrc Src;
-    __device__ static Src keys(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.K, a.KS, row); }
-    __device__ static Src values_of(const Args& a, const Segment& sg, long long row) { return mx_rows<D>(sg.V, a.VS, row); }
-    __device__ static int chunk(int kk, int g) { return D / 4 * g + 4 * kk; }
-    using Off = typename R::Off;
-    __device__ static Off offsets(int lane) { return R::offsets(lane); }
-    __device__ static void load_k(K& k, Src p, int k0, int last, Off o, int) {
-#if defined(__HIP_DEVICE_COMPILE__)
-        k.k = typename R::Group(p, k0, kKeys, last).key(0, o);
-#endif
-    }
-    __device__ static void load_v(V& v, Src p, int k0, int last, Off o, int) {
-#if defined(__HIP_DEVICE_COMPILE__)
-        const typename R::Group x(p, k0, kKeys, last);
-        dev::static_for<4>([&](auto jc) { v.v[decltype(jc)::value] = x.value(decltype(jc)::value, o); });
-#endif
-    }
-    // Half of a word: four coordinates.
-    template <int H>
-    __device__ static f32x4 half(unsigned w, float s) {
-        const mx::f32x2 a = mx::pair_f32<2 * H>(w, s), b = mx::pair_f32<2 * H + 1>(w, s);
-        return f32x4{a[0], a[1], b[0], b[1]};
-    }
-    __device__ static void logits(f32x4 (&s)[1], const K& k, const typename P::Q& q) {
-        typename P::K x;
-        dev::static_for<kKK>([&](auto c) {
-            constexpr int kk = decltype(c)::value;
-            x.v[0][kk] = half<kk % 2>(k.k.c[kk / 2], mx::scale(k.k.s));
-        });
-        P::logits(s, x, q);
-    }
-    template <int NR, int RT>
-    __device__ static void values(f32x4 (&o)[RT][kDV], const V& v, const f32x4 (&p)[RT][1]) {
-        typename P::V x;
-        dev::static_for<4 * kDV / 4>([&](auto c) {
-            constexpr int j = decltype(c)::value / (kDV / 4), i = decltype(c)::value % (kDV / 4);
-            x.v[j][i] = half<i>(v.v[j].c, mx::scale(v.v[j].s));
-        });
-        P::template values<NR>(o, x, p);
-    }
-};
-
-}  // namespace
-}  // namespace attend
-
-namespace attend {
-namespace {
 template <int D, bool WIN>
-hipError_t stream_mx(const Args& a, int rt, hipStream_t s) {
+hipError_t stream_mx(const Args& a, int dtype, int rt, hipStream_t s) {
+    if (dtype == BKV_F32) return rt == 1 ? stream_rows<Wide<Mx3<D>>, D, 1, WIN>(a, s) : stream_rows<Mx3<D>, D, 2, WIN>(a, s);
     switch (rt) {
-        case 1: return stream_rows<MxWide<D>, D, 1, WIN>(a, s);
+        case 1: return stream_rows<Wide<Mx<D>>, D, 1, WIN>(a, s);
         case 2: return stream_rows<Mx<D>, D, 2, WIN>(a, s);
         case 3: return stream_rows<Mx<D>, D, 3, WIN>(a, s);
         default: return stream_rows<Mx<D>, D, 4, WIN>(a, s);
     }
 }
+
 }  // namespace
 }  // namespace attend
 
 hipError_t launch_attend_stream_mx(const attend::Args& a, int dtype, int rt, hipStream_t s) {
     using namespace attend;
-    if (dtype == BKV_F32) return a.D == 128 ? stream<MxF32<128>, 128>(a, rt > 1, s) : stream<MxF32<64>, 64>(a, rt > 1, s);
-    if (a.window > 0) return a.D == 128 ? stream_mx<128, true>(a, rt, s) : stream_mx<64, true>(a, rt, s);
-    return a.D == 128 ? stream_mx<128, false>(a, rt, s) : stream_mx<64, false>(a, rt, s);
+    if (a.window > 0) return a.D == 128 ? stream_mx<128, true>(a, dtype, rt, s) : stream_mx<64, true>(a, dtype, rt, s);
+    return a.D == 128 ? stream_mx<128, false>(a, dtype, rt, s) : stream_mx<64, false>(a, dtype, rt, s);
 }
 hipError_t launch_attend_row_mass_mx(const attend::Args& a, int ns, int chunk, hipStream_t s) {
     using namespace attend;

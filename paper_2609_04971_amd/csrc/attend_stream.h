@@ -42,6 +42,7 @@ struct Bf16 {
     typedef uint16_t elem;
     static constexpr int kKeys = 32;    // keys per group
     static constexpr bool kLazy = false;  // maxima are looked for only where weights get large
+    static constexpr int kTerms = 1;      // bf16 terms of a query
     static constexpr int kTiles = 2;    // S tiles of 16 keys
     static constexpr int kKK = D / 32;  // 16-byte loads per lane and key tile
     static constexpr int kDV = D / 16;
@@ -127,6 +128,17 @@ struct Bf16 {
             s[a] = acc;
         });
     }
+    // Coordinate dd of the lane's keys.
+    template <int dd>
+    __device__ static bf16x8_t coordinate(const V& v) {
+        constexpr unsigned sel = dd % 2 ? 0x07060302u : 0x05040100u;  // a half of two registers
+        dev::u32x4 t;
+        dev::static_for<4>([&](auto c) {
+            constexpr int i = decltype(c)::value;
+            t[i] = __builtin_amdgcn_perm(v.v[2 * i + 1][dd / 2], v.v[2 * i][dd / 2], sel);
+        });
+        return __builtin_bit_cast(bf16x8_t, t);
+    }
     // o += V^T P^T.  The weights go in as two bf16 terms, high part and rest,
     // so that their rounding (2^-17) stays below the output's own: the
     // streaming kernel waits for memory, and the second product is free.
@@ -146,13 +158,7 @@ struct Bf16 {
         });
         dev::static_for<kDV>([&](auto dc) {
             constexpr int dd = decltype(dc)::value;
-            constexpr unsigned sel = dd % 2 ? 0x07060302u : 0x05040100u;  // a half of two registers
-            dev::u32x4 t;
-            dev::static_for<4>([&](auto c) {
-                constexpr int i = decltype(c)::value;
-                t[i] = __builtin_amdgcn_perm(v.v[2 * i + 1][dd / 2], v.v[2 * i][dd / 2], sel);
-            });
-            const bf16x8_t a = __builtin_bit_cast(bf16x8_t, t);
+            const bf16x8_t a = coordinate<dd>(v);
             dev::static_for<NR>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value;
                 o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[rt], o[rt][dd], 0, 0, 0);
@@ -171,6 +177,7 @@ struct F32 {
     typedef float elem;
     static constexpr int kKeys = 16;
     static constexpr bool kLazy = false;
+    static constexpr int kTerms = 1;
     static constexpr int kTiles = 1;
     static constexpr int kKK = D / 16;
     static constexpr int kDV = D / 16;
@@ -251,11 +258,14 @@ template <class E, int D>
 __device__ __forceinline__ typename E::Q load_q(const Args& a, const Row& x, bool valid, int g) {
     typename E::Q q;
     const typename E::elem* p = static_cast<const typename E::elem*>(a.q) + x.q;
-    dev::static_for<E::kKK>([&](auto c) {
-        constexpr int kk = decltype(c)::value;
-        typedef std::remove_reference_t<decltype(q.v[0])> V;
-        q.v[kk] = valid ? *reinterpret_cast<const V*>(p + E::chunk(kk, g)) : V{};
-    });
+    if constexpr (E::kTerms > 1)
+        E::query_terms(q, p, valid, g);
+    else
+        dev::static_for<E::kKK>([&](auto c) {
+            constexpr int kk = decltype(c)::value;
+            typedef std::remove_reference_t<decltype(q.v[0])> V;
+            q.v[kk] = valid ? *reinterpret_cast<const V*>(p + E::chunk(kk, g)) : V{};
+        });
     return q;
 }
 
@@ -312,8 +322,9 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     // those of the item's keys, [R][chunk + kPadL]
     extern __shared__ __attribute__((aligned(16))) float dyn[];
     __shared__ float s_m[kWaves][16], s_z[kWaves][16], s_norm[kKeptRows];
-    // rows of more tiles than two leave their queries there, a lane's part each
-    constexpr bool kQLds = RT > 2;
+    // rows of more tiles than two, or one in several terms, leave their queries
+    // there, a lane's part each
+    constexpr bool kQLds = RT > 2 || (RT > 1 && E::kTerms > 1);
     static_assert(RT <= kWaves, "a wave loads one tile's queries");
     __shared__ typename E::Q s_q[kQLds ? RT : 1][kQLds ? 64 : 1];
     lds_float* const s_o = (lds_float*)dyn;
