@@ -156,13 +156,6 @@ struct Mx3 : Mx<D> {
     typedef float elem;
     static constexpr int kTerms = 3, kKK = M::kKK, kTiles = M::kTiles, kDV = M::kDV;
     struct Q { dev::u32x4 v[kTerms][kKK]; };
-    // The high halves of two floats, and what they leave.
-    __device__ static unsigned cut(float& x, float& y) {
-        const unsigned w = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
-        x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-        y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
-        return w;
-    }
     __device__ static void query_terms(Q& q, const float* p, bool valid, int g) {
         dev::static_for<kKK>([&](auto c) {
             constexpr int kk = decltype(c)::value;
@@ -175,7 +168,7 @@ struct Mx3 : Mx<D> {
             dev::static_for<kTerms * 4>([&](auto ic) {
                 constexpr int t = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
                 float a = x[i / 2][2 * (i % 2)], b = x[i / 2][2 * (i % 2) + 1];
-                q.v[t][kk][i] = cut(a, b);
+                q.v[t][kk][i] = mx::cut(a, b);
                 x[i / 2][2 * (i % 2)] = a;
                 x[i / 2][2 * (i % 2) + 1] = b;
             });
@@ -209,7 +202,7 @@ struct Mx3 : Mx<D> {
         dev::static_for<NR * 4>([&](auto ic) {
             constexpr int rt = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
             float a = p[rt][i / 2][2 * (i % 2)], b = p[rt][i / 2][2 * (i % 2) + 1];
-            dev::static_for<kTerms>([&](auto tc) { w[rt][decltype(tc)::value][i] = cut(a, b); });
+            dev::static_for<kTerms>([&](auto tc) { w[rt][decltype(tc)::value][i] = mx::cut(a, b); });
         });
         dev::static_for<kDV>([&](auto dc) {
             constexpr int dd = decltype(dc)::value;

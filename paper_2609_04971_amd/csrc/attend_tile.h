@@ -542,7 +542,7 @@ __global__ __launch_bounds__(kThreads, E::kMassResident) void tile_mass_kernel(A
         const RowAt<E> rows_at = at.opaque();
         dev::static_for<E::KK>([&](auto kc) {
             constexpr int kk = decltype(kc)::value;
-            const typename E::frag q = rows_at.frag(stage + 32 * rw * D, kc);
+            const auto q = rows_at.frag(stage + 32 * rw * D, kc);
             s[0] = E::dot(q, kr[0][kk], s[0]);
             s[1] = E::dot(q, kr[1][kk], s[1]);
         });

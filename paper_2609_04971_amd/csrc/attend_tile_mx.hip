@@ -92,34 +92,69 @@ struct Mx : Bf16<D_> {
     };
 };
 
-// fp32 queries, for the weights' sums.
+// fp32 queries, for the weights' sums: three bf16 terms of a query's coordinates,
+// cut off one after another as they come from LDS, against keys that are exact in
+// bf16.  Two chunks of four floats make a step of 16 coordinates.
 template <int D_>
-struct MxF32 : F32<D_> {
-    using P = F32<D_>;
+struct Mx3 {
     static constexpr int D = D_;
-    static constexpr int kCodes = mx::Row<D>::kCodes, kScales = mx::Row<D>::kScales;
-    typedef typename P::frag frag;
+    typedef float elem;
+    typedef bf16x8_t frag;  // of a key
+    static constexpr int EPC = 4, CPR = D / 4, KK = D / 16, kMassResident = 2;
     typedef MxSrc Src;
     __device__ __forceinline__ static Src keys(const Args& a, const Segment& sg, long long row) {
         return mx_rows<D>(sg.K, a.KS, row);
     }
-    // Chunk 2 kk + h of a key: half a word of codes.
-    struct KeyAt {
-        const uint16_t* c;
-        const uint8_t* s;
-        int h;
-        __device__ __forceinline__ KeyAt(Src K, int row, int h_)
-            : c(reinterpret_cast<const uint16_t*>(K.c + (long long)row * kCodes)), s(K.s + (long long)row * kScales), h(h_) {}
-        template <int KK>
-        __device__ __forceinline__ frag operator()(std::integral_constant<int, KK>) const {
-            const unsigned w = c[2 * KK + h];
-            const float x = mx::scale(s[KK / 4]);
-            const mx::f32x2 lo = mx::pair_f32<0>(w, x), hi = mx::pair_f32<1>(w, x);
-            return frag{lo[0], lo[1], hi[0], hi[1]};
-        }
-    };
+    typedef typename Mx<D>::KeyAt KeyAt;
+    struct Query { frag t[3]; };
+    __device__ __forceinline__ static f32x16 dot(const Query& a, frag b, f32x16 c) {
+        dev::static_for<3>([&](auto tc) {  // the smallest term first
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.t[2 - decltype(tc)::value], b, c, 0, 0, 0);
+        });
+        return c;
+    }
 };
 
+}  // namespace
+
+// Rows of floats: chunks 4 kk + 2 h and the next of row lane % 32.
+template <int D_>
+struct RowAt<Mx3<D_>> {
+    using E = Mx3<D_>;
+    int k;
+    __device__ __forceinline__ explicit RowAt(int lane) {
+        const int r = lane & 31, h = lane >> 5;
+        k = r * E::D + ((2 * h) ^ swz<E>(r)) * E::EPC;
+    }
+    __device__ __forceinline__ RowAt opaque() const {
+        RowAt x = *this;
+        asm volatile("" : "+v"(x.k));
+        return x;
+    }
+    template <int KK>
+    __device__ __forceinline__ typename E::Query frag(const float* stage, std::integral_constant<int, KK>) const {
+        f32x4 x[2];
+        dev::static_for<2>([&](auto ec) {
+            constexpr int e = decltype(ec)::value;
+            x[e] = *reinterpret_cast<const f32x4*>(stage + (k ^ ((4 * KK + e) * E::EPC)));
+        });
+        typename E::Query q;
+        dev::static_for<3>([&](auto tc) {
+            dev::u32x4 w;
+            dev::static_for<4>([&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                float a = x[i / 2][2 * (i % 2)], b = x[i / 2][2 * (i % 2) + 1];
+                w[i] = mx::cut(a, b);
+                x[i / 2][2 * (i % 2)] = a;
+                x[i / 2][2 * (i % 2) + 1] = b;
+            });
+            q.t[decltype(tc)::value] = __builtin_bit_cast(bf16x8_t, w);
+        });
+        return q;
+    }
+};
+
+namespace {
 }  // namespace
 }  // namespace attend
 
@@ -131,7 +166,7 @@ hipError_t launch_attend_tile_mx(const attend::Args& a, const attend::Segment& s
 hipError_t launch_attend_tile_mass_mx(const attend::Args& a, int dtype, float* part, int parts, hipStream_t s) {
     using namespace attend;
     if (dtype == BKV_BF16) return a.D == 128 ? tile_mass<Mx<128>>(a, part, parts, s) : tile_mass<Mx<64>>(a, part, parts, s);
-    return a.D == 128 ? tile_mass<MxF32<128>>(a, part, parts, s) : tile_mass<MxF32<64>>(a, part, parts, s);
+    return a.D == 128 ? tile_mass<Mx3<128>>(a, part, parts, s) : tile_mass<Mx3<64>>(a, part, parts, s);
 }
 
 }  // namespace bkv

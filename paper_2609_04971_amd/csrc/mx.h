@@ -59,5 +59,14 @@ __device__ __forceinline__ dev::u32x4 eight_bf16(unsigned codes, float scale) {
                       pair_bf16<3>(codes, scale)};
 }
 
+// The high halves of two floats, and what they leave of them: three cuts take all
+// of their 24 bits, as bf16 terms.
+__device__ __forceinline__ unsigned cut(float& x, float& y) {
+    const unsigned w = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+    x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+    return w;
+}
+
 }  // namespace mx
 }  // namespace bkv
