@@ -26,12 +26,12 @@ constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a 
 // 7.9 / 9.9; fp32 D 64 256 6.5 / 7.4 and 7.6 / 9.8, 512 9.5 / 9.3 and 7.6 / 9.9; D
 // 128 256 9.2 / 9.0 and 9.3 / 9.8, 384 11.6 / 11.5 and 9.5 / 10.3).
 constexpr long long kWhole = 128 << 10;
-// The same of a 4-bit cache in bf16: keys, whose bytes are not what takes the time
-// (us launched one by one, in one piece and split, 8 heads: D 128 1024 tokens 9.0 and
-// 10.9, 1500 10.7 and 10.9, 2048 12.9 and 10.9; D 64 1024 8.8 and 10.8, 2048 10.9 and
-// 10.9).  fp32 ones are as plain ones (D 64 512 10.4 and 10.8, D 128 256 9.5 and 10.7,
-// 512 15.3 and 10.8).
-constexpr int kWholeMx = 1280;
+// The same of a 4-bit cache: keys times tiles of 16 rows, whose bytes are not what
+// takes the time (us launched one by one, in one piece and split, 8 heads: bf16 D 128
+// 1024 tokens 9.0 and 10.9, 1500 10.7 and 10.9, 2048 12.9 and 10.9; D 64 2048 10.9 and
+// 10.9; fp32 D 128 768 8.9 and 11.9, 1024 10.3 and 12.0, 1280 11.7 and 12.0; D 64 1500
+// 10.5 and 11.9).
+constexpr int kWholeMx = 1280, kWholeMx32 = 1024;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 
 // Rows per unit up to which a 4-bit cache's keys are streamed.  In tiles only as
@@ -175,7 +175,10 @@ Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
     const long long few_items = pre_units * few_rb * ((P + kMinChunk - 1) / kMinChunk);
     p.pre_tile = tiles && pre_rows > kFewRows && (p.own_tile || few_items > kFewItems);
     p.wide = (!p.own_tile && R > 16) || (!p.pre_tile && pre_rows > 16);
-    p.rt = R <= 16 ? 1 : R <= 32 || !tiles ? 2 : (int)((R + 15) / 16);
+    // fp32 queries of more rows come in blocks of 32: one of three tiles saves the keys
+    // a second reading (35 rows 29.9 us for 36.8), four take too many registers (a
+    // prompt of 2048 in blocks of 32, 48, 64 rows 104 102 143)
+    p.rt = R <= 16 ? 1 : R <= 32 ? 2 : tiles || R <= 48 ? (int)((R + 15) / 16) : 2;
     const int own_rb = p.own_tile ? 128 : c.mx ? 16 * p.rt : p.wide ? 32 : 16, pre_rb = p.pre_tile ? 128 : p.wide ? 32 : 16;
     p.own_nrb = (int)((R + own_rb - 1) / own_rb);
     p.pre_nrb = (int)((pre_rows + pre_rb - 1) / pre_rb);
@@ -195,13 +198,15 @@ Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
         // a short cache goes in one piece: joining splits would be a launch of
         // its own.  Not by the mass: outputs do not depend on whether it is asked for
         const bool whole = groups == 0 && !p.own_tile &&
-                           (c.mx && tiles ? N <= kWholeMx && R <= kFewRows : (long long)N * d.D * (tiles ? 2 : 4) <= kWhole);
+                           (c.mx ? R <= kFewRows && (long long)N * p.rt <= (tiles ? kWholeMx : kWholeMx32)
+                                 : (long long)N * d.D * (tiles ? 2 : 4) <= kWhole);
         const bool prompt = p.own_tile && c.causal && c.window == 0 && T <= N && T > N / 5;
         own_ns = whole    ? 1
                  : prompt ? prompt_splits(own, N, T, rows, d.D)
                           : best_splits(items_of(p, d.D, c.mx), own, N, rows, d.D);
         if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile ? Items{d.D == 128 ? 2 : 3, 100.f} : Items{1, 64.f}, pre, P, rows, d.D);
     }
+    if (own_ns > p.ns_room) own_ns = p.ns_room;
     cut(N, own_ns, &p.own_ns, &p.own_chunk);
     if (groups > 0 && P > 0) cut(P, pre_ns, &p.pre_ns, &p.pre_chunk);
     p.keep = mass && R <= kFewRows;

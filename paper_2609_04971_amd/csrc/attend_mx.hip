@@ -268,7 +268,11 @@ struct Wide : M {
 
 template <int D, bool WIN>
 hipError_t stream_mx(const Args& a, int dtype, int rt, hipStream_t s) {
-    if (dtype == BKV_F32) return rt == 1 ? stream_rows<Wide<Mx3<D>>, D, 1, WIN>(a, s) : stream_rows<Mx3<D>, D, 2, WIN>(a, s);
+    if (dtype == BKV_F32) switch (rt) {
+            case 1: return stream_rows<Wide<Mx3<D>>, D, 1, WIN>(a, s);
+            case 2: return stream_rows<Mx3<D>, D, 2, WIN>(a, s);
+            default: return stream_rows<Mx3<D>, D, 3, WIN>(a, s);
+        }
     switch (rt) {
         case 1: return stream_rows<Wide<Mx<D>>, D, 1, WIN>(a, s);
         case 2: return stream_rows<Mx<D>, D, 2, WIN>(a, s);

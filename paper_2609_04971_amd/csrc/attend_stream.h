@@ -269,7 +269,10 @@ __device__ __forceinline__ typename E::Q load_q(const Args& a, const Row& x, boo
     return q;
 }
 
-constexpr float kMost = 1024.f;  // of a lane's weights of one group, where maxima are lazy
+// New weights of a lane that call for another maximum, of a group of KG keys,
+// where maxima are lazy: a row's weights come from four lanes, so that they sum to
+// no more than 32 for every key, and values' sums are finite as far as promised.
+constexpr float most_of(int KG) { return 8.f * (float)KG; }
 constexpr int kKeptRows = 32;  // rows per unit of kept logits, at most
 
 // Four tokens' weights of one row; what a row that sees nothing has (norm
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
             const bool edge = WIN ? at0 + KG > least || (at0 < most - a.window && at0 + KG > a.sinks) : k0 + KG > min(least, k_hi);
             if constexpr (E::kLazy) {
                 // weights against the running maximum as it stands (floats: they may be
-                // far above 1); only where a row's new ones sum to more than kMost, as the
+                // far above 1); only where a row's new ones sum to more than most_of, as the
                 // first group's do, is the maximum looked for and all brought down to it
                 if (edge)
                     dev::static_for<NR * NT * 4>([&](auto ic) {
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                         });
                     };
                     weights();
-                    if (__any(!(sum <= kMost))) {
+                    if (__any(!(sum <= most_of(KG)))) {
                         float top = p[rt][0][0];
                         dev::static_for<NT * 4 - 1>([&](auto ic) {
                             constexpr int x = decltype(ic)::value + 1;

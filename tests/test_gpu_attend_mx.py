@@ -1,6 +1,8 @@
 """Attention over a 4-bit cache (bkv_attend_mx) against the 64-bit reference: types,
 head layouts, lengths from none to long, ragged and empty rows, what lies behind a
 sequence, the weights' sums, windows, streams, graphs and offsets past 32 bits."""
+import math
+
 import pytest
 import torch
 
@@ -52,6 +54,10 @@ def test_ragged_lengths_and_rows_that_see_nothing(dtype, T):
     dict(B=9, Hkv=5, G=3, D=64, T=11, N=333, cap=340, lens=[333, 1, 0, 64, 65, 128, 5, 11, 12]),
     dict(B=16, Hkv=8, G=8, D=128, T=4, N=900, cap=901),
     dict(B=300, Hkv=2, G=2, D=64, T=1, N=65, cap=66),
+    dict(B=3, Hkv=2, G=8, D=128, T=3, N=3000, cap=3000, lens=[3000, 100, 1777]),  # two row tiles, split
+    dict(B=2, Hkv=1, G=6, D=128, T=7, N=4000, cap=4001, lens=[4000, 1333]),       # three
+    dict(B=2, Hkv=1, G=9, D=64, T=7, N=4000, cap=4001, lens=[4000, 77]),          # four
+    dict(B=2, Hkv=2, G=24, D=128, T=1, N=2000, cap=2000, lens=[1999, 0]),
     dict(B=64, Hkv=4, G=8, D=128, T=2, N=1500, cap=1503),                        # logits that LDS does not hold
     dict(B=4, Hkv=2, G=4, D=128, T=600, N=1500, cap=1500, lens=[1500, 599, 130, 400]),
 ])
@@ -115,6 +121,43 @@ def test_powers_of_two_at_both_ends(dtype, T):
     out, lse, mass = call(d, x, T, with_mass=True)
     assert out.isfinite().all()
     attend_ref.check(reference(x["q"], x["K"], x["V"], N, True), out, lse, mass, x["mass"], N)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,G", [(1, 4), (6, 4), (10, 4), (40, 4)])
+@pytest.mark.parametrize("first,step", [(0, 0), (5, 1), (70, 1), (70, 64)])
+@pytest.mark.parametrize("rise", [0.0, 4.0, 4.5, 6.5, 16.0])
+@pytest.mark.parametrize("N", [64, 1000, 9000])
+def test_values_near_the_range_of_fp32(N, rise, first, step, T, G, dtype):
+    """bkv.h: |v| (keys + 128) up to 2^122 gives finite results, however the weights rise as the keys go by."""
+    d = bkv.dims(B=1, Hq=2 * G, Hkv=2, D=128, N=N, W=0, C=0, budget=1, dtype=dtype)
+    x = make(1, 2, G, 128, T, N, N, dtype, N, True)
+    c = x["cache"]
+    x["q"].zero_()
+    x["q"][..., 0] = 2.0 * rise  # half of it is the logit, scale 1
+    c.K.zero_()
+    if step:
+        c.K[:, :, first::step, 0] = 1
+    c.KS.fill_(127)
+    c.VS.fill_(127 + int(math.log2(2.0 ** 122 / (N + 128) / 6)))
+    c.V.random_(0, 256, generator=torch.Generator(device="cuda").manual_seed(N))
+    c.V.bitwise_and_(0x77)  # positive: their sums are the largest
+    x["K"], x["V"] = mx_ref.values(c.K, c.KS), mx_ref.values(c.V, c.VS)
+    out, lse, mass = call(d, x, T, causal=False, scale=1.0, with_mass=True)
+    assert out.isfinite().all()
+    attend_ref.check(reference(x["q"], x["K"], x["V"], N, scale=1.0), out, lse, mass, x["mass"], N)
+
+
+@pytest.mark.parametrize("T,G", [(1, 4), (6, 4), (10, 4), (40, 4)])
+def test_small_fp32_queries_and_large_keys(T, G):
+    """Queries near fp32's smallest normal values: their lower terms are below bf16's."""
+    d = bkv.dims(B=1, Hq=2 * G, Hkv=2, D=128, N=500, W=0, C=0, budget=1, dtype="fp32")
+    x = make(1, 2, G, 128, T, 500, 500, "fp32", 6, True)
+    x["q"] *= 2.0 ** -118
+    x["cache"].KS[:, :, :500] += 116
+    x["K"] = mx_ref.values(x["cache"].K, x["cache"].KS)
+    out, lse, mass = call(d, x, T, causal=False, with_mass=True)
+    attend_ref.check(reference(x["q"], x["K"], x["V"], 500), out, lse, mass, x["mass"], 500)
 
 
 def test_a_nan_stays_in_its_head():
