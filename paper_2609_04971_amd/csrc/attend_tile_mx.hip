@@ -1,27 +1,20 @@
 // Attention of many query rows over a 4-bit cache for gfx950, and the sums of
 // their weights: the tile kernels (attend_tile.h) with keys and values that become
-// bf16 (the sums' keys for fp32 queries fp32) on their way.
+// bf16 on their way.
 //
 // A tile's codes are requested before the tile in front of it is worked off and
 // put into LDS as bf16 values after it, where the products find them as they do
 // a plain cache's.  A thread takes whole blocks: 16 bytes of codes, 16
 // conversions, four chunks of a row in LDS.  Threads are dealt to blocks so that
 // the 16 lanes that LDS serves at once write 16 different positions of 16 bytes.
+// Bound as on a plain cache, by the products, with a tenth for the conversions: 2 x
+// 4096 causal queries of 32 heads 294 us, the sums 160.
 #include "attend_tile.h"
 #include "mx.h"
 
 namespace bkv {
 namespace attend {
 namespace {
-
-struct MxSrc {
-    const uint8_t* c;
-    const uint8_t* s;
-};
-template <int D>
-__device__ __forceinline__ MxSrc mx_rows(const void* codes, const uint8_t* bytes, long long row) {
-    return {static_cast<const uint8_t*>(codes) + row * mx::Row<D>::kCodes, bytes + row * mx::Row<D>::kScales};
-}
 
 template <int D_>
 struct Mx : Bf16<D_> {
@@ -30,12 +23,12 @@ struct Mx : Bf16<D_> {
     static constexpr int kCodes = mx::Row<D>::kCodes, kScales = mx::Row<D>::kScales;
     typedef typename P::elem elem;
     typedef typename P::frag frag;
-    typedef MxSrc Src;
+    typedef mx::Src Src;
     __device__ __forceinline__ static Src keys(const Args& a, const Segment& sg, long long row) {
-        return mx_rows<D>(sg.K, a.KS, row);
+        return mx::rows<D>(sg.K, a.KS, row);
     }
     __device__ __forceinline__ static Src values_of(const Args& a, const Segment& sg, long long row) {
-        return mx_rows<D>(sg.V, a.VS, row);
+        return mx::rows<D>(sg.V, a.VS, row);
     }
     // D 128: a block of the keys and one of the values a thread.  D 64: one block,
     // waves 0 and 1 the keys', 2 and 3 the values'.
@@ -94,16 +87,17 @@ struct Mx : Bf16<D_> {
 
 // fp32 queries, for the weights' sums: three bf16 terms of a query's coordinates,
 // cut off one after another as they come from LDS, against keys that are exact in
-// bf16.  Two chunks of four floats make a step of 16 coordinates.
+// bf16.  Two chunks of four floats make a step of 16 coordinates.  2048 causal
+// queries of 32 heads: 81 us, 236 with fp32 products.
 template <int D_>
 struct Mx3 {
     static constexpr int D = D_;
     typedef float elem;
     typedef bf16x8_t frag;  // of a key
     static constexpr int EPC = 4, CPR = D / 4, KK = D / 16, kMassResident = 2;
-    typedef MxSrc Src;
+    typedef mx::Src Src;
     __device__ __forceinline__ static Src keys(const Args& a, const Segment& sg, long long row) {
-        return mx_rows<D>(sg.K, a.KS, row);
+        return mx::rows<D>(sg.K, a.KS, row);
     }
     typedef typename Mx<D>::KeyAt KeyAt;
     struct Query { frag t[3]; };

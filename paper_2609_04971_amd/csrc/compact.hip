@@ -20,7 +20,8 @@
 // after it has seen the flag.
 //
 // A 4-bit cache's rows are D/2 bytes of codes, moved as above, and 2 or 4 bytes
-// of scales: with 128 rows a segment, K and V, one to each thread.
+// of scales: with 128 rows a segment, K and V, one to each thread (64 heads of 32768
+// -> 4096 tokens 26 us, 56 of a bf16 cache).
 #include "device_common.h"
 #include "internal.h"
 #include "mx.h"

@@ -139,7 +139,9 @@ __device__ __forceinline__ void move_rows(char* K, char* V, const int* src, cons
     }
 }
 
-// The same moves of a 4-bit cache's scales, head h.
+// The same moves of a 4-bit cache's scales, head h.  Four bytes here and there:
+// 4608 heads of 4096 -> 3584 on masses that no eviction has seen take 246 us, 70 of
+// them for these, whose stores meet parts of nearly every line.
 template <int NT>
 __device__ __forceinline__ void move_scales(const MassArgs& a, int h, const int* src, const int* dst, int n) {
     for (int e = threadIdx.x; e < 2 * n; e += NT) {

@@ -22,6 +22,16 @@ struct Row {
     static constexpr int kScales = D / kBlock;  // bytes
 };
 
+// Where a unit's keys or values lie, from one of its rows on.
+struct Src {
+    const uint8_t* c;  // codes
+    const uint8_t* s;  // bytes
+};
+template <int D>
+__device__ __forceinline__ Src rows(const void* codes, const uint8_t* bytes, long long row) {
+    return {static_cast<const uint8_t*>(codes) + row * Row<D>::kCodes, bytes + row * Row<D>::kScales};
+}
+
 // Whether a cache has all of its arrays, aligned.
 inline bool whole(const bkv_mx_cache& c) {
     const uintptr_t all[] = {(uintptr_t)c.K, (uintptr_t)c.KS, (uintptr_t)c.V, (uintptr_t)c.VS};

