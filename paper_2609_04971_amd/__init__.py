@@ -428,7 +428,7 @@ def attend_window(d: Dims, q, K, V, out, ws, window: int, sinks: int = 0, lens=N
     dev = _device_of(q, "q")
     T, _, (qp, kp, vp, lp, op, ep, _) = _attend_args(d, q, K, V, out, lens, lse, None, dev)
     wp, wn = _arg_ws(ws, dev)
-    st = lib().bkv_attend_window(ctypes.byref(d), qp, T, kp, vp, window, sinks, lp, scale, op, ep, wp, wn,
+    st = lib().bkv_attend_window(ctypes.byref(d), qp, T, kp, vp, int(window), int(sinks), lp, scale, op, ep, wp, wn,
                                  torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_window")
 
@@ -486,7 +486,7 @@ def _mx_args(d, k, v, cache, at):
     shape = (B, d.Hkv, T, d.D)
     kp = None if k is None else _arg(k, shape, dt, "k", dev)
     vp = None if v is None else _arg(v, shape, dt, "v", dev)
-    first, ap = (0, _arg(at, (B,), torch.int32, "at", dev)) if isinstance(at, torch.Tensor) else (at, None)
+    first, ap = (0, _arg(at, (B,), torch.int32, "at", dev)) if isinstance(at, torch.Tensor) else (int(at), None)
     return kp, vp, T, first, ap, _arg_mx(d, cache, dev), torch._C._cuda_getCurrentRawStream(dev)
 
 
@@ -513,7 +513,7 @@ def attend_mx(d: Dims, q, cache: MxCache, out, ws, lens=None, lse=None, mass=Non
     T, _, (qp, lp, op, ep, mp) = _attend_rows(d, q, out, lens, lse, mass, dev)
     cp = _arg_mx(d, cache, dev)
     wp, wn = _arg_ws(ws, dev)
-    st = lib().bkv_attend_mx(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, ctypes.byref(cp), window, sinks, lp, scale,
+    st = lib().bkv_attend_mx(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, ctypes.byref(cp), int(window), int(sinks), lp, scale,
                              op, ep, mp, wp, wn, torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_mx")
 

@@ -84,9 +84,9 @@ struct Items {
     int resident;  // at once on a compute unit, as far as that shares anything
     float around;  // keys in the time that an item costs around its own
 };
-Items items_of(const Plan& p, int D, bool mx) {
-    if (p.own_tile) return {D == 128 ? 2 : 3, 100.f};
-    return {mx && (p.rt == 3 || (p.rt == 4 && D == 64)) ? 2 : 1, 64.f};
+Items items_of(bool tile, int rt, int D) {  // rt: row tiles, of a 4-bit cache
+    if (tile) return {D == 128 ? 2 : 3, 100.f};
+    return {rt == 3 || (rt == 4 && D == 64) ? 2 : 1, 64.f};
 }
 int best_splits(Items it, long long base, int n, long long rows, int D) {
     constexpr float kRound[4] = {0.f, 1.f, 1.7f, 2.4f};
@@ -203,15 +203,15 @@ Plan make_plan(const bkv_dims& d, int T, const Shape& c) {
         const bool prompt = p.own_tile && c.causal && c.window == 0 && T <= N && T > N / 5;
         own_ns = whole    ? 1
                  : prompt ? prompt_splits(own, N, T, rows, d.D)
-                          : best_splits(items_of(p, d.D, c.mx), own, N, rows, d.D);
-        if (groups > 0 && P > 0) pre_ns = best_splits(p.pre_tile ? Items{d.D == 128 ? 2 : 3, 100.f} : Items{1, 64.f}, pre, P, rows, d.D);
+                          : best_splits(items_of(p.own_tile, c.mx ? p.rt : 0, d.D), own, N, rows, d.D);
+        if (groups > 0 && P > 0) pre_ns = best_splits(items_of(p.pre_tile, 0, d.D), pre, P, rows, d.D);
     }
     if (own_ns > p.ns_room) own_ns = p.ns_room;
     cut(N, own_ns, &p.own_ns, &p.own_chunk);
     if (groups > 0 && P > 0) cut(P, pre_ns, &p.pre_ns, &p.pre_chunk);
     p.keep = mass && R <= kFewRows;
     if (mass && !p.keep && tiles && R <= kRegRows)
-        cut(d.N, best_splits({1, 64.f}, (long long)d.B * d.Hkv, d.N, 0, d.D), &p.mass_ns, &p.mass_chunk);
+        cut(d.N, best_splits(items_of(false, 0, d.D), (long long)d.B * d.Hkv, d.N, 0, d.D), &p.mass_ns, &p.mass_chunk);
     size_t off = 0;
     p.part_o = off;
     if (p.ns_room > 1) off = up(off + sizeof(float) * (size_t)rows * p.ns_room * d.D, kAlign);
@@ -306,7 +306,8 @@ bkv_status run(const bkv_dims* d, const Call& c, hipStream_t stream) {
     if (p.end > 0 && (!ws || ws_bytes < p.end || !aligned(ws))) return BKV_ERR_WORKSPACE;
     if (p.own_ns + p.pre_ns > p.ns_room) return BKV_ERR_WORKSPACE;  // (the room covers every N and P)
     // what is written, then what is only read; of the last head the tokens that are there
-    const size_t row = (size_t)d->D * (d->dtype == BKV_BF16 ? 2 : 4), cache_row = c.mx ? (size_t)d->D / 2 : row, queries = (size_t)d->B * d->Hq * T;
+    const size_t row = (size_t)d->D * (d->dtype == BKV_BF16 ? 2 : 4), cache_row = c.mx ? (size_t)d->D / 2 : row;
+    const size_t queries = (size_t)d->B * d->Hq * T;
     auto tokens = [](size_t units, size_t n, size_t cap) { return n > 0 ? (units - 1) * cap + n : 0; };
     const size_t own_tokens = tokens((size_t)d->B * d->Hkv, d->N, d->N_cap);
     const size_t pre_tokens = groups > 0 ? tokens((size_t)groups * d->Hkv, P, P_cap) : 0;

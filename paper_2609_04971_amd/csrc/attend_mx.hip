@@ -204,7 +204,8 @@ struct Mx3 : Mx<D> {
             const bf16x8_t a = P::template coordinate<dd>(v);
             dev::static_for<NR * kTerms>([&](auto rc) {
                 constexpr int rt = decltype(rc)::value / kTerms, t = kTerms - 1 - decltype(rc)::value % kTerms;
-                o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, w[rt][t]), o[rt][dd], 0, 0, 0);
+                const bf16x8_t b = __builtin_bit_cast(bf16x8_t, w[rt][t]);
+                o[rt][dd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, o[rt][dd], 0, 0, 0);
             });
         });
     }

@@ -430,14 +430,16 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     E::logits(p[rt], kr, q[rt]);
                 });
             E::load_k(kr, K, key(k0 + KG * kWaves), last, off, lane);
-            const bool edge = WIN ? at0 + KG > least || (at0 < most - a.window && at0 + KG > a.sinks) : k0 + KG > min(least, k_hi);
+            const bool edge = WIN ? at0 + KG > least || (at0 < most - a.window && at0 + KG > a.sinks)
+                                  : k0 + KG > min(least, k_hi);
             if constexpr (E::kLazy) {
                 // weights against the running maximum as it stands (floats: they may be
                 // far above 1); only where a row's new ones sum to more than most_of, as the
                 // first group's do, is the maximum looked for and all brought down to it
                 if (edge)
                     dev::static_for<NR * NT * 4>([&](auto ic) {
-                        constexpr int rt = decltype(ic)::value / (NT * 4), ti = decltype(ic)::value / 4 % NT, i = decltype(ic)::value % 4;
+                        constexpr int rt = decltype(ic)::value / (NT * 4), ti = decltype(ic)::value / 4 % NT,
+                                      i = decltype(ic)::value % 4;
                         const int j = at0 + 16 * ti + 4 * g + i;
                         if (j >= min(lim[rt], WIN ? most : k_hi) || (WIN && j < lim[rt] - a.window && j >= a.sinks))
                             p[rt][ti][i] = -INFINITY;
@@ -449,10 +451,11 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                             constexpr int ti = decltype(tc)::value;
                             const int at = k0 + 16 * ti + 4 * g;
                             if (at >= k_hi) return;  // a group may end behind the rows' room
+                            const f32x4 l = p[rt][ti] * a.scale2;
                             if (keep == kKeepLds)
-                                *(lds_f32x4*)(s_l + ((16 * rt + col) * lds_stride + (at - k_lo))) = p[rt][ti] * a.scale2;
+                                *(lds_f32x4*)(s_l + ((16 * rt + col) * lds_stride + (at - k_lo))) = l;
                             else
-                                *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = p[rt][ti] * a.scale2;
+                                *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = l;
                         });
                     f32x4 e[NT];
                     float sum;
@@ -483,45 +486,45 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                     dev::static_for<NT>([&](auto tc) { p[rt][decltype(tc)::value] = e[decltype(tc)::value]; });
                 });
             } else {
-            dev::static_for<NR>([&](auto rc) {
-                constexpr int rt = decltype(rc)::value;
-                float top = kLowest;
-                dev::static_for<NT * 4>([&](auto ic) {
-                    constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-                    float l = p[rt][ti][i] * a.scale2;
-                    if constexpr (WIN) {
-                        const int j = at0 + 16 * ti + 4 * g + i;
-                        if (edge && (j >= min(lim[rt], most) || (j < lim[rt] - a.window && j >= a.sinks))) l = -INFINITY;
-                    } else if (edge && k0 + 16 * ti + 4 * g + i >= min(lim[rt], k_hi)) {
-                        l = -INFINITY;
-                    }
-                    p[rt][ti][i] = l;
-                    top = fmaxf(top, l);
-                });
-                if (keep && 16 * rt + col < sg.rows)  // a kept unit is one row block
-                    dev::static_for<NT>([&](auto tc) {
-                        constexpr int ti = decltype(tc)::value;
-                        const int at = k0 + 16 * ti + 4 * g;
-                        if (keep == kKeepLds)
-                            *(lds_f32x4*)(s_l + ((16 * rt + col) * lds_stride + (at - k_lo))) = p[rt][ti];
-                        else
-                            *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = p[rt][ti];
+                dev::static_for<NR>([&](auto rc) {
+                    constexpr int rt = decltype(rc)::value;
+                    float top = kLowest;
+                    dev::static_for<NT * 4>([&](auto ic) {
+                        constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                        float l = p[rt][ti][i] * a.scale2;
+                        if constexpr (WIN) {
+                            const int j = at0 + 16 * ti + 4 * g + i;
+                            if (edge && (j >= min(lim[rt], most) || (j < lim[rt] - a.window && j >= a.sinks))) l = -INFINITY;
+                        } else if (edge && k0 + 16 * ti + 4 * g + i >= min(lim[rt], k_hi)) {
+                            l = -INFINITY;
+                        }
+                        p[rt][ti][i] = l;
+                        top = fmaxf(top, l);
                     });
-                top = fmaxf(top, dev::shfl_xor_f(top, 16));
-                top = fmaxf(top, dev::shfl_xor_f(top, 32));
-                if (__any(top > m[rt])) {
-                    const float mn = fmaxf(m[rt], top), f = exp2_hw(m[rt] - mn);
-                    m[rt] = mn;
-                    z[rt] *= f;
-                    dev::static_for<DV>([&](auto dc) { o[rt][decltype(dc)::value] *= f; });
-                }
-                dev::static_for<NT * 4>([&](auto ic) {
-                    constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
-                    const float e = exp2_hw(p[rt][ti][i] - m[rt]);
-                    p[rt][ti][i] = e;
-                    z[rt] += e;
+                    if (keep && 16 * rt + col < sg.rows)  // a kept unit is one row block
+                        dev::static_for<NT>([&](auto tc) {
+                            constexpr int ti = decltype(tc)::value;
+                            const int at = k0 + 16 * ti + 4 * g;
+                            if (keep == kKeepLds)
+                                *(lds_f32x4*)(s_l + ((16 * rt + col) * lds_stride + (at - k_lo))) = p[rt][ti];
+                            else
+                                *reinterpret_cast<f32x4*>(glob + (long long)(16 * rt + col) * a.lstride + at) = p[rt][ti];
+                        });
+                    top = fmaxf(top, dev::shfl_xor_f(top, 16));
+                    top = fmaxf(top, dev::shfl_xor_f(top, 32));
+                    if (__any(top > m[rt])) {
+                        const float mn = fmaxf(m[rt], top), f = exp2_hw(m[rt] - mn);
+                        m[rt] = mn;
+                        z[rt] *= f;
+                        dev::static_for<DV>([&](auto dc) { o[rt][decltype(dc)::value] *= f; });
+                    }
+                    dev::static_for<NT * 4>([&](auto ic) {
+                        constexpr int ti = decltype(ic)::value / 4, i = decltype(ic)::value % 4;
+                        const float e = exp2_hw(p[rt][ti][i] - m[rt]);
+                        p[rt][ti][i] = e;
+                        z[rt] += e;
+                    });
                 });
-            });
             }
             if constexpr (E::kLazy) {
                 E::template values<NR>(o, vr, p, [&](auto hc) __attribute__((always_inline)) {
