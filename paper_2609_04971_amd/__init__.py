@@ -10,6 +10,7 @@ and if it is not built that first use raises ImportError.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import NamedTuple
 
@@ -348,6 +349,18 @@ def _arg(t, shape, dtype, name, dev):
     raise ValueError(f"{name} is on GPU {t.get_device()}, the current device is {dev}")
 
 
+def _i32(x, name):
+    """x as a C int32, which ctypes would cut any other integer down to."""
+    if type(x) is not int:
+        try:
+            x = operator.index(x)
+        except TypeError:
+            raise ValueError(f"{name} must be an integer, got {x!r}") from None
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name} must fit 32 bits, got {x}")
+    return x
+
+
 def _device_of(t, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
@@ -425,10 +438,11 @@ def attend_window(d: Dims, q, K, V, out, ws, window: int, sinks: int = 0, lens=N
     """attend() where query t, the cache's token p = len - T + t, sees the tokens
     j <= p with j > p - window or j < sinks.  The workspace is that of
     attend_workspace(d, T)."""
+    window, sinks = _i32(window, "window"), _i32(sinks, "sinks")
     dev = _device_of(q, "q")
     T, _, (qp, kp, vp, lp, op, ep, _) = _attend_args(d, q, K, V, out, lens, lse, None, dev)
     wp, wn = _arg_ws(ws, dev)
-    st = lib().bkv_attend_window(ctypes.byref(d), qp, T, kp, vp, int(window), int(sinks), lp, scale, op, ep, wp, wn,
+    st = lib().bkv_attend_window(ctypes.byref(d), qp, T, kp, vp, window, sinks, lp, scale, op, ep, wp, wn,
                                  torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_window")
 
@@ -476,6 +490,8 @@ def _arg_mx(d, cache, dev):
 
 
 def _mx_args(d, k, v, cache, at):
+    each = isinstance(at, torch.Tensor)
+    first = 0 if each else _i32(at, "at")
     t, name = (k, "k") if k is not None else (v, "v")
     if t is None:
         raise ValueError("k or v is required")
@@ -486,7 +502,7 @@ def _mx_args(d, k, v, cache, at):
     shape = (B, d.Hkv, T, d.D)
     kp = None if k is None else _arg(k, shape, dt, "k", dev)
     vp = None if v is None else _arg(v, shape, dt, "v", dev)
-    first, ap = (0, _arg(at, (B,), torch.int32, "at", dev)) if isinstance(at, torch.Tensor) else (int(at), None)
+    ap = _arg(at, (B,), torch.int32, "at", dev) if each else None
     return kp, vp, T, first, ap, _arg_mx(d, cache, dev), torch._C._cuda_getCurrentRawStream(dev)
 
 
@@ -509,11 +525,12 @@ def attend_mx(d: Dims, q, cache: MxCache, out, ws, lens=None, lse=None, mass=Non
               causal: bool = False, window: int = 0, sinks: int = 0):
     """attend() over a 4-bit cache; q and out have the dims' type.  window > 0: as
     attend_window() (then causal, and without mass)."""
+    window, sinks = _i32(window, "window"), _i32(sinks, "sinks")
     dev = _device_of(q, "q")
     T, _, (qp, lp, op, ep, mp) = _attend_rows(d, q, out, lens, lse, mass, dev)
     cp = _arg_mx(d, cache, dev)
     wp, wn = _arg_ws(ws, dev)
-    st = lib().bkv_attend_mx(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, ctypes.byref(cp), int(window), int(sinks), lp, scale,
+    st = lib().bkv_attend_mx(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, ctypes.byref(cp), window, sinks, lp, scale,
                              op, ep, mp, wp, wn, torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_mx")
 

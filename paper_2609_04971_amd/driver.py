@@ -89,6 +89,7 @@ class PeriodicEviction:
             raise ValueError("cache is 'plain' or 'mx'")
         if cache == "mx" and compaction == "fill" and mode != "mass":
             raise ValueError("the scoring modes compact a 4-bit cache in order")
+        window, sinks = bkv._i32(window, "window"), bkv._i32(sinks, "sinks")
         if window < 0 or sinks < 0:
             raise ValueError("window and sinks are not negative")
         if window and (not attention or mode == "mass"):
