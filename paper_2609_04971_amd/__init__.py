@@ -419,6 +419,7 @@ def attend_shared(d: Dims, q, PK, PV, K, V, out, ws, P: int | None = None, p_len
     """attend() for groups of consecutive sequences that share a prefix PK, PV
     [groups,Hkv,P_cap,D], of which the first P tokens are valid (default: all;
     p_lens [groups] int32: ragged).  mass collects the own tokens' weights."""
+    P = None if P is None else _i32(int(P), "P")
     dev = _device_of(q, "q")
     if not isinstance(PK, torch.Tensor) or PK.dim() != 4:
         raise ValueError("PK must be a tensor [groups, Hkv, P_cap, D]")
@@ -429,7 +430,7 @@ def attend_shared(d: Dims, q, PK, PV, K, V, out, ws, P: int | None = None, p_len
     pl = None if p_lens is None else _arg(p_lens, (groups,), torch.int32, "p_lens", dev)
     wp, wn = _arg_ws(ws, dev)
     st = lib().bkv_attend_shared(ctypes.byref(d), ATTEND_CAUSAL if causal else 0, qp, T, groups, pk, pv,
-                                 P_cap if P is None else int(P), P_cap, pl, kp, vp, lp, scale, op, ep, mp, wp, wn,
+                                 P_cap if P is None else P, P_cap, pl, kp, vp, lp, scale, op, ep, mp, wp, wn,
                                  torch._C._cuda_getCurrentRawStream(dev))
     _check(st, "bkv_attend_shared")
 

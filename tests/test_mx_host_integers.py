@@ -1,5 +1,5 @@
-"""Positions and windows that are no 32-bit integers, without a GPU: ctypes would cut
-them down to others (2**32 + 5 to 5), so the binding and the driver refuse them."""
+"""Positions, windows and prefixes that are no 32-bit integers, without a GPU: ctypes would
+cut them down to others (2**32 + 5 to 5), so the binding and the driver refuse them."""
 import numpy as np
 import pytest
 import torch
@@ -37,3 +37,10 @@ def test_windows(name, bad):
 @pytest.mark.parametrize("good", [0, 7, -1, True, np.int32(7), np.int64(-3), 2 ** 31 - 1, -2 ** 31])
 def test_integers_of_any_kind_pass(good):
     assert bkv._i32(good, "x") == int(good) and type(bkv._i32(good, "x")) in (int, bool)
+
+
+@pytest.mark.parametrize("bad", [2 ** 31, -2 ** 31 - 1, 2 ** 32, 2 ** 32 + 5])
+def test_prefixes(bad):
+    q = torch.zeros(2, 8, 1, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="^P must"):
+        bkv.attend_shared(DIMS, q, q, q, q, q, q, None, P=bad)
