@@ -418,8 +418,11 @@ bkv_status bkv_evict_mass(const bkv_dims* d, int32_t flags, void* K, void* V, fl
  * at most 125, and rounds every coordinate over 2^e to the nearest code, ties to
  * the even one (magnitudes past 6 to 6): a coordinate of 2^e or more is off by at
  * most a fifth of itself, a smaller one by at most 2^e / 4 (e past -124; e is below
- * 125 wherever a <= 7 2^125).  Values are exact in bf16.
- * Rows written otherwise need bytes of 3 to 252; others give unspecified values. */
+ * 125 wherever a <= 7 2^125).  Values are exact in bf16.  A block with an infinity
+ * or a NaN among its coordinates is stored as byte 255 and codes 0: byte 255
+ * stands for NaNs in all 32, whatever the codes.
+ * Rows written otherwise need bytes of 3 to 252, or 255; others give unspecified
+ * values. */
 typedef struct {
     uint8_t* K;
     uint8_t* KS;

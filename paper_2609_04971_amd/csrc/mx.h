@@ -15,6 +15,10 @@ constexpr int kBlock = 32;
 // e + 127: subnormal coordinates fall below half of the smallest code, and the
 // largest code stays finite.
 constexpr int kLeast = 3, kMost = 252;
+// The byte of a block that held an infinity or a NaN: the conversions make NaNs of
+// all of its codes.  There is no code for either, and a number in their place
+// would hide them.
+constexpr unsigned kNan = 255;
 
 template <int D>
 struct Row {
@@ -43,12 +47,13 @@ inline bool whole(const bkv_mx_cache& c) {
 // 2^e of a block's byte.
 __device__ __forceinline__ float scale(unsigned byte) { return __uint_as_float(byte << 23); }
 
-// The byte of a block whose largest magnitude is `top`: the smallest e with top
-// <= 7 2^e.  7 rounds to 6, no worse than the half step between 4 and 6, and
-// from there on the next power is the closer one.
-__device__ __forceinline__ unsigned scale_byte(float top) {
-    const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 2;
-    return (unsigned)min(max(e, kLeast), kMost);
+// The byte of a block whose largest magnitude has the bits `top`: the smallest e
+// with top <= 7 2^e.  7 rounds to 6, no worse than the half step between 4 and 6,
+// and from there on the next power is the closer one.  Magnitudes are ordered as
+// their bits are, infinities and then NaNs last.
+__device__ __forceinline__ unsigned scale_byte(unsigned top) {
+    const int e = (int)((top + 0x1fffffu) >> 23) - 2;
+    return top >= 0x7f800000u ? kNan : (unsigned)min(max(e, kLeast), kMost);
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -1,9 +1,9 @@
 // Rows into the 4-bit cache and out of it (bkv_store_mx, bkv_load_mx), gfx950.
 //
 // A block's byte comes from its largest magnitude, a maximum over the four
-// lanes that hold its 32 coordinates; its codes are those magnitudes over 2^e
-// (exact) rounded to the nearest code, ties to the even one, which the
-// conversion instruction does.  Both ways a thread takes eight coordinates of
+// lanes that hold its 32 coordinates, taken on the bits, which a NaN does not get
+// lost in; its codes are those magnitudes over 2^e (exact) rounded to the nearest
+// code, ties to the even one, which the conversion instruction does.  Both ways a thread takes eight coordinates of
 // K and of V: bound by the bytes (36 x 8 heads of 4096 rows of D 128, 0.76 GB: 124
 // us stored, 6.1 TB/s, 108 loaded, 7.1; one row of 4608 heads 3.3 each).
 #include "internal.h"
@@ -34,8 +34,8 @@ __device__ __forceinline__ long long cache_row(const MxArgs& a, unsigned r) {
 }
 
 template <int CTRL>
-__device__ __forceinline__ float dpp_max(float v) {
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, false)));
+__device__ __forceinline__ unsigned dpp_max(unsigned v) {
+    return max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false));
 }
 
 // The eight coordinates at p as floats.
@@ -73,8 +73,8 @@ __global__ __launch_bounds__(kThreads) void store_kernel(MxArgs a) {
         dev::static_for<2>([&](auto sc) {
             constexpr int s = decltype(sc)::value;
             if (!a.in[s]) return;
-            float top = 0.f;
-            dev::static_for<kPer>([&](auto e) { top = fmaxf(top, fabsf(x[s][decltype(e)::value])); });
+            unsigned top = 0;
+            dev::static_for<kPer>([&](auto e) { top = max(top, __float_as_uint(x[s][decltype(e)::value]) & 0x7fffffffu); });
             top = dpp_max<0x4e>(dpp_max<0xb1>(top));  // the block's four lanes
             const unsigned byte = mx::scale_byte(top);
             unsigned w = 0;
@@ -82,6 +82,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(MxArgs a) {
                 constexpr int k = decltype(e)::value;
                 w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[s][2 * k], x[s][2 * k + 1], mx::scale(byte), k);
             });
+            if (byte == mx::kNan) w = 0;
             reinterpret_cast<unsigned*>(a.codes[s])[to * TPR + c] = w;
             if (c % 4 == 0) a.scales[s][to * (TPR / 4) + c / 4] = (uint8_t)byte;
         });
