@@ -326,11 +326,18 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     // those of the item's keys, [R][chunk + kPadL]
     extern __shared__ __attribute__((aligned(16))) float dyn[];
     __shared__ float s_m[kWaves][16], s_z[kWaves][16], s_norm[kKeptRows];
-    // rows of more tiles than two, or one in several terms, leave their queries
-    // there, a lane's part each
-    constexpr bool kQLds = RT > 2 || (RT > 1 && E::kTerms > 1);
+    // rows of more tiles than two, or of two in several terms, leave their queries
+    // in LDS, a lane's part each.  Two tiles, beside which logits may be kept, lend
+    // them the place of the waves' sums, which are put there when every key is done
+    constexpr bool kQLds = RT > 2 || (RT > 1 && E::kTerms > 1), kQLent = kQLds && RT == 2;
     static_assert(RT <= kWaves, "a wave loads one tile's queries");
-    __shared__ typename E::Q s_q[kQLds ? RT : 1][kQLds ? 64 : 1];
+    typedef typename E::Q Query;
+    __shared__ Query s_q_own[kQLds && !kQLent ? RT * 64 : 1];
+    // (items of two tiles have 16 rows in one: a.o_rows)
+    static_assert(!kQLent || RT * 64 * sizeof(Query) <= sizeof(float) * kWaves * 16 * DP);
+    Query* const s_q = kQLent ? reinterpret_cast<Query*>(dyn) : s_q_own;
+    // items that may keep logits there have to leave kLdsRoom of a half of a compute unit's LDS
+    static_assert(16 * RT > kKeptRows || kLdsRoom + sizeof s_m + sizeof s_z + sizeof s_norm + sizeof s_q_own <= 80 * 1024);
     lds_float* const s_o = (lds_float*)dyn;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -365,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         const bool valid = rr < sg.rows;
         const Row x = decode_row(a, unit, sg.seqs, valid ? rr : 0);
         if constexpr (kQLds) {
-            if (wave == rt) s_q[kQLds ? rt : 0][lane] = load_q<E, D>(a, x, valid, g);
+            if (wave == rt) s_q[rt * 64 + lane] = load_q<E, D>(a, x, valid, g);
         } else {
             q[rt] = load_q<E, D>(a, x, valid, g);
         }
@@ -401,7 +408,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
     auto query = [&](auto rc) __attribute__((always_inline)) {
         if constexpr (kQLds) {
             asm volatile("" ::: "memory");  // or all of them would be kept in registers
-            return s_q[decltype(rc)::value][lane];
+            return s_q[decltype(rc)::value * 64 + lane];
         } else {
             return q[decltype(rc)::value];
         }
@@ -546,6 +553,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
         walk(std::integral_constant<int, RT>{});
     }
 
+    if constexpr (kQLent) __syncthreads();  // no wave needs the queries any more
     // join the waves, one row tile at a time
     dev::static_for<RT>([&](auto rc) {
         constexpr int rt = decltype(rc)::value;
