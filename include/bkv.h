@@ -450,8 +450,9 @@ bkv_status bkv_load_mx(const bkv_dims* d, const bkv_mx_cache* cache, int32_t T, 
 /* bkv_attend (flags, lens, lse, mass, scale, workspace and all else as there) over
  * a 4-bit cache, with the keys and values that its rows stand for; dtype of the
  * dims: that of q and out, bf16 or fp32.  Products and weights are rounded as on a
- * plain cache of that type; fp32 queries and weights enter the matrix cores with
- * all of their bits, as three bf16 terms.
+ * plain cache of that type (bf16: weights as two bf16 terms where G T <= 32, else
+ * as one); fp32 queries and weights enter the matrix cores with all of their
+ * bits, as three bf16 terms.
  *   window  0: none, and sinks is not used.  >= 1: queries see what they see in
  *           bkv_attend_window; then T > 1 needs BKV_ATTEND_CAUSAL, and mass has
  *           to be NULL (BKV_ERR_INVALID).

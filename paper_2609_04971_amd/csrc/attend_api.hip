@@ -27,10 +27,16 @@ constexpr int kMinChunk = 128;      // keys: one group of 32 for each wave of a 
 // 128 256 9.2 / 9.0 and 9.3 / 9.8, 384 11.6 / 11.5 and 9.5 / 10.3).
 constexpr long long kWhole = 128 << 10;
 // The same of a 4-bit cache: keys times tiles of 16 rows, whose bytes are not what
-// takes the time (us launched one by one, in one piece and split, 8 heads: bf16 D 128
-// 1024 tokens 9.0 and 10.9, 1500 10.7 and 10.9, 2048 12.9 and 10.9; D 64 2048 10.9 and
-// 10.9; fp32 D 128 768 8.9 and 11.9, 1024 10.3 and 12.0, 1280 11.7 and 12.0; D 64 1500
-// 10.5 and 11.9).
+// takes the time.  The limits lie between where the two break even captured, in
+// front, and one by one (us captured / one by one, in one piece and split, 8 heads,
+// 4 rows: bf16 D 128 1024 tokens 8.5 / 9.0 and 8.2 / 11.6, 1280 9.7 / 10.1 and 8.6 /
+// 11.7, 1536 10.8 / 11.2 and 8.4 / 11.7; D 64 1280 7.9 / 8.3 and 7.9 / 11.6, 2048 10.4 /
+// 10.8 and 7.7 / 11.7; fp32 D 128 768 8.4 / 8.9 and 8.7 / 11.5, 1024 9.9 / 10.3 and 8.7 /
+// 11.6, 1280 11.3 / 11.7 and 9.3 / 11.6; D 64 1024 7.9 / 8.4 and 8.0 / 11.5.  32 rows: bf16
+// D 128 512 9.3 / 9.6 and 9.3 / 11.6, 640 10.1 / 10.5 and 9.8 / 11.7, 768 11.1 / 11.4 and
+// 9.9 / 11.6; D 64 640 7.9 / 8.2 and 8.3 / 11.6; fp32 D 64 512 9.2 / 9.4 and 8.7 / 11.7; D
+// 128 256 10.1 / 10.2 and 10.8 / 11.7, 384 11.7 / 11.9 and 10.9 / 11.8, and behind both ways
+// at 512, 13.4 / 13.5 and 11.0 / 11.8, where three terms of two tiles bound).
 constexpr int kWholeMx = 1280, kWholeMx32 = 1024;
 constexpr int kFewRows = 32;        // rows per unit up to which keys are streamed and the logits kept for the mass
 

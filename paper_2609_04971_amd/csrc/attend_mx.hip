@@ -9,7 +9,7 @@
 // Few rows are bound by the bytes (4608 heads of 3584 tokens, 4 rows, 2.3 GB: 375
 // us, 6.1 TB/s, where the loads alone take 368; one of 65536 tokens, 8 heads: 16.6),
 // from about 16 rows on the products and conversions take as long (512 heads of
-// 8000 tokens, 32 rows: 125 us, 557 MB; 4000 tokens, 40 rows: 74, 278 MB).
+// 8000 tokens, 32 rows: 125 us, 557 MB; 4000 tokens, 40 rows: 70, 278 MB).
 #include "attend_stream.h"
 #include "mx.h"
 
@@ -121,6 +121,9 @@ struct Mx : Bf16<D> {
         next(std::integral_constant<int, 0>{});
         products<NR>(o, x, p);
     }
+    // (us, weights of three and four row tiles as one term and as two: 35 rows of 8 x 4
+    // heads of up to 16001 tokens 26.3 29.5, 63 rows 36.9 43.0; 40 rows of 512 heads of
+    // 4000 70 85)
     template <int NR, int RT>
     __device__ static void products(f32x4 (&o)[RT][kDV], const typename P::V& v, const f32x4 (&p)[RT][kTiles]) {
         P::template values<NR, RT, (RT > 2)>(o, v, p);

@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kThreads) void stream_kernel(Args a) {
                                   : k0 + KG > min(least, k_hi);
             if constexpr (E::kLazy) {
                 // weights against the running maximum as it stands (floats: they may be
-                // far above 1); only where a row's new ones sum to more than most_of, as the
+                // far above 1); only where a lane's new ones sum to more than most_of, as the
                 // first group's do, is the maximum looked for and all brought down to it
                 if (edge)
                     dev::static_for<NR * NT * 4>([&](auto ic) {

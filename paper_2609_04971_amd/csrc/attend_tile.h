@@ -165,7 +165,10 @@ struct Bf16 {
     // but the products bound this kernel (us, one term and two: prompt of 2 x 4096
     // with weights 425 531, 500 queries against 24001 105 156, 5 drafted tokens 46
     // 50, 64 samples of a prompt 115 121).  Normalisers summed from the rounded
-    // weights: 2.16e-3, at 440 and 119 us.
+    // weights: 2.16e-3, at 440 and 119 us.  Windows and 4-bit caches have the same
+    // errors and the same choice (one term and two: a window's prompt of 16384 938
+    // 1310, its chunks of 500 at D 64 53 71; prompt of 2 x 4096 over a 4-bit cache 267
+    // 368, at D 64 153 220).
     struct Weights { frag p[4]; };
     template <int I>  // weight I % 16 of key tile I / 16
     __device__ __forceinline__ static void put(Weights& w, std::integral_constant<int, I>, float e) {
@@ -334,7 +337,7 @@ __device__ __forceinline__ void tile_step(State<E>& st, const RowAt<E>& at, cons
 // prompt of 16384 of 32 heads that sees 4096 and 4 tokens 940 us (1.02 PFLOP/s of
 // what is seen).  Of D 64, windows and 4-bit caches fit three workgroups a compute
 // unit once their registers are held to it (a window's prompt of 8192 95 us, 108
-// with two; 2 x 4096 over a 4-bit cache 153, 162).
+// with two; 2 x 4096 over a 4-bit cache 153, three of its registers spilled, 162).
 template <class E, bool WIN>
 constexpr int tile_resident() { return E::D == 64 && (WIN || E::kStages > 0) ? 3 : 2; }
 template <class E, bool WIN>
